@@ -420,6 +420,164 @@ l2kv_status l2kv_length_order(const int32_t* lens, int32_t n_seq, int32_t* order
 size_t l2kv_decode_ragged_workspace_bytes(int32_t n_seq, int32_t Hq, int64_t max_len, int32_t D);
 
 /* ---------------------------------------------------------------------------
+ * Before and beside the compressed cache: rotary positions, attention of whole
+ * prompts, drafted trees.
+ *
+ * Tokens of several sequences are packed: sequence s = tokens
+ * offsets[s] .. offsets[s+1]-1 of every tensor (DEVICE int64 [n_seq+1],
+ * ascending, first entry 0; sequences may be empty; tokens behind the last one are
+ * neither read nor written).  As above, contents of device arrays cannot be
+ * checked on the host: the kernels force what they read into the buffers.
+ * Q, K and V of a token are heads of D contiguous elements, a token's heads side by
+ * side; the *_stride arguments are the ELEMENTS between two tokens (>= heads*D,
+ * a multiple of 16 bytes), so the three may be parts of one projection's output.
+ * ------------------------------------------------------------------------ */
+
+/* Which two elements of a head are turned together, of the first rot_dim = R:
+ * HALF (i, i + R/2), INTERLEAVED (2i, 2i + 1), i = 0 .. R/2-1. */
+typedef enum { L2KV_ROTARY_HALF = 0, L2KV_ROTARY_INTERLEAVED = 1 } l2kv_rotary_layout;
+
+/* Frequencies for contexts `factor` times longer than the original:
+ * PLAIN    f_i = base^(-2i/R)
+ * LINEAR   f_i / factor (positions are interpolated)
+ * BASE     base raised to base * factor^(R/(R-2)): the last pair slows down by
+ *          the factor, the first not at all
+ * BANDS    pairs that turn at least `high` times over original_len keep f_i, those
+ *          that turn at most `low` times take f_i / factor, between them a
+ *          linear ramp in the number of turns */
+typedef enum { L2KV_ROTARY_PLAIN = 0, L2KV_ROTARY_LINEAR = 1, L2KV_ROTARY_BASE = 2, L2KV_ROTARY_BANDS = 3 } l2kv_rotary_scaling;
+
+/*
+ * The angles per position of the R/2 pairs, in radians (host function, to be
+ * copied to the device once).  rot_dim: a multiple of 16, 16..256; base > 0;
+ * factor > 0 is not read for PLAIN, original_len > 0 and 0 <= low < high for BANDS only.
+ * Errors: NULL, SHAPE.
+ */
+l2kv_status l2kv_rotary_freqs(int32_t rot_dim, double base, l2kv_rotary_scaling scaling, double factor,
+                              int64_t original_len, double low, double high, double* h_freqs);
+
+/*
+ * Rotary positions on the way into the cache: l2kv_stream_append for any number
+ * of tokens per sequence and one layer, with the rotation in it.  Token t at
+ * position p = positions[t] has the pairs (x1, x2) of every query and key head
+ * turned by theta = p * freqs[i]:
+ *     x1' = amplitude * (x1 cos theta - x2 sin theta)
+ *     x2' = amplitude * (x2 cos theta + x1 sin theta)
+ * in fp64, rounded once; elements from rot_dim on, and V, are copied.
+ *   Q, K, V    in : [total_tokens] x Hq, Hkv, Hkv heads; Q may be NULL together
+ *                   with Qr (keys and values only; Hq and q_stride are not read)
+ *   positions  in : DEVICE int32 [total_tokens], of either sign
+ *   freqs      in : DEVICE double [rot_dim/2]
+ *   Qr        out : [total_tokens][Hq][D], dense
+ *   Kc, Vc    out : [Hkv][total_slots][D]; norms_c, pos_c [Hkv][total_slots]:
+ *                   squared norm of the key AS STORED, summed as in
+ *                   l2kv_norms, and positions[t]
+ *   token_offsets, slot_offsets, lens_in: the j-th token of sequence s goes to
+ *                   slot lens_in[s] + j of the sequence; a token that finds its
+ *                   sequence's slots occupied is not stored (its queries are turned
+ *                   all the same).  lens_out[s] = lens_in[s] + tokens stored; may be
+ *                   NULL (calls for further layers), must not be lens_in.
+ *                   All four NULL, n_seq not read: token t goes to row t of every
+ *                   plane (prompts, packed as they are; nodes of drafted trees).
+ * Errors: NULL (also for one of the three arrays without the others), SHAPE
+ * (rot_dim not a multiple of 16 or above D, layout, total_slots < total_tokens
+ * without offsets, amplitude not finite, more than 2^24-1 workgroups of four tokens, ...), DTYPE, ALIGN, LAUNCH.
+ */
+l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                               int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                               int64_t v_stride, const int32_t* positions, const double* freqs, int32_t rot_dim,
+                               l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                               const int64_t* token_offsets, const int64_t* slot_offsets,
+                               const int32_t* lens_in, int32_t* lens_out, int64_t total_slots, void* Qr,
+                               void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream);
+
+/*
+ * Causal attention of packed prompts (Eq. 2 with the mask of a decoder): query i of
+ * the n_q tokens of sequence s attends to its rows j <= i + n_kv - n_q, that is,
+ * the last query sees all n_kv rows and the first ones of a prompt, or all that
+ * was in the cache before, are seen by every query.  n_kv may be larger than n_q (a further chunk of
+ * a prompt, over a cache that may have been compressed) or smaller (the
+ * first queries then see nothing).  A query that sees no row, or whose scores are all
+ * minus infinity, gets zeros.  Rows that a query does not see have no effect on
+ * it, whatever they hold.
+ *   Q    in : [total_q] x Hq heads
+ *   K, V in : KV head h starts h * kv_head_stride elements in; sequence s has rows
+ *             kv_offsets[s] on, n_kv = kv_lens[s] of them, or up to
+ *             kv_offsets[s+1] where kv_lens is NULL (always at most up to there).
+ *             total_rows: rows that can be read from the start of every head.
+ *             Planes [Hkv][total_rows][D]: kv_head_stride = total_rows * D.
+ *             Caches [B][Hkv][T][D]: kv_head_stride = T*D, kv_offsets[b] = b*Hkv*T,
+ *             kv_lens[b] <= T, total_rows = ((B-1)*Hkv + 1) * T.
+ *   max_kv  : an upper bound of all n_kv (sizes the workspace and the
+ *             decomposition; rows beyond it are still attended to)
+ *   O   out : [total_q][Hq][D], dense, of type dt
+ *   workspace: l2kv_prompt_attn_workspace_bytes(...) bytes, 16-aligned; contents
+ *             irrelevant before and after.  May be NULL where that is 0.
+ * Arithmetic: fp32 scores, softmax and sums; for bf16, products on the matrix unit
+ * with the softmax weights rounded to bf16 (their sum is that of the rounded ones) and O
+ * rounded once.
+ * Errors: NULL, SHAPE (Hq % Hkv != 0, Hq/Hkv > 8 -- > 4 for D = 256 --, ...), DTYPE, WORKSPACE, ALIGN, LAUNCH.
+ */
+l2kv_status l2kv_prompt_attn(const void* Q, const void* K, const void* V, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
+                             int32_t Hkv, int32_t D, int64_t total_q, int64_t q_stride, const int64_t* q_offsets,
+                             int64_t total_rows, int64_t kv_head_stride, const int64_t* kv_offsets,
+                             const int32_t* kv_lens, int64_t max_kv, float scale, void* O, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+size_t l2kv_prompt_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv,
+                                        int32_t D, l2kv_dtype dt);
+
+/*
+ * Attention of drafted tokens over a slot cache: decode attention with several
+ * queries per sequence that also see one another as a mask allows (a tree of
+ * drafts: a node sees its ancestors and itself).  Node i of sequence s attends to the
+ * lens[s] occupied slots and to those nodes j of its sequence whose bit is set:
+ *     mask[node][j / 32] >> (j % 32) & 1
+ * with i's own bit the caller's to set.  The nodes' keys and values are not in the
+ * cache but in Kt, Vt (l2kv_rotary_append without offsets puts them there, with
+ * positions by their depth); l2kv_stream_append_path moves those that are
+ * accepted.  A node that sees no row gets zeros; what a node does not see has no effect on it.
+ *   Q      in : [total_nodes] x Hq heads, node_offsets DEVICE int64 [n_seq+1]
+ *   Kc, Vc in : one layer's planes, kv_head_stride, total_slots, slot_offsets as
+ *               kv_head_stride, total_rows, kv_offsets of l2kv_prompt_attn
+ *   lens   in : DEVICE int32 [n_seq], at most as many as the sequence has slots; 0 allowed
+ *   max_len   : an upper bound of all lens (as max_kv of l2kv_prompt_attn; 0 allowed)
+ *   Kt, Vt in : [Hkv][total_nodes][D]
+ *   mask   in : DEVICE uint32 [total_nodes][mask_words], mask_words >= 1; nodes of a
+ *               sequence beyond 32 * mask_words are not seen
+ *   O     out : [total_nodes][Hq][D], dense, of type dt
+ *   workspace : l2kv_tree_attn_workspace_bytes(...), as for l2kv_prompt_attn
+ * Arithmetic and errors: as l2kv_prompt_attn.
+ */
+l2kv_status l2kv_tree_attn(const void* Q, const void* Kc, const void* Vc, const void* Kt, const void* Vt, l2kv_dtype dt,
+                           int32_t n_seq, int32_t Hq, int32_t Hkv, int32_t D, int64_t total_nodes, int64_t q_stride,
+                           const int64_t* node_offsets, const uint32_t* mask, int32_t mask_words,
+                           int64_t total_slots, int64_t kv_head_stride, const int64_t* slot_offsets,
+                           const int32_t* lens, int64_t max_len, float scale, void* O, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+size_t l2kv_tree_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_nodes, int64_t max_len,
+                                      int32_t D, l2kv_dtype dt);
+
+/*
+ * The accepted tokens of a drafted tree join the cache, all layers in one call:
+ * rows path[s][0 .. path_lens[s]-1] of sequence s's nodes, in that order, go to slots
+ * lens_in[s], lens_in[s]+1, ... of every plane, K, V, norm and token id, and
+ * lens_out[s] = lens_in[s] + the number stored (at most as many as there is room
+ * for, and none for a sequence without nodes).  An entry outside the sequence's nodes
+ * is forced into them.
+ *   Kt, Vt in : [n_planes][total_nodes][D]; norms_t, pos_t [n_planes][total_nodes]
+ *   path   in : DEVICE int32 [n_seq][max_path]; path_lens DEVICE int32 [n_seq], 0..max_path
+ * lens_out must not be lens_in.  Errors: NULL, SHAPE, DTYPE, ALIGN, LAUNCH.
+ */
+l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t,
+                                    l2kv_dtype dt, int32_t n_planes, int32_t n_seq, int32_t D, int64_t total_nodes,
+                                    const int64_t* node_offsets, const int32_t* path, int32_t max_path,
+                                    const int32_t* path_lens, const int64_t* slot_offsets, int64_t total_slots,
+                                    const int32_t* lens_in, int32_t* lens_out, void* Kc, void* Vc,
+                                    float* norms_c, int32_t* pos_c, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Attention-loss analysis (Sec. 3, Eq. 5-7)
  *
  * When m of the T cached pairs of a head are dropped, the attention loss L^m is

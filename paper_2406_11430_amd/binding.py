@@ -21,6 +21,8 @@ CALLS_PATH = os.path.join(_HERE, "l2kv_calls.so")
 
 L2KV_F32, L2KV_BF16 = 0, 1
 L2KV_KEEP_LOWEST, L2KV_KEEP_HIGHEST = 0, 1
+L2KV_ROTARY_HALF, L2KV_ROTARY_INTERLEAVED = 0, 1
+L2KV_ROTARY_PLAIN, L2KV_ROTARY_LINEAR, L2KV_ROTARY_BASE, L2KV_ROTARY_BANDS = 0, 1, 2, 3
 L2KV_OK = 0
 
 # name -> (restype, argtypes); mirrors include/l2kv.h declaration by declaration
@@ -73,6 +75,30 @@ SIGNATURES = {
                                           C.c_void_p]),
     "l2kv_length_order": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
     "l2kv_decode_ragged_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int64, C.c_int32]),
+    "l2kv_rotary_freqs": (C.c_int, [C.c_int32, C.c_double, C.c_int, C.c_double, C.c_int64, C.c_double,
+                                    C.c_double, C.c_void_p]),
+    "l2kv_rotary_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32,
+                                     C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                     C.c_void_p, C.c_int32, C.c_int, C.c_double, C.c_int32, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "l2kv_prompt_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32,
+                                   C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
+                                   C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_void_p,
+                                   C.c_void_p, C.c_size_t, C.c_void_p]),
+    "l2kv_prompt_attn_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                                      C.c_int32, C.c_int]),
+    "l2kv_tree_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                 C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                 C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p,
+                                 C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
+                                 C.c_void_p]),
+    "l2kv_tree_attn_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                                    C.c_int32, C.c_int]),
+    "l2kv_stream_append_path": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32,
+                                          C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                          C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "l2kv_norm_ranks": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t,
                                   C.c_void_p]),
     "l2kv_norm_ranks_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
@@ -486,6 +512,148 @@ def l2kv_length_order(lens: torch.Tensor, order: torch.Tensor, stream=None) -> N
     n_seq = lens.numel()
     _i32(lens, n_seq), _i32(order, n_seq)
     _check("l2kv_length_order", lib().l2kv_length_order(_ptr(lens), n_seq, _ptr(order), _stream(stream)))
+
+
+# ------------------------------------------------------------ rotary positions, prompts, drafted trees
+def l2kv_rotary_freqs(rot_dim: int, base: float = 10000.0, scaling: int = L2KV_ROTARY_PLAIN, factor: float = 1.0,
+                      original_len: int = 0, low: float = 1.0, high: float = 32.0) -> torch.Tensor:
+    """Angles per position of the rot_dim/2 pairs, a float64 tensor on the host (copy it to the device once)."""
+    freqs = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.float64)
+    _check("l2kv_rotary_freqs", lib().l2kv_rotary_freqs(int(rot_dim), float(base), int(scaling), float(factor),
+                                                       int(original_len), float(low), float(high), freqs.data_ptr()))
+    return freqs
+
+
+def _tokens(t: torch.Tensor):
+    """[tokens, heads, D] whose heads lie side by side, tokens any distance apart -> that distance in elements."""
+    if not t.is_cuda:
+        raise ValueError("l2kv works on device tensors only")
+    n, heads, D = t.shape
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise ValueError("l2kv needs the heads of a token side by side, got strides %s" % (t.stride(),))
+    return t.stride(0) if n > 1 else heads * D
+
+
+def l2kv_rotary_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor,
+                       freqs: torch.Tensor, Qr: Optional[torch.Tensor], Kc: torch.Tensor, Vc: torch.Tensor,
+                       norms_c: torch.Tensor, pos_c: torch.Tensor, token_offsets: Optional[torch.Tensor] = None,
+                       slot_offsets: Optional[torch.Tensor] = None, lens_in: Optional[torch.Tensor] = None,
+                       lens_out: Optional[torch.Tensor] = None, layout: int = L2KV_ROTARY_HALF,
+                       amplitude: float = 1.0, stream=None) -> None:
+    """Q ``[tokens, Hq, D]`` -> Qr (same shape, dense); K, V ``[tokens, Hkv, D]`` -> Kc, Vc ``[Hkv, total_slots, D]``,
+    norms_c, pos_c ``[Hkv, total_slots]``.  The tokens of Q, K and V may be any distance apart (parts of one projection)."""
+    _dev(positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, slot_offsets, lens_in, lens_out)
+    total, Hkv, D = K.shape
+    k_stride, v_stride = _tokens(K), _tokens(V)
+    Hq, q_stride = (0, 0) if Q is None else (Q.shape[1], _tokens(Q))
+    planes, total_slots, Dc = Kc.shape
+    assert V.shape == K.shape and V.dtype == K.dtype == Kc.dtype == Vc.dtype and Vc.shape == Kc.shape
+    assert (planes, Dc) == (Hkv, D) and norms_c.shape == (Hkv, total_slots) and norms_c.dtype == torch.float32
+    assert pos_c.shape == (Hkv, total_slots) and pos_c.dtype == torch.int32
+    if Q is not None:
+        assert Q.shape == (total, Hq, D) and Q.dtype == K.dtype
+        assert Qr is None or (Qr.shape == Q.shape and Qr.dtype == Q.dtype)
+    assert freqs.dtype == torch.float64
+    _i32(positions, total)
+    n_seq = 0
+    if token_offsets is not None:
+        n_seq = token_offsets.numel() - 1
+        _i64(token_offsets, n_seq + 1)
+        for t, check in ((slot_offsets, _i64), (lens_in, _i32), (lens_out, _i32)):
+            if t is not None:
+                check(t, n_seq + (check is _i64))
+    _check("l2kv_rotary_append", lib().l2kv_rotary_append(
+        _ptr(Q), _ptr(K), _ptr(V), _dtype_code(K), total, Hq, Hkv, D, q_stride, k_stride, v_stride, _ptr(positions),
+        _ptr(freqs), 2 * freqs.numel(), int(layout), float(amplitude), n_seq, _ptr(token_offsets), _ptr(slot_offsets),
+        _ptr(lens_in), _ptr(lens_out), total_slots, _ptr(Qr), _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c),
+        _stream(stream)))
+
+
+def _code(dtype) -> int:
+    return _dtype_code(torch.empty(0, dtype=dtype)) if isinstance(dtype, torch.dtype) else int(dtype)
+
+
+def l2kv_prompt_attn_workspace_bytes(n_seq: int, Hq: int, Hkv: int, total_q: int, max_kv: int, D: int, dtype) -> int:
+    return int(lib().l2kv_prompt_attn_workspace_bytes(int(n_seq), int(Hq), int(Hkv), int(total_q), int(max_kv), int(D), _code(dtype)))
+
+
+def l2kv_tree_attn_workspace_bytes(n_seq: int, Hq: int, Hkv: int, total_nodes: int, max_len: int, D: int, dtype) -> int:
+    return int(lib().l2kv_tree_attn_workspace_bytes(int(n_seq), int(Hq), int(Hkv), int(total_nodes), int(max_len), int(D), _code(dtype)))
+
+
+def _planes(K: torch.Tensor, V: torch.Tensor):
+    """Planes [Hkv, rows, D] or caches [B, Hkv, T, D] -> (Hkv, rows from the start of every head, elements between heads)."""
+    _dev(K, V)
+    assert V.shape == K.shape and V.dtype == K.dtype
+    if K.dim() == 4:
+        B, Hkv, T, D = K.shape
+        return Hkv, ((B - 1) * Hkv + 1) * T, T * D
+    Hkv, rows, D = K.shape
+    return Hkv, rows, rows * D
+
+
+def l2kv_prompt_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, q_offsets: torch.Tensor,
+                     kv_offsets: torch.Tensor, kv_lens: Optional[torch.Tensor], max_kv: int, O: torch.Tensor,
+                     workspace: Optional[torch.Tensor], scale: float = 0.0, stream=None) -> None:
+    """Q ``[total_q, Hq, D]`` (tokens any distance apart), K/V ``[Hkv, rows, D]`` or ``[B, Hkv, T, D]`` -> O ``[total_q, Hq, D]``
+    of Q's type.  Offsets are device int64 ``[n_seq + 1]`` (in rows; of a ``[B, Hkv, T, D]`` cache b*Hkv*T), kv_lens int32 or None."""
+    _dev(q_offsets, kv_offsets, kv_lens, O, workspace)
+    total_q, Hq, D = Q.shape
+    q_stride = _tokens(Q)
+    Hkv, rows, head_stride = _planes(K, V)
+    n_seq = q_offsets.numel() - 1
+    assert K.shape[-1] == D and K.dtype == Q.dtype == O.dtype and O.shape == Q.shape
+    _i64(q_offsets, n_seq + 1), _i64(kv_offsets, n_seq + 1)
+    if kv_lens is not None:
+        _i32(kv_lens, n_seq)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check("l2kv_prompt_attn", lib().l2kv_prompt_attn(
+        _ptr(Q), _ptr(K), _ptr(V), _dtype_code(Q), n_seq, Hq, Hkv, D, total_q, q_stride, _ptr(q_offsets), rows, head_stride,
+        _ptr(kv_offsets), _ptr(kv_lens), int(max_kv), float(scale), _ptr(O), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def l2kv_tree_attn(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, lens: torch.Tensor, slot_offsets: torch.Tensor,
+                   max_len: int, Kt: torch.Tensor, Vt: torch.Tensor, node_offsets: torch.Tensor, mask: torch.Tensor,
+                   O: torch.Tensor, workspace: Optional[torch.Tensor], scale: float = 0.0, stream=None) -> None:
+    """Q ``[nodes, Hq, D]``, Kc/Vc ``[Hkv, total_slots, D]`` or ``[B, Hkv, T, D]``, Kt/Vt ``[Hkv, nodes, D]``, mask
+    ``[nodes, words]`` int32 (bit j of a row: its node sees node j of its sequence) -> O ``[nodes, Hq, D]`` of Q's type."""
+    _dev(lens, slot_offsets, Kt, Vt, node_offsets, mask, O, workspace)
+    total, Hq, D = Q.shape
+    q_stride = _tokens(Q)
+    Hkv, slots, head_stride = _planes(Kc, Vc)
+    n_seq = node_offsets.numel() - 1
+    assert Kc.shape[-1] == D and Kc.dtype == Q.dtype == O.dtype and O.shape == Q.shape
+    assert Kt.shape == (Hkv, total, D) and Vt.shape == Kt.shape and Kt.dtype == Vt.dtype == Q.dtype
+    assert mask.dtype == torch.int32 and mask.dim() == 2 and mask.shape[0] == total
+    _i64(node_offsets, n_seq + 1), _i64(slot_offsets, n_seq + 1), _i32(lens, n_seq)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check("l2kv_tree_attn", lib().l2kv_tree_attn(
+        _ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(Kt), _ptr(Vt), _dtype_code(Q), n_seq, Hq, Hkv, D, total, q_stride, _ptr(node_offsets),
+        _ptr(mask), mask.shape[1], slots, head_stride, _ptr(slot_offsets), _ptr(lens), int(max_len), float(scale), _ptr(O),
+        _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def l2kv_stream_append_path(Kt: torch.Tensor, Vt: torch.Tensor, norms_t: torch.Tensor, pos_t: torch.Tensor,
+                            node_offsets: torch.Tensor, path: torch.Tensor, path_lens: torch.Tensor,
+                            slot_offsets: torch.Tensor, lens_in: torch.Tensor, lens_out: torch.Tensor,
+                            Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor,
+                            stream=None) -> None:
+    """Rows path ``[n_seq, max_path]`` (path_lens of each) of the nodes ``[n_planes, total_nodes, D]`` -> the next free slots."""
+    _dev(Kt, Vt, norms_t, pos_t, node_offsets, path, path_lens, slot_offsets, lens_in, lens_out, Kc, Vc, norms_c, pos_c)
+    n_planes, total, D = Kt.shape
+    n_seq, max_path = path.shape
+    planes, total_slots, Dc = Kc.shape
+    assert Vt.shape == Kt.shape and Vc.shape == Kc.shape and (planes, Dc) == (n_planes, D)
+    assert Kt.dtype == Vt.dtype == Kc.dtype == Vc.dtype
+    assert norms_t.shape == (n_planes, total) and pos_t.shape == (n_planes, total)
+    assert norms_c.shape == (n_planes, total_slots) and pos_c.shape == (n_planes, total_slots)
+    assert norms_t.dtype == norms_c.dtype == torch.float32 and pos_t.dtype == pos_c.dtype == torch.int32
+    _i64(node_offsets, n_seq + 1), _i64(slot_offsets, n_seq + 1), _i32(path, n_seq * max_path)
+    _i32(path_lens, n_seq), _i32(lens_in, n_seq), _i32(lens_out, n_seq)
+    _check("l2kv_stream_append_path", lib().l2kv_stream_append_path(
+        _ptr(Kt), _ptr(Vt), _ptr(norms_t), _ptr(pos_t), _dtype_code(Kt), n_planes, n_seq, D, total, _ptr(node_offsets),
+        _ptr(path), max_path, _ptr(path_lens), _ptr(slot_offsets), total_slots, _ptr(lens_in), _ptr(lens_out), _ptr(Kc),
+        _ptr(Vc), _ptr(norms_c), _ptr(pos_c), _stream(stream)))
 
 
 # ------------------------------------------------------------ attention-loss analysis

@@ -36,6 +36,8 @@ inline int elem_bytes(l2kv_dtype dt) { return dt == L2KV_F32 ? 4 : 2; }
 inline bool dim_ok(int32_t D, l2kv_dtype dt) { return D == 64 || D == 128 || (D == 256 && dt == L2KV_BF16); }
 // query heads per KV head the decode kernels are built for
 inline int32_t max_group(int32_t D) { return D == 256 ? 4 : 8; }
+// rotated part of a head: whole pieces of 8 elements in both halves
+inline bool rot_dim_ok(int32_t R, int32_t D) { return R >= 16 && R <= D && R % 16 == 0; }
 constexpr int64_t kMaxTokens = 0x7fffffffLL;          // token indices are int32
 constexpr int64_t kMaxHeads = 0x7fffffffLL;
 // smallest selection workspace the calls accept; the size query returns more where several
@@ -429,6 +431,180 @@ l2kv_status l2kv_length_order(const int32_t* lens, int32_t n_seq, int32_t* order
     if (lens == order) return L2KV_ERR_SHAPE;
     if (!aligned(lens, 4) || !aligned(order, 4)) return L2KV_ERR_ALIGN;
     return length_order_dispatch(lens, n_seq, 0, order, static_cast<hipStream_t>(stream));
+}
+
+/* ---- rotary positions, prompts, drafted trees ------------------------------ */
+
+l2kv_status l2kv_rotary_freqs(int32_t rot_dim, double base, l2kv_rotary_scaling scaling, double factor, int64_t original_len,
+                              double low, double high, double* h_freqs) {
+    if (h_freqs == nullptr) return L2KV_ERR_NULL;
+    if (!rot_dim_ok(rot_dim, 256) || !(base > 0.0) || !std::isfinite(base)) return L2KV_ERR_SHAPE;
+    const bool plain = scaling == L2KV_ROTARY_PLAIN, bands = scaling == L2KV_ROTARY_BANDS;
+    if (!plain && !bands && scaling != L2KV_ROTARY_LINEAR && scaling != L2KV_ROTARY_BASE) return L2KV_ERR_SHAPE;
+    if (!plain && (!(factor > 0.0) || !std::isfinite(factor))) return L2KV_ERR_SHAPE;
+    if (bands && (original_len <= 0 || !(low >= 0.0) || !(high > low) || !std::isfinite(high))) return L2KV_ERR_SHAPE;
+    const double R = rot_dim;
+    if (scaling == L2KV_ROTARY_BASE) base *= std::pow(factor, R / (R - 2.0));
+    for (int32_t i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / R);
+        if (scaling == L2KV_ROTARY_LINEAR) f /= factor;
+        if (bands) {
+            const double turns = static_cast<double>(original_len) * f / 6.283185307179586;
+            double keep = (turns - low) / (high - low);
+            keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        h_freqs[i] = f;
+    }
+    return L2KV_OK;
+}
+
+// Elements between two tokens of `heads` heads: no overlap, rows 16-byte aligned, no product of it beyond 63 bits.
+static l2kv_status check_token_stride(int64_t stride, int64_t tokens, int32_t heads, int32_t D, l2kv_dtype dt) {
+    if (stride < static_cast<int64_t>(heads) * D || stride > (int64_t{1} << 58) / tokens) return L2KV_ERR_SHAPE;
+    return (stride * elem_bytes(dt)) % 16 != 0 ? L2KV_ERR_ALIGN : L2KV_OK;
+}
+
+l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                               int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                               int64_t v_stride, const int32_t* positions, const double* freqs, int32_t rot_dim,
+                               l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                               const int64_t* token_offsets, const int64_t* slot_offsets,
+                               const int32_t* lens_in, int32_t* lens_out, int64_t total_slots, void* Qr,
+                               void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
+    if (K == nullptr || V == nullptr || positions == nullptr || freqs == nullptr || Kc == nullptr || Vc == nullptr ||
+        norms_c == nullptr || pos_c == nullptr || (Q == nullptr) != (Qr == nullptr))
+        return L2KV_ERR_NULL;
+    const bool packed = token_offsets == nullptr;
+    if ((slot_offsets == nullptr) != packed || (lens_in == nullptr) != packed || (packed && lens_out != nullptr))
+        return L2KV_ERR_NULL;
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (Q == nullptr) Hq = 0;
+    if (total_tokens <= 0 || total_tokens > kMaxTokens || Hkv <= 0 || Hkv > 65535 || Hq < 0 || Hq > 65535 || (Q != nullptr && Hq == 0) ||
+        !dim_ok(D, dt) || total_slots <= 0 || total_slots > kMaxTokens)
+        return L2KV_ERR_SHAPE;
+    if (!rot_dim_ok(rot_dim, D) || (layout != L2KV_ROTARY_HALF && layout != L2KV_ROTARY_INTERLEAVED) || !std::isfinite(amplitude))
+        return L2KV_ERR_SHAPE;
+    if (packed ? total_slots < total_tokens : (n_seq <= 0 || lens_in == lens_out)) return L2KV_ERR_SHAPE;
+    if (Q != nullptr)
+        if (l2kv_status st = check_token_stride(q_stride, total_tokens, Hq, D, dt); st != L2KV_OK) return st;
+    if (l2kv_status st = check_token_stride(k_stride, total_tokens, Hkv, D, dt); st != L2KV_OK) return st;
+    if (l2kv_status st = check_token_stride(v_stride, total_tokens, Hkv, D, dt); st != L2KV_OK) return st;
+    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Qr, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) ||
+        !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(positions, 4) || !aligned(freqs, 8) || !aligned(token_offsets, 8) ||
+        !aligned(slot_offsets, 8) || !aligned(lens_in, 4) || !aligned(lens_out, 4))
+        return L2KV_ERR_ALIGN;
+    RotaryArgs a = {};
+    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(K), a.V = static_cast<const char*>(V);
+    a.positions = positions, a.freqs = freqs;
+    a.token_off = token_offsets, a.slot_off = slot_offsets, a.lens_in = lens_in, a.lens_out = lens_out;
+    a.Qr = static_cast<char*>(Qr), a.Kc = static_cast<char*>(Kc), a.Vc = static_cast<char*>(Vc);
+    a.norms_c = norms_c, a.pos_c = pos_c;
+    a.total_tokens = total_tokens, a.total_slots = total_slots;
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.amplitude = amplitude, a.n_seq = n_seq, a.Hq = Hq, a.Hkv = Hkv, a.rot = rot_dim;
+    return rotary_dispatch(a, dt, D, layout == L2KV_ROTARY_INTERLEAVED, static_cast<hipStream_t>(stream));
+}
+
+// Sizes shared by the two attentions of many query rows, and by their workspaces.
+static bool rows_sizes_ok(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
+    if (!dtype_ok(dt) || !dim_ok(D, dt) || n_seq <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > max_group(D)) return false;
+    if (total_q <= 0 || total_q > kMaxTokens || max_kv < 0 || max_kv > kMaxTokens) return false;
+    // at most 2^24 workgroups of 256 lanes: a block has at least 4 tokens (32 rows, groups of 8)
+    return (total_q / 4 + n_seq) <= ((int64_t{1} << 24) - 1) / Hkv;
+}
+
+static size_t rows_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
+    if (!rows_sizes_ok(n_seq, Hq, Hkv, total_q, max_kv, D, dt)) return 0;
+    return rows_plan(n_seq, Hkv, Hq / Hkv, total_q, max_kv, D, dt).partial_bytes;
+}
+
+size_t l2kv_prompt_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
+                                        l2kv_dtype dt) {
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt);
+}
+
+size_t l2kv_tree_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_nodes, int64_t max_len, int32_t D,
+                                      l2kv_dtype dt) {
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_nodes, max_len, D, dt);
+}
+
+// The rest of both calls, from the checks that they share to the launch.
+static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, int64_t max_kv, float scale, void* workspace,
+                             size_t workspace_bytes, bool tree, void* stream) {
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (!rows_sizes_ok(a.n_seq, Hq, a.Hkv, a.total_q, max_kv, D, dt) || !std::isfinite(scale)) return L2KV_ERR_SHAPE;
+    if (a.total_rows <= 0 || a.total_rows > kMaxTokens || max_kv > a.total_rows || (!tree && max_kv == 0)) return L2KV_ERR_SHAPE;
+    // a head may start inside the rows of another ([B][Hkv][T][D] caches), but not at the same place
+    if (a.kv_head_stride < (a.Hkv > 1 ? D : 0) || a.kv_head_stride > (int64_t{1} << 58) / a.Hkv) return L2KV_ERR_SHAPE;
+    l2kv_status st = check_token_stride(a.q_stride, a.total_q, Hq, D, dt);
+    if (st == L2KV_ERR_SHAPE) return st;
+    a.G = Hq / a.Hkv;
+    const RowsPlan plan = rows_plan(a.n_seq, a.Hkv, a.G, a.total_q, max_kv, D, dt);
+    if (workspace_bytes < plan.partial_bytes || (workspace == nullptr && plan.partial_bytes > 0)) return L2KV_ERR_WORKSPACE;
+    if (st != L2KV_OK || (a.kv_head_stride * elem_bytes(dt)) % 16 != 0) return L2KV_ERR_ALIGN;
+    if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Kt, 16) || !aligned(a.Vt, 16) || !aligned(a.O, 16) ||
+        !aligned(a.q_off, 8) || !aligned(a.kv_off, 8) || !aligned(a.kv_lens, 4) || !aligned(a.mask, 4) || !aligned(workspace, 16))
+        return L2KV_ERR_ALIGN;
+    a.scale = (scale > 0.f ? scale : 1.0f / std::sqrt(static_cast<float>(D))) * 1.44269504f;      // powers of two from here on
+    a.partial = static_cast<float*>(workspace);
+    return rows_attn_dispatch(a, plan, D, dt, tree, static_cast<hipStream_t>(stream));
+}
+
+l2kv_status l2kv_prompt_attn(const void* Q, const void* K, const void* V, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
+                             int32_t Hkv, int32_t D, int64_t total_q, int64_t q_stride, const int64_t* q_offsets,
+                             int64_t total_rows, int64_t kv_head_stride, const int64_t* kv_offsets,
+                             const int32_t* kv_lens, int64_t max_kv, float scale, void* O, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    if (Q == nullptr || K == nullptr || V == nullptr || O == nullptr || q_offsets == nullptr || kv_offsets == nullptr)
+        return L2KV_ERR_NULL;
+    RowsArgs a = {};
+    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(K), a.V = static_cast<const char*>(V), a.O = static_cast<char*>(O);
+    a.q_off = q_offsets, a.kv_off = kv_offsets, a.kv_lens = kv_lens;
+    a.total_q = total_q, a.total_rows = total_rows, a.kv_head_stride = kv_head_stride, a.q_stride = q_stride;
+    a.n_seq = n_seq, a.Hkv = Hkv;
+    return rows_attn(a, dt, Hq, D, max_kv, scale, workspace, workspace_bytes, false, stream);
+}
+
+l2kv_status l2kv_tree_attn(const void* Q, const void* Kc, const void* Vc, const void* Kt, const void* Vt, l2kv_dtype dt,
+                           int32_t n_seq, int32_t Hq, int32_t Hkv, int32_t D, int64_t total_nodes, int64_t q_stride,
+                           const int64_t* node_offsets, const uint32_t* mask, int32_t mask_words,
+                           int64_t total_slots, int64_t kv_head_stride, const int64_t* slot_offsets,
+                           const int32_t* lens, int64_t max_len, float scale, void* O, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    if (Q == nullptr || Kc == nullptr || Vc == nullptr || Kt == nullptr || Vt == nullptr || O == nullptr || node_offsets == nullptr ||
+        mask == nullptr || slot_offsets == nullptr || lens == nullptr)
+        return L2KV_ERR_NULL;
+    if (dtype_ok(dt) && mask_words <= 0) return L2KV_ERR_SHAPE;
+    RowsArgs a = {};
+    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(Kc), a.V = static_cast<const char*>(Vc);
+    a.Kt = static_cast<const char*>(Kt), a.Vt = static_cast<const char*>(Vt), a.O = static_cast<char*>(O);
+    a.q_off = node_offsets, a.kv_off = slot_offsets, a.kv_lens = lens, a.mask = mask;
+    a.total_q = total_nodes, a.total_rows = total_slots, a.kv_head_stride = kv_head_stride, a.q_stride = q_stride;
+    a.n_seq = n_seq, a.Hkv = Hkv, a.mask_words = mask_words;
+    return rows_attn(a, dt, Hq, D, max_len, scale, workspace, workspace_bytes, true, stream);
+}
+
+l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t,
+                                    l2kv_dtype dt, int32_t n_planes, int32_t n_seq, int32_t D, int64_t total_nodes,
+                                    const int64_t* node_offsets, const int32_t* path, int32_t max_path,
+                                    const int32_t* path_lens, const int64_t* slot_offsets, int64_t total_slots,
+                                    const int32_t* lens_in, int32_t* lens_out, void* Kc, void* Vc,
+                                    float* norms_c, int32_t* pos_c, void* stream) {
+    if (Kt == nullptr || Vt == nullptr || norms_t == nullptr || pos_t == nullptr || node_offsets == nullptr || path == nullptr ||
+        path_lens == nullptr || slot_offsets == nullptr || lens_in == nullptr || lens_out == nullptr || Kc == nullptr || Vc == nullptr ||
+        norms_c == nullptr || pos_c == nullptr)
+        return L2KV_ERR_NULL;
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (n_planes <= 0 || n_seq <= 0 || max_path <= 0 || total_nodes <= 0 || total_nodes > kMaxTokens || total_slots <= 0 ||
+        total_slots > kMaxTokens || !dim_ok(D, dt) || lens_in == lens_out)
+        return L2KV_ERR_SHAPE;
+    if (!aligned(Kt, 16) || !aligned(Vt, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(norms_t, 4) || !aligned(pos_t, 4) ||
+        !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(path, 4) || !aligned(path_lens, 4) || !aligned(lens_in, 4) ||
+        !aligned(lens_out, 4) || !aligned(node_offsets, 8) || !aligned(slot_offsets, 8))
+        return L2KV_ERR_ALIGN;
+    return append_path_dispatch(Kt, Vt, norms_t, pos_t, dt, n_planes, n_seq, D, total_nodes, node_offsets, path, max_path, path_lens,
+                                slot_offsets, total_slots, lens_in, lens_out, Kc, Vc, norms_c, pos_c, static_cast<hipStream_t>(stream));
 }
 
 /* ---- attention-loss analysis ---------------------------------------------- */

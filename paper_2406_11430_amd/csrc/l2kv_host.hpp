@@ -6,6 +6,7 @@
 
 #include "../../include/l2kv.h"
 #include "ragged_plan.hpp"
+#include "rows_attn.hpp"
 
 namespace l2kv {
 
@@ -147,5 +148,33 @@ l2kv_status alr_dispatch(const void* Q, const void* K, l2kv_dtype dt, const int3
                          int32_t Hq, int32_t Hkv, int64_t T, int32_t D, int64_t k_head_stride, float scale,
                          int64_t m, double* alr, double* loss, double* loss_ref, void* workspace,
                          hipStream_t stream);
+
+// Rotary positions into the cache (rotary.hip).  token_off NULL: token t goes to row t, slot_off and lens are not read.
+struct RotaryArgs {
+    const char *Q, *K, *V;
+    const int32_t* positions;
+    const double* freqs;
+    const int64_t *token_off, *slot_off;
+    const int32_t* lens_in;
+    int32_t* lens_out;
+    char *Qr, *Kc, *Vc;
+    float* norms_c;
+    int32_t* pos_c;
+    int64_t total_tokens, total_slots, q_stride, k_stride, v_stride;      // strides of tokens, in elements
+    double amplitude;
+    int32_t n_seq, Hq, Hkv, rot, tokens_per_block;
+};
+l2kv_status rotary_dispatch(RotaryArgs args, l2kv_dtype dt, int32_t D, bool interleaved, hipStream_t stream);
+
+// Attention of many query rows (rows_attn.hip).
+RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt);
+l2kv_status rows_attn_dispatch(RowsArgs args, const RowsPlan& plan, int32_t D, l2kv_dtype dt, bool tree, hipStream_t stream);
+
+// The accepted path of a drafted tree (append_path.hip).
+l2kv_status append_path_dispatch(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t, l2kv_dtype dt,
+                                 int32_t n_planes, int32_t n_seq, int32_t D, int64_t total_nodes, const int64_t* node_off,
+                                 const int32_t* path, int32_t max_path, const int32_t* path_lens, const int64_t* slot_off,
+                                 int64_t total_slots, const int32_t* lens_in, int32_t* lens_out, void* Kc, void* Vc,
+                                 float* norms_c, int32_t* pos_c, hipStream_t stream);
 
 }  // namespace l2kv

@@ -1,0 +1,7 @@
+// Prompt and tree attention over bf16 rows of 256 elements: one translation unit per row type, so that they compile in parallel.
+#include "rows_attn_kernels.hpp"
+
+namespace l2kv {
+template l2kv_status rows_attn_launch<BF16, 256, false>(const RowsArgs&, bool, hipStream_t);
+template l2kv_status rows_attn_launch<BF16, 256, true>(const RowsArgs&, bool, hipStream_t);
+}  // namespace l2kv

@@ -1,0 +1,7 @@
+// Prompt and tree attention over f32 rows of 64 elements: one translation unit per row type, so that they compile in parallel.
+#include "rows_attn_kernels.hpp"
+
+namespace l2kv {
+template l2kv_status rows_attn_launch<F32, 64, false>(const RowsArgs&, bool, hipStream_t);
+template l2kv_status rows_attn_launch<F32, 64, true>(const RowsArgs&, bool, hipStream_t);
+}  // namespace l2kv
