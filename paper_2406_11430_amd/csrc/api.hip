@@ -516,7 +516,7 @@ static bool rows_sizes_ok(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_
 
 static size_t rows_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
     if (!rows_sizes_ok(n_seq, Hq, Hkv, total_q, max_kv, D, dt)) return 0;
-    return rows_plan(n_seq, Hkv, Hq / Hkv, total_q, max_kv, D, dt).partial_bytes;
+    return rows_plan(n_seq, Hkv, Hq / Hkv, total_q, max_kv, D, dt).bytes;
 }
 
 size_t l2kv_prompt_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
@@ -541,7 +541,7 @@ static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, i
     if (st == L2KV_ERR_SHAPE) return st;
     a.G = Hq / a.Hkv;
     const RowsPlan plan = rows_plan(a.n_seq, a.Hkv, a.G, a.total_q, max_kv, D, dt);
-    if (workspace_bytes < plan.partial_bytes || (workspace == nullptr && plan.partial_bytes > 0)) return L2KV_ERR_WORKSPACE;
+    if (workspace_bytes < plan.bytes || (workspace == nullptr && plan.bytes > 0)) return L2KV_ERR_WORKSPACE;
     if (st != L2KV_OK || (a.kv_head_stride * elem_bytes(dt)) % 16 != 0) return L2KV_ERR_ALIGN;
     if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Kt, 16) || !aligned(a.Vt, 16) || !aligned(a.O, 16) ||
         !aligned(a.q_off, 8) || !aligned(a.kv_off, 8) || !aligned(a.kv_lens, 4) || !aligned(a.mask, 4) || !aligned(workspace, 16))

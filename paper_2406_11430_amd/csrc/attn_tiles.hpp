@@ -1,7 +1,7 @@
 // Attention of many query rows over the keys of one KV head, on the matrix unit (gfx950, wave64): what the prompt and the
 // tree kernels share.
 //
-// A wave holds kNQ tiles of 32 query rows and goes over the keys in tiles of 32.  Scores are formed transposed, S^T = K.Q^T, and so
+// A wave holds 32 query rows and goes over the keys in tiles of 32.  Scores are formed transposed, S^T = K.Q^T, and so
 // is the output, O^T = V^T.P^T: the 32x32 result of the matrix instruction gives lane l the column l % 32 and the rows
 // 8*(i/4) + 4*(l/32) + i%4, i = 0..15.  A lane therefore holds 16 scores of ONE query, its maximum needs the other half of
 // the wave only where it rises, a factor on the accumulators is a plain per-lane product, and, because the order of the keys inside a
@@ -51,9 +51,15 @@ template <typename E, int D> struct AttnRow {
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
-// All of this wave's loads to LDS are done.
-__device__ __forceinline__ void wait_loads_to_lds() {
-    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+// This wave's loads to LDS are done, but for the last `tiles` tiles of kLoads each (at most kMost of them stay on their way).
+template <int kLoads, int kMost>
+__device__ __forceinline__ void wait_loads_to_lds(int32_t tiles) {
+    constexpr auto left = [](int n) { return (kWaitVmcnt0 | (n & 15) | (n >> 4) << 14); };
+    static_assert(kLoads * kMost < 64, "what the counter of loads can hold");
+    if (kMost >= 2 && tiles >= 2) __builtin_amdgcn_s_waitcnt(left(2 * kLoads * (kMost >= 2)));
+    else if (kMost >= 1 && tiles >= 1) __builtin_amdgcn_s_waitcnt(left(kLoads * (kMost >= 1)));
+    else __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    static_assert(kMost <= 2, "the cases above");
     asm volatile("" ::: "memory");
 }
 
@@ -96,6 +102,8 @@ template <typename E, int D> struct TileAddress {
             v[0] = v[1] = 4 * half * R::kBytes + (((row / 4) ^ R::v_swizzle(4 * half)) << 4) + (row % 4) * 4;
         }
     }
+    // What is worked out from the places from here on is not held any longer than it is used: registers.
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(k), "+v"(v[0]), "+v"(v[1])); }
     // piece 2t + half of the lane's row of a K tile
     __device__ __forceinline__ u32x4_t key(const char* tile, int t) const {
         return *reinterpret_cast<const u32x4_t*>(tile + (k ^ (t << 5)));
@@ -120,24 +128,21 @@ __device__ __forceinline__ void load_query(QueryTile<E, D>& q, const char* row, 
     for (int t = 0; t < AttnRow<E, D>::kQWords / 4; ++t) q.piece[t] = *reinterpret_cast<const u32x4_t*>(row + (2 * t + half) * 16);
 }
 
-// K tile . Q^T for kNQ query tiles.
-template <typename E, int D, int kNQ>
-__device__ __forceinline__ void scores(const char* tile, const TileAddress<E, D>& at, const QueryTile<E, D> (&q)[kNQ], f32x16_t (&s)[kNQ]) {
+// K tile . Q^T.
+template <typename E, int D>
+__device__ __forceinline__ void scores(const char* tile, const TileAddress<E, D>& at, const QueryTile<E, D>& q, f32x16_t& s) {
+    s = f32x16_t{};
 #pragma unroll
     for (int t = 0; t < AttnRow<E, D>::kQWords / 4; ++t) {
+        if (AttnRow<E, D>::kBytes == 512 && t % 4 == 0) __builtin_amdgcn_sched_barrier(0);      // few operands on their way: registers
         const u32x4_t k = at.key(tile, t);
+        if constexpr (E::kBytes == 2) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q.piece[t]), s, 0, 0, 0);
+        } else {
+            // one product of two columns at a time: 8t + j and 8t + 4 + j
+            const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q.piece[t]);
 #pragma unroll
-        for (int n = 0; n < kNQ; ++n) {
-            if (t == 0) s[n] = f32x16_t{};
-            if constexpr (E::kBytes == 2) {
-                s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[n].piece[t]),
-                                                              s[n], 0, 0, 0);
-            } else {
-                // one product of two columns at a time: 8t + j and 8t + 4 + j
-                const f32x4_t kf = __builtin_bit_cast(f32x4_t, k), qf = __builtin_bit_cast(f32x4_t, q[n].piece[t]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j], qf[j], s[n], 0, 0, 0);
-            }
+            for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j], qf[j], s, 0, 0, 0);
         }
     }
 }
@@ -147,34 +152,25 @@ template <> struct Weights<BF16> { uint32_t w[8]; };
 template <> struct Weights<F32> { float w[16]; };
 
 // o += V^T tile . P^T.
-template <typename E, int D, int kNQ>
-__device__ __forceinline__ void weighted_values(const char* tile, const TileAddress<E, D>& at, const Weights<E> (&p)[kNQ],
-                                                f32x16_t (&o)[kNQ][D / kTile]) {
+template <typename E, int D>
+__device__ __forceinline__ void weighted_values(const char* tile, const TileAddress<E, D>& at, const Weights<E>& p, f32x16_t (&o)[D / kTile]) {
     if constexpr (E::kBytes == 2) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+            const u32x4_t w = {p.w[4 * t], p.w[4 * t + 1], p.w[4 * t + 2], p.w[4 * t + 3]};
 #pragma unroll
             for (int d = 0; d < D / kTile; ++d) {
+                if (AttnRow<E, D>::kBytes == 512 && d % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                 const u32x2_t a = at.values(tile, t, 0, d), b = at.values(tile, t, 1, d);
                 const u32x4_t v = {a[0], a[1], b[0], b[1]};
-#pragma unroll
-                for (int n = 0; n < kNQ; ++n) {
-                    const u32x4_t w = {p[n].w[4 * t], p[n].w[4 * t + 1], p[n].w[4 * t + 2], p[n].w[4 * t + 3]};
-                    o[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w),
-                                                                     o[n][d], 0, 0, 0);
-                }
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w), o[d], 0, 0, 0);
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 16; ++i)
 #pragma unroll
-            for (int d = 0; d < D / kTile; ++d) {
-                const float v = at.value(tile, i, d);
-#pragma unroll
-                for (int n = 0; n < kNQ; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[n].w[i], o[n][d], 0, 0, 0);
-            }
-        }
+            for (int d = 0; d < D / kTile; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(at.value(tile, i, d), p.w[i], o[d], 0, 0, 0);
     }
 }
 
@@ -196,59 +192,67 @@ template <typename E, int D> __device__ __forceinline__ bool values_not_finite(c
     return __ballot(bad) != 0;
 }
 
-// o += V^T.P^T for a tile with hidden keys and values that are not finite: 0 times an infinity is not zero.  First the finite values
-// alone, in the order of weighted_values, so that a row that sees none of the others has the same bits whatever they are; then the others,
-// one key at a time, added where a bit of `seen` says so.  Slow.
+// For a tile with hidden keys, where 0 times an infinity is not zero: the operand of 16 keys (bf16: t = 0, 1) or two (fp32: t = 0..15) with
+// the finite values of the keys to keep, or the others; and the weights that go with it.
 template <typename E, int D>
-__device__ __forceinline__ void weighted_values_seen(const char* tile, const TileAddress<E, D>& at, const Weights<E>& p, uint32_t seen,
-                                                     f32x16_t (&o)[D / kTile], int lane) {
-    const int half = lane / kTile;
-    // operand of 16 keys (bf16: t, 0..1) or two (fp32: t, 0..15)
-    auto operand = [&](int t, int d, const u32x4_t& keep, bool finite) {
-        u32x4_t v = {0, 0, 0, 0};
-        if constexpr (E::kBytes == 2) {
-            const u32x2_t a = at.values(tile, t, 0, d), b = at.values(tile, t, 1, d);
-            v = u32x4_t{a[0], a[1], b[0], b[1]};
-        } else {
-            v[0] = __builtin_bit_cast(uint32_t, at.value(tile, t, d));
-        }
+__device__ __forceinline__ u32x4_t values_operand(const char* tile, const TileAddress<E, D>& at, int t, int d) {
+    if constexpr (E::kBytes == 2) {
+        const u32x2_t a = at.values(tile, t, 0, d), b = at.values(tile, t, 1, d);
+        return u32x4_t{a[0], a[1], b[0], b[1]};
+    } else {
+        return u32x4_t{__builtin_bit_cast(uint32_t, at.value(tile, t, d)), 0, 0, 0};
+    }
+}
+template <typename E> __device__ __forceinline__ u32x4_t weights_operand(const Weights<E>& p, int t) {
+    u32x4_t w = {0, 0, 0, 0};
+    if constexpr (E::kBytes == 2) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t bad = not_finite_bits<E>(v[i]);
-            v[i] &= keep[i] & (finite ? ~bad : bad);
+            const uint32_t first = p.w[i], second = p.w[4 + i];
+            w[i] = t == 0 ? first : second;
         }
-        return v;
-    };
-    auto product = [&](const u32x4_t& v, const u32x4_t& w, const f32x16_t& c) {
-        if constexpr (E::kBytes == 2)
-            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w), c, 0, 0, 0);
-        else
-            return __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, (uint32_t)v[0]), __builtin_bit_cast(float, (uint32_t)w[0]), c, 0, 0, 0);
-    };
-    auto weights = [&](int t) {
-        u32x4_t w = {0, 0, 0, 0};
-        if constexpr (E::kBytes == 2) {
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t first = p.w[i], second = p.w[4 + i];
-                w[i] = t == 0 ? first : second;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[0] = i == t ? __builtin_bit_cast(uint32_t, p.w[i]) : w[0];
-        }
-        return w;
-    };
-    const u32x4_t whole = {~0u, ~0u, ~0u, ~0u};
+        for (int i = 0; i < 16; ++i) w[0] = i == t ? __builtin_bit_cast(uint32_t, p.w[i]) : w[0];
+    }
+    return w;
+}
+template <typename E> __device__ __forceinline__ f32x16_t value_product(const u32x4_t& v, const u32x4_t& w, const f32x16_t& c) {
+    if constexpr (E::kBytes == 2)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, (uint32_t)v[0]), __builtin_bit_cast(float, (uint32_t)w[0]), c, 0, 0, 0);
+}
+
+// o += V^T.P^T over the finite values of a tile, in the order of weighted_values: a row that sees none of the others has the same
+// bits whatever they are.  Returns whether there are others.
+template <typename E, int D>
+__device__ __forceinline__ bool finite_values(const char* tile, const TileAddress<E, D>& at, const Weights<E>& p, f32x16_t (&o)[D / kTile]) {
+    uint32_t any = 0;
 #pragma unroll 1
     for (int t = 0; t < (E::kBytes == 2 ? 2 : 16); ++t) {
-        const u32x4_t w = weights(t);
+        const u32x4_t w = weights_operand<E>(p, t);
 #pragma unroll
         for (int d = 0; d < D / kTile; ++d) {
-            o[d] = product(operand(t, d, whole, true), w, o[d]);
+            u32x4_t v = values_operand<E, D>(tile, at, t, d);
+#pragma unroll
+            for (int i = 0; i < (E::kBytes == 2 ? 4 : 1); ++i) {
+                const uint32_t bad = not_finite_bits<E>(v[i]);
+                v[i] &= ~bad;
+                any |= bad;
+            }
+            o[d] = value_product<E>(v, w, o[d]);
             __builtin_amdgcn_sched_barrier(0);                     // one product at a time: registers
         }
     }
+    return __ballot(any != 0) != 0;
+}
+
+// The values that are not finite, one key at a time: where a bit of `seen` says so, its product is added.  Slow.
+template <typename E, int D>
+__device__ __forceinline__ void other_values(const char* tile, const TileAddress<E, D>& at, const Weights<E>& p, uint32_t seen,
+                                             f32x16_t (&o)[D / kTile], int lane) {
+    const int half = lane / kTile;
 #pragma unroll 1
     for (int key = 0; key < kTile; ++key) {
         const bool mine = (key >> 2 & 1) == half, add = (seen >> key) & 1;
@@ -257,10 +261,13 @@ __device__ __forceinline__ void weighted_values_seen(const char* tile, const Til
         u32x4_t keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) keep[i] = mine && (E::kBytes == 4 || j / 2 == i) ? (E::kBytes == 4 ? ~0u : (j % 2 == 0 ? 0xffffu : 0xffff0000u)) : 0u;
-        const u32x4_t w = weights(t);
+        const u32x4_t w = weights_operand<E>(p, t);
 #pragma unroll
         for (int d = 0; d < D / kTile; ++d) {
-            const f32x16_t one = product(operand(t, d, keep, false), w, f32x16_t{});
+            u32x4_t v = values_operand<E, D>(tile, at, t, d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] &= keep[i] & not_finite_bits<E>(v[i]);
+            const f32x16_t one = value_product<E>(v, w, f32x16_t{});
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] += add ? one[i] : 0.f;
             __builtin_amdgcn_sched_barrier(0);
@@ -278,51 +285,41 @@ __device__ __forceinline__ float sum_of_halves(float v) {
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
-// Running softmax of a wave's kNQ tiles of query rows.
-template <typename E, int D, int kNQ> struct RowState {
-    f32x16_t o[kNQ][D / kTile];
-    float m[kNQ];          // what weights are relative to, in powers of two; the same in both halves
-    float l[kNQ];          // sum of the weights of this lane's keys
+// Running softmax of a wave's 32 query rows.
+template <typename E, int D> struct RowState {
+    f32x16_t o[D / kTile];
+    float m;               // what weights are relative to, in powers of two; the same in both halves
+    float l;               // sum of the weights of this lane's keys
     __device__ __forceinline__ void clear() {
+        m = -__builtin_inff();
+        l = 0.f;
 #pragma unroll
-        for (int n = 0; n < kNQ; ++n) {
-            m[n] = -__builtin_inff();
-            l[n] = 0.f;
-#pragma unroll
-            for (int d = 0; d < D / kTile; ++d) o[n][d] = f32x16_t{};
-        }
+        for (int d = 0; d < D / kTile; ++d) o[d] = f32x16_t{};
     }
 };
 
-// Scores (hidden ones -inf) to weights, moving the maximum where scores rise too far above it.  scale: softmax scale times log2(e).
+// Scores of kTiles tiles of keys (hidden ones -inf) to weights, moving the maximum where scores rise too far above it.  scale: softmax scale times log2(e).
 // bf16 weights are rounded for the matrix unit, and the sum is taken over the ROUNDED ones, so the weights of a row sum to one exactly
 // as they are applied: rounding one key that outweighs the rest has no effect at all.
-template <typename E, int D, int kNQ>
-__device__ __forceinline__ void softmax_step(RowState<E, D, kNQ>& st, f32x16_t (&s)[kNQ], Weights<E> (&p)[kNQ], float scale) {
-    bool rise = false;
-    float top[kNQ];
+template <typename E, int D, int kTiles>
+__device__ __forceinline__ void softmax_step(RowState<E, D>& st, const f32x16_t (&s)[kTiles], Weights<E> (&p)[kTiles], float scale) {
+    float top = s[0][0];
 #pragma unroll
-    for (int n = 0; n < kNQ; ++n) {
-        top[n] = s[n][0];
+    for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top[n] = fmaxf(top[n], s[n][i]);
-        top[n] *= scale;
-        rise |= top[n] > st.m[n] + kRiseAllowed;
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top *= scale;
+    if (__ballot(top > st.m + kRiseAllowed) != 0) {
+        const float m = fmaxf(st.m, max_of_halves(top));
+        const float f = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+        st.m = m;
+        st.l *= f;
+#pragma unroll
+        for (int d = 0; d < D / kTile; ++d) st.o[d] *= f;
     }
-    if (__ballot(rise) != 0) {
+    const float m = st.m == -__builtin_inff() ? 0.f : st.m;                // nothing seen yet: exp2(-inf) = 0
 #pragma unroll
-        for (int n = 0; n < kNQ; ++n) {
-            const float m = fmaxf(st.m[n], max_of_halves(top[n]));
-            const float f = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
-            st.m[n] = m;
-            st.l[n] *= f;
-#pragma unroll
-            for (int d = 0; d < D / kTile; ++d) st.o[n][d] *= f;
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < kNQ; ++n) {
-        const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];      // nothing seen yet: exp2(-inf) = 0
+    for (int n = 0; n < kTiles; ++n) {
         float e[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -m));
@@ -332,13 +329,13 @@ __device__ __forceinline__ void softmax_step(RowState<E, D, kNQ>& st, f32x16_t (
             for (int i = 0; i < 8; ++i) {
                 const f32x2_t two = {e[2 * i], e[2 * i + 1]};
                 p[n].w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2_t));
-                st.l[n] = dot2_bf16(p[n].w[i], 0x3f803f80u, st.l[n]);
+                st.l = dot2_bf16(p[n].w[i], 0x3f803f80u, st.l);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 p[n].w[i] = e[i];
-                st.l[n] += e[i];
+                st.l += e[i];
             }
         }
     }

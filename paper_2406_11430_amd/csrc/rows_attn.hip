@@ -3,62 +3,60 @@
 
 namespace l2kv {
 
-extern template l2kv_status rows_attn_launch<BF16, 64, false>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 64, true>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 128, false>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 128, true>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 256, false>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 256, true>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 64, false>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 64, true>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 128, false>(const RowsArgs&, bool, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 128, true>(const RowsArgs&, bool, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 64, false>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 64, true>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 128, false>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 128, true>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 256, false>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 256, true>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 64, false>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 64, true>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 128, false>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 128, true>(const RowsArgs&, int, hipStream_t);
 
-template <typename E, int D> static void shapes(bool wide, int32_t* rows, int32_t* keys) {
-    using S = RowsShapes<E, D>;
-    *rows = wide ? S::kWideRows : kTile;
-    *keys = wide ? S::kWideKeys : S::kNarrowKeys;
+struct ShapeSizes { int32_t rows, keys; };
+template <int kRowBytes, int kShape> static constexpr ShapeSizes sizes_of() {
+    using S = RowsShape<kRowBytes, kShape>;
+    return {S::kWR * kTile, S::kWK * S::kNK * kTile};
+}
+template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
+    constexpr ShapeSizes all[4] = {sizes_of<kRowBytes, 0>(), sizes_of<kRowBytes, 1>(), sizes_of<kRowBytes, 2>(), sizes_of<kRowBytes, 3>()};
+    return all[shape];
 }
 
 RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
+    const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
+    auto sizes = [&](int shape) { return row_bytes == 128 ? shape_sizes<128>(shape) : (row_bytes == 256 ? shape_sizes<256>(shape) : shape_sizes<512>(shape)); };
     RowsPlan p;
-    // rows of an average sequence; a workgroup of the wide shape reads the keys once for all its rows
-    const int64_t mean_rows = total_q * G / n_seq;
-    p.wide = mean_rows > kTile;
-    int32_t keys;
-    if (dt == L2KV_F32) {
-        if (D == 64) shapes<F32, 64>(p.wide, &p.block_rows, &keys);
-        else shapes<F32, 128>(p.wide, &p.block_rows, &keys);
-    } else if (D == 64) {
-        shapes<BF16, 64>(p.wide, &p.block_rows, &keys);
-    } else if (D == 128) {
-        shapes<BF16, 128>(p.wide, &p.block_rows, &keys);
-    } else {
-        shapes<BF16, 256>(p.wide, &p.block_rows, &keys);
-    }
-    p.tokens_per_block = p.block_rows / G;
+    // the smallest block that takes the rows of a sequence, somewhat more than the average where there are several
+    const int64_t rows = total_q * G / n_seq, room = n_seq == 1 ? rows : rows + rows / 4;
+    p.shape = 3;
+    while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
+    const ShapeSizes s = sizes(p.shape);
+    p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
-    p.n_blocks = (int32_t)blocks;                               // at most 2^32 (checked by the caller): total_q, n_seq < 2^31
-    const int64_t tiles = (max_kv + keys - 1) / keys;
-    const int64_t work = blocks * Hkv, want = 2 * device_compute_units();
-    int64_t shares = work >= want / 2 ? 1 : want / work;
-    const int64_t least = 4;                                    // tiles of a share
-    if (shares > tiles / least) shares = tiles / least < 1 ? 1 : tiles / least;
-    p.tiles_per_share = (int32_t)((tiles + shares - 1) / shares);
-    if (p.tiles_per_share < 1) p.tiles_per_share = 1;
-    p.max_shares = (int32_t)((tiles + p.tiles_per_share - 1) / p.tiles_per_share);
-    if (p.max_shares < 1) p.max_shares = 1;
-    p.partial_bytes = p.max_shares == 1 ? 0 : (size_t)blocks * Hkv * p.max_shares * p.block_rows * (D + 2) * sizeof(float);
+    p.n_blocks = (int32_t)blocks;
+    const int64_t items = blocks * Hkv, slots = device_compute_units();
+    const int64_t tiles = max_kv / s.keys + 2;                     // of an item, at most (its nodes in one)
+    // Many items, or items that are not worth cutting: a workgroup each.
+    p.workgroups = 0;
+    p.least_tiles = dt == L2KV_F32 ? 3 : 5;                        // one is what an item counts for by itself
+    if (items < 4 * slots && tiles > 6 && n_seq <= 1024) {
+        const int64_t most = items * tiles / (p.least_tiles - 1);
+        p.workgroups = (int32_t)(most < slots ? most : slots);
+    }
+    p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * s.rows * rows_partial_floats(D) * sizeof(float);
+    p.bytes = p.workgroups < 2 ? 0 : p.partial_bytes + (size_t)p.workgroups * sizeof(RowsJoin);
     return p;
 }
 
 l2kv_status rows_attn_dispatch(RowsArgs a, const RowsPlan& p, int32_t D, l2kv_dtype dt, bool tree, hipStream_t stream) {
-    a.block_rows = p.block_rows;
     a.tokens_per_block = p.tokens_per_block;
     a.n_blocks = p.n_blocks;
-    a.tiles_per_share = p.tiles_per_share;
-    a.max_shares = p.max_shares;
-#define L2KV_ROWS(E, D_) return tree ? rows_attn_launch<E, D_, true>(a, p.wide, stream) : rows_attn_launch<E, D_, false>(a, p.wide, stream)
+    a.workgroups = p.workgroups < 2 ? 0 : p.workgroups;
+    a.least_tiles = p.least_tiles;
+    a.joins = reinterpret_cast<RowsJoin*>(reinterpret_cast<char*>(a.partial) + p.partial_bytes);
+#define L2KV_ROWS(E, D_) return tree ? rows_attn_launch<E, D_, true>(a, p.shape, stream) : rows_attn_launch<E, D_, false>(a, p.shape, stream)
     if (dt == L2KV_F32) {
         if (D == 64) L2KV_ROWS(F32, 64);
         L2KV_ROWS(F32, 128);

@@ -6,24 +6,35 @@
 
 namespace l2kv {
 
+// An item that several workgroups have parts of, as the one in whose stretch it begins leaves it for the join.
+struct RowsJoin {
+    int64_t first_row;         // of O: (token, query head) of its first row
+    int32_t parts, rows, slot, unused;
+};
+
 struct RowsArgs {
     const char *Q, *K, *V, *Kt, *Vt;
     char* O;
     float* partial;
+    RowsJoin* joins;
     const int64_t *q_off, *kv_off;
     const int32_t* kv_lens;
     const uint32_t* mask;
     int64_t total_q, total_rows, kv_head_stride, q_stride;      // strides in elements
     int32_t n_seq, Hkv, G, mask_words;
-    int32_t block_rows, tokens_per_block, n_blocks, tiles_per_share, max_shares;
+    int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
     float scale;                                                // softmax scale times log2(e)
 };
 
-// How a launch is cut: blocks of query rows, and shares of the tiles of keys.
+// How a launch is cut: the shape of its workgroups, which takes blocks of so many tokens, and the number of workgroups that take equal
+// stretches of all keys (0: one workgroup per block and KV head).
 struct RowsPlan {
-    bool wide;
-    int32_t block_rows, tokens_per_block, n_blocks, tiles_per_share, max_shares;
-    size_t partial_bytes;
+    int shape;
+    int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
+    size_t partial_bytes, bytes;       // of the parts, and of the joins behind them as well
 };
+
+// One row of what a workgroup has of an item: D sums, the maximum that they are relative to, the sum of weights; 16-byte aligned.
+constexpr int rows_partial_floats(int D) { return D + 4; }
 
 }  // namespace l2kv

@@ -1,8 +1,10 @@
 // Kernels of l2kv_prompt_attn and l2kv_tree_attn: attention of many query rows, packed over sequences.
 //
 // The G query heads of a KV head are rows of one problem: row r of a block is token r / G, head r % G, so K and V are read once for all of
-// them.  One workgroup takes a block of rows of one (sequence, KV head), over all its keys or, where rows are few, over a share of the
-// tiles of keys; the shares are joined by a second kernel.
+// them.  An item is one block of rows of one (sequence, KV head) over all keys that it sees.  A launch either has one workgroup per item
+// (many items: those that run at a time read the same keys), or a fixed number of workgroups that take equal stretches of all items'
+// keys laid end to end, whatever the lengths are; what a stretch has of an item that others have parts of goes to memory, and a second
+// kernel joins the parts.
 #pragma once
 
 #include "attn_tiles.hpp"
@@ -11,68 +13,163 @@
 
 namespace l2kv {
 
-// Block `id` of the launch: which tokens of which sequence, and the keys they see.
-struct RowsBlock {
-    int32_t seq;
-    int64_t first_token;       // in Q and O
-    int32_t tokens;            // 0: no such block
-    int32_t first_in_seq;      // of its first token
-    int32_t n_tokens;          // of the sequence
-    int64_t first_row;         // of the sequence's cached rows in a plane
-    int32_t n_rows;
-    int32_t row_tiles, tiles;  // over cached rows, and over nodes as well
+struct RowsSeq {
+    int64_t q_first, row_first;        // first token in Q and O, first cached row in a plane
+    int32_t n_q, n_rows, blocks;
 };
 
-// Blocks are counted so that sequence s has ids from q_off[s] / tokens_per_block + s on: room for all its blocks, and which sequence an
-// id belongs to is found among the offsets alone, 64 at a time.
+// Quotient of numbers that are not negative; most have 32 bits, where a division is a tenth of the instructions.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
+    if (((n | d) >> 32) == 0) return (uint32_t)n / (uint32_t)d;
+    return (int64_t)((uint64_t)n / (uint64_t)d);
+}
+
+__device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int32_t s) {
+    const Range q = clamped_range(a.q_off, s, a.total_q), kv = clamped_range(a.kv_off, s, a.total_rows);
+    int64_t rows = kv.count;
+    if (a.kv_lens != nullptr) {
+        const int64_t len = a.kv_lens[s];
+        rows = len < 0 ? 0 : (len < rows ? len : rows);
+    }
+    return RowsSeq{q.first, kv.first, (int32_t)q.count, (int32_t)rows, (int32_t)(((uint32_t)q.count + (uint32_t)a.tokens_per_block - 1) / (uint32_t)a.tokens_per_block)};
+}
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+__device__ __forceinline__ RowsSeq uniform(const RowsSeq& q) {
+    return RowsSeq{uniform(q.q_first), uniform(q.row_first), __builtin_amdgcn_readfirstlane(q.n_q), __builtin_amdgcn_readfirstlane(q.n_rows),
+                   __builtin_amdgcn_readfirstlane(q.blocks)};
+}
+
+// Lengths of items, in keys.  A block of a prompt sees the rows up to its last token's limit; a block of a tree all cached rows and all
+// nodes, in whole tiles each.  An item counts for one tile more than it has, so that none is empty.
+template <bool kTree, int kTileKeys> struct RowsLength {
+    static __device__ __forceinline__ int64_t keys(const RowsArgs& a, const RowsSeq& q, int64_t block) {
+        if constexpr (kTree) {
+            return (((int64_t)q.n_rows + kTileKeys - 1) / kTileKeys + ((int64_t)q.n_q + kTileKeys - 1) / kTileKeys) * kTileKeys;
+        } else {
+            const int64_t end = (block + 1) * a.tokens_per_block, limit = (end < q.n_q ? end : q.n_q) + q.n_rows - q.n_q;
+            return limit < 0 ? 0 : limit;
+        }
+    }
+    // of the blocks before `block`, together
+    static __device__ __forceinline__ int64_t before(const RowsArgs& a, const RowsSeq& q, int64_t block) {
+        if constexpr (kTree) {
+            return block * (kTileKeys + keys(a, q, 0));
+        } else {
+            const int64_t step = a.tokens_per_block, more = (int64_t)q.n_rows - q.n_q;
+            const int64_t none = more >= 0 ? 0 : (uint32_t)-more / (uint32_t)step;            // blocks that see nothing
+            int64_t sum = block * kTileKeys;
+            if (block > none) sum += step * (block * (block + 1) - none * (none + 1)) / 2 + more * (block - none);
+            if (block == q.blocks && block > none) sum -= block * step - q.n_q;
+            return sum;
+        }
+    }
+};
+
+// An item and a place in it.
+struct RowsItem {
+    RowsSeq q;
+    int32_t seq, head, block;
+    int64_t start, at;                 // of the item in the line of all items, of the place in the item
+};
+
+// Inclusive prefix sum of a wave's numbers below 2^56, by two of 32 bits.
+__device__ __forceinline__ int64_t wave_prefix(int64_t v) {
+    return ((int64_t)wave_inclusive_sum((uint32_t)(v >> 24)) << 24) + wave_inclusive_sum((uint32_t)v & 0xffffffu);
+}
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
+}
+
+// Keys of a stretch where all items count for `total`: the same for every workgroup, but at least some tiles, so that short problems are
+// not cut to pieces.
+template <int kTileKeys> __device__ __forceinline__ int64_t rows_stretch(const RowsArgs& a, int64_t total) {
+    const int64_t even = quotient(total + a.workgroups - 1, a.workgroups);
+    return even < a.least_tiles * kTileKeys ? a.least_tiles * kTileKeys : even;
+}
+
+// The stretch of this workgroup, [begin, end), and the item that it begins in; false if there is none.  A lane for each sequence, 64 at
+// a time.
 template <bool kTree, int kTileKeys>
-__device__ __forceinline__ RowsBlock rows_block(const RowsArgs& a, int32_t id, int lane) {
-    RowsBlock b;
+__device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& it, int64_t& stretch, int64_t& end, int lane) {
+    using L = RowsLength<kTree, kTileKeys>;
+    RowsSeq q = {};
+    int64_t mine = 0, upto = 0, total = 0;                     // of the lane's sequence, of those up to it, of all
+    int32_t s0 = 0;
+    auto look = [&] {
+        q = RowsSeq{};
+        if (s0 + lane < a.n_seq) q = rows_seq(a, s0 + lane);
+        mine = a.Hkv * L::before(a, q, q.blocks);
+        upto = wave_prefix(mine);
+    };
+    for (; s0 < a.n_seq; s0 += kWaveSize) {
+        look();
+        total += of_lane(upto, kWaveSize - 1);
+    }
+    stretch = rows_stretch<kTileKeys>(a, total);
+    const int64_t begin = blockIdx.x * stretch;
+    if (begin >= total) return false;
+    end = begin + stretch < total ? begin + stretch : total;
+    int64_t base = 0;                                          // of the sequences before s0
+    if (a.n_seq > kWaveSize) s0 = 0, look();
+    else s0 = 0;
+    uint64_t behind;
+    while ((behind = __ballot(base + upto > begin)) == 0) {    // ends at the last sequences, where it is total > begin
+        base += of_lane(upto, kWaveSize - 1);
+        s0 += kWaveSize;
+        look();
+    }
+    const int which = __builtin_ctzll(behind);
+    it.seq = s0 + which;
+    it.q = RowsSeq{of_lane(q.q_first, which), of_lane(q.row_first, which), __builtin_amdgcn_readlane(q.n_q, which),
+                   __builtin_amdgcn_readlane(q.n_rows, which), __builtin_amdgcn_readlane(q.blocks, which)};
+    int64_t rest = begin - base - of_lane(upto - mine, which);
+    const int64_t head_keys = L::before(a, it.q, it.q.blocks);
+    it.head = (int32_t)quotient(rest, head_keys);
+    rest -= it.head * head_keys;
+    // the last block that begins at or before the place, 64 candidates a step
+    int32_t lo = 0, count = it.q.blocks;
+    while (count > 1) {
+        const int32_t step = (count + kWaveSize - 1) / kWaveSize;
+        const uint64_t found = __ballot((int64_t)lane * step < count && L::before(a, it.q, lo + (int64_t)lane * step) <= rest);
+        const int32_t last = found == 0 ? 0 : 63 - __builtin_clzll(found);
+        lo += last * step;
+        count = count - last * step < step ? count - last * step : step;
+    }
+    it.block = __builtin_amdgcn_readfirstlane(lo);
+    it.head = __builtin_amdgcn_readfirstlane(it.head);
+    it.at = uniform(rest - L::before(a, it.q, it.block));
+    it.start = uniform(begin - it.at);
+    return true;
+}
+
+// The item of a workgroup of its own.  Blocks are counted so that sequence s has ids from q_off[s] / tokens_per_block + s on: room for all
+// its blocks, and which sequence an id belongs to is found among the offsets alone, 64 at a time.
+template <bool kTree, int kTileKeys>
+__device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, int lane) {
+    it.head = (int32_t)(blockIdx.x % (uint32_t)a.Hkv);
+    const int32_t id = a.n_blocks - 1 - (int32_t)(blockIdx.x / (uint32_t)a.Hkv);      // the last tokens of a sequence see most: they go first
     int32_t lo = 0, count = a.n_seq;
     while (count > 1) {
         const int32_t step = (count + kWaveSize - 1) / kWaveSize;
         const int32_t mine = lo + lane * step;
         bool at_or_before = false;
-        if (lane * step < count) {
-            const int64_t off = a.q_off[mine];
-            at_or_before = off / a.tokens_per_block + mine <= id;
+        if ((int64_t)lane * step < count) {
+            const int64_t off = a.q_off[mine], inside = off < 0 ? 0 : (off < a.total_q ? off : a.total_q);
+            at_or_before = (int64_t)((uint32_t)inside / (uint32_t)a.tokens_per_block) + mine <= id;
         }
         const uint64_t found = __ballot(at_or_before);
         const int32_t last = found == 0 ? 0 : 63 - __builtin_clzll(found);
-        const int32_t left = count - last * step;
         lo += last * step;
-        count = left < step ? left : step;
+        count = count - last * step < step ? count - last * step : step;
     }
-    b.seq = __builtin_amdgcn_readfirstlane(lo);
-    const Range q = clamped_range(a.q_off, b.seq, a.total_q);
-    const int64_t at = (id - (q.first / a.tokens_per_block + b.seq)) * a.tokens_per_block;
-    b.tokens = 0;
-    if (at < 0 || at >= q.count) return b;
-    b.first_token = q.first + at;
-    b.first_in_seq = (int32_t)at;
-    b.n_tokens = (int32_t)q.count;
-    b.tokens = (int32_t)(q.count - at < a.tokens_per_block ? q.count - at : a.tokens_per_block);
-    const Range kv = clamped_range(a.kv_off, b.seq, a.total_rows);
-    b.first_row = kv.first;
-    int64_t rows = kv.count;
-    if (a.kv_lens != nullptr) {
-        const int64_t len = a.kv_lens[b.seq];
-        rows = len < 0 ? 0 : (len < kv.count ? len : kv.count);
-    }
-    b.n_rows = (int32_t)rows;
-    int64_t last = rows;                                       // cached rows that any of the tokens sees
-    if constexpr (!kTree) {
-        const int64_t limit = at + b.tokens + rows - q.count;
-        last = limit < 0 ? 0 : limit;
-    }
-    b.row_tiles = (int32_t)((last + kTileKeys - 1) / kTileKeys);
-    b.tiles = b.row_tiles + (kTree ? (int32_t)((q.count + kTileKeys - 1) / kTileKeys) : 0);
-    return b;
-}
-
-__device__ __forceinline__ int32_t rows_shares(const RowsArgs& a, const RowsBlock& b) {
-    const int32_t n = (b.tiles + a.tiles_per_share - 1) / a.tiles_per_share;
-    return n < 1 ? 1 : (n < a.max_shares ? n : a.max_shares);
+    it.seq = __builtin_amdgcn_readfirstlane(lo);
+    it.q = uniform(rows_seq(a, it.seq));
+    const int64_t block = uniform(id - ((int64_t)((uint32_t)it.q.q_first / (uint32_t)a.tokens_per_block) + it.seq));
+    it.block = (int32_t)block;
+    it.start = it.at = 0;
+    return block >= 0 && block < it.q.blocks;
 }
 
 template <typename E> __device__ __forceinline__ void store_four(char* at, const float (&v)[4]) {
@@ -86,268 +183,324 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
     }
 }
 
-// kWR x kWK waves: kWR groups of 32 * kNQ rows each, the keys of a tile shared among kWK waves of a group.  A tile has kWK * kNK * 32 keys.
-template <typename E, int D, int kNQ, int kWR, int kWK, int kNK, bool kTree>
-__global__ __launch_bounds__(kWaveSize * kWR * kWK, kWR * kWK >= 8 ? 2 : 1)
+// kWR x kWK waves: kWR groups of 32 rows each, the keys of a tile shared among kWK waves of a group.  A tile has kWK * kNK * 32 keys;
+// kStages of them have room in LDS, all but one on their way while that one is worked on.
+template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree>
+__global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {
     using R = AttnRow<E, D>;
-    constexpr int kWaves = kWR * kWK, kTileKeys = kWK * kNK * kTile;
+    constexpr int kWaves = kWR * kWK, kTileKeys = kWK * kNK * kTile, kBlockRows = kWR * kTile;
     constexpr int kHalf = kTileKeys * R::kBytes;               // bytes of a tile of K, and of one of V
-    constexpr int kJoinFloats = (kWK - 1) * kWR * kNQ * (D / 2 + 2) * kWaveSize;
-    static_assert(kJoinFloats * 4 <= 4 * kHalf, "the waves' results fit where the tiles were");
-    __shared__ __attribute__((aligned(16))) char lds[4 * kHalf];
+    constexpr int kJoinFloats = (kWK - 1) * kWR * (D / 2 + 2) * kWaveSize;
+    constexpr int kLoads = 2 * kHalf / 1024 / kWaves;          // of a wave, for a tile
+    using L = RowsLength<kTree, kTileKeys>;
+    // Sized at the launch: the compiler takes a workgroup that fills the LDS for one wave per SIMD whatever else it is told, and spreads its
+    // registers over both files, with copies between them in every tile.
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_char_t*)lds;
 
-    const int lane = threadIdx.x % kWaveSize, half = lane / kTile;
+    const int lane = threadIdx.x % kWaveSize;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const int wr = wave % kWR, wk = wave / kWR;
-    const int32_t head = blockIdx.x % a.Hkv;
-    const int32_t id = a.n_blocks - 1 - (int32_t)(blockIdx.x / a.Hkv);      // the last tokens of a sequence see most: they go first
-    const RowsBlock b = rows_block<kTree, kTileKeys>(a, id, lane);
-    if (b.tokens == 0) return;
-    const int32_t shares = rows_shares(a, b), share = blockIdx.y;
-    if (share >= shares) return;
-    const int32_t first_tile = share * a.tiles_per_share;
-    const int32_t end_tile = share + 1 == shares ? b.tiles : first_tile + a.tiles_per_share;
+    const TileAddress<E, D> place(lane);
 
-    // rows of this lane
-    QueryTile<E, D> q[kNQ];
-    int32_t token[kNQ], g[kNQ];
-#pragma unroll
-    for (int n = 0; n < kNQ; ++n) {
-        const uint32_t row = (wr * kNQ + n) * kTile + lane % kTile;
-        token[n] = (int32_t)(row / (uint32_t)a.G);
-        g[n] = (int32_t)(row - (uint32_t)token[n] * (uint32_t)a.G);
-        const int32_t t = token[n] < b.tokens ? token[n] : b.tokens - 1;
-        load_query<E, D>(q[n], a.Q + ((b.first_token + t) * a.q_stride + (int64_t)(head * a.G + g[n]) * D) * E::kBytes, half);
+    RowsItem it;
+    int64_t end, stretch = 0;                                  // of this workgroup's stretch
+    if (a.workgroups == 0) {
+        if (!rows_own_item<kTree, kTileKeys>(a, it, lane)) return;
+        end = kTileKeys + L::keys(a, it.q, it.block);
+    } else {
+        if (threadIdx.x == 0) a.joins[blockIdx.x].parts = 0;   // until an item begins here that ends elsewhere
+        if (!rows_stretch_item<kTree, kTileKeys>(a, it, stretch, end, lane)) return;
     }
-    const char* const K = a.K + ((int64_t)head * a.kv_head_stride + b.first_row * D) * E::kBytes;
-    const char* const V = a.V + ((int64_t)head * a.kv_head_stride + b.first_row * D) * E::kBytes;
-    const int64_t node_base = kTree ? ((int64_t)head * a.total_q + b.first_token - b.first_in_seq) * R::kBytes : 0;
+    for (int slot = 0;; slot = 1) {                            // one item after the other
+        int row = wr * kTile + lane % kTile, half = lane / kTile;
+        asm volatile("" : "+v"(row), "+v"(half));              // what follows from them is not held from item to item: registers
+        const int64_t keys = L::keys(a, it.q, it.block), item_end = it.start + kTileKeys + keys;
+        const int64_t here_end = (end < item_end ? end : item_end) - it.start;
+        // tile t stands at (t + 1) * kTileKeys of its item
+        const int32_t first_tile = it.at <= kTileKeys ? 0 : (int32_t)((it.at - 1) / kTileKeys);
+        const int32_t end_tile = here_end <= kTileKeys ? 0 : (int32_t)((here_end - 1) / kTileKeys);
+        const bool whole = it.at == 0 && item_end <= end;
+        const int32_t first_in_seq = it.block * a.tokens_per_block;
+        const int64_t first_token = it.q.q_first + first_in_seq;
+        const int32_t tokens = it.q.n_q - first_in_seq < a.tokens_per_block ? it.q.n_q - first_in_seq : a.tokens_per_block;
+        const int32_t row_tiles = kTree ? (int32_t)(((int64_t)it.q.n_rows + kTileKeys - 1) / kTileKeys) : 0x7fffffff;
+        const bool live = wr * kTile < tokens * a.G;           // this wave has rows
 
-    const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_char_t*)lds;
-    auto stage = [&](int32_t tile, int where) {
-        const uint32_t to = lds_at + where;
-        const bool nodes = kTree && tile >= b.row_tiles;
-        const int64_t k0 = (int64_t)(nodes ? tile - b.row_tiles : tile) * kTileKeys;
-        const char* const k = nodes ? a.Kt + node_base : K;
-        const char* const v = nodes ? a.Vt + node_base : V;
-        const int64_t rows = nodes ? b.n_tokens : b.n_rows;
-        stage_rows<E, D, kTileKeys, kWaves, false>(k, k0, rows, to, wave, lane);
-        stage_rows<E, D, kTileKeys, kWaves, true>(v, k0, rows, to + kHalf, wave, lane);
-    };
-    // Which of the 32 keys from k0 on a row sees.
-    auto seen = [&](bool nodes, int64_t k0, int n) -> uint32_t {
-        int64_t bound = (nodes ? b.n_tokens : b.n_rows) - k0;
-        if constexpr (!kTree) bound = (int64_t)b.first_in_seq + token[n] + 1 + b.n_rows - b.n_tokens - k0;
-        uint32_t bits = bound >= kTile ? ~0u : (bound <= 0 ? 0u : (1u << bound) - 1u);
-        if constexpr (kTree) {
-            if (nodes) {
-                const int64_t word = k0 / kTile;
-                const int32_t t = token[n] < b.tokens ? token[n] : b.tokens - 1;
-                bits &= word < a.mask_words ? a.mask[(b.first_token + t) * a.mask_words + word] : 0u;
-            }
-        }
-        return bits;
-    };
+        // of this lane; rows behind the last are copies of it and not stored
+        const int32_t t = row / a.G < tokens ? row / a.G : tokens - 1;
+        QueryTile<E, D> q;
+        auto load_queries = [&](int32_t r) {
+            const int32_t own = r / a.G < tokens ? r / a.G : tokens - 1, g = r % a.G;
+            load_query<E, D>(q, a.Q + ((first_token + own) * a.q_stride + (int64_t)(it.head * a.G + g) * D) * E::kBytes, half);
+        };
+        load_queries(row);
+        const char* const K = a.K + ((int64_t)it.head * a.kv_head_stride + it.q.row_first * D) * E::kBytes;
+        const char* const V = a.V + ((int64_t)it.head * a.kv_head_stride + it.q.row_first * D) * E::kBytes;
+        const int64_t node_base = kTree ? ((int64_t)it.head * a.total_q + it.q.q_first) * R::kBytes : 0;
 
-    // Tiles of which every row sees every key come first: no masks, and nothing that only masks need.
-    const int64_t open_keys = kTree ? b.n_rows : (int64_t)b.first_in_seq + 1 + b.n_rows - b.n_tokens;
-    int32_t open_end = open_keys < kTileKeys ? 0 : (int32_t)(open_keys / kTileKeys);
-    open_end = open_end < end_tile ? open_end : end_tile;
-
-    const TileAddress<E, D> at(lane);
-    RowState<E, D, kNQ> st;
-    st.clear();
-    auto open_tile = [&](const char* here) {
-#pragma unroll
-        for (int j = 0; j < kNK; ++j) {
-            const char* const k = here + (wk * kNK + j) * kTile * R::kBytes;
-            f32x16_t s[kNQ];
-            Weights<E> p[kNQ];
-            scores<E, D, kNQ>(k, at, q, s);
-            softmax_step<E, D, kNQ>(st, s, p, a.scale);
-            weighted_values<E, D, kNQ>(k + kHalf, at, p, st.o);
-        }
-    };
-    auto masked_tile = [&](const char* here, int32_t tile) {
-        const bool nodes = kTree && tile >= b.row_tiles;
-        const int64_t k0 = (int64_t)(nodes ? tile - b.row_tiles : tile) * kTileKeys;
-#pragma unroll 1
-        for (int j = 0; j < kNK; ++j) {
-            const int sub = (wk * kNK + j) * kTile;
-            const char* const k = here + sub * R::kBytes;
-            uint32_t bits[kNQ];
-            bool any = false;
-#pragma unroll
-            for (int n = 0; n < kNQ; ++n) {
-                bits[n] = seen(nodes, k0 + sub, n);
-                any |= bits[n] != 0;
-            }
-            if (__ballot(any) == 0) continue;
-            f32x16_t s[kNQ];
-            Weights<E> p[kNQ];
-            scores<E, D, kNQ>(k, at, q, s);
-#pragma unroll
-            for (int n = 0; n < kNQ; ++n) {
-                const uint32_t mine = bits[n] >> (4 * half);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[n][i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[n][i] : -__builtin_inff();
-            }
-            softmax_step<E, D, kNQ>(st, s, p, a.scale);
-            if (values_not_finite<E, D>(k + kHalf, lane)) {
-#pragma unroll
-                for (int n = 0; n < kNQ; ++n) weighted_values_seen<E, D>(k + kHalf, at, p[n], bits[n], st.o[n], lane);
-            } else {
-                weighted_values<E, D, kNQ>(k + kHalf, at, p, st.o);
-            }
-        }
-    };
-    int32_t tile = first_tile;
-    if (tile < end_tile) stage(tile, 0);
-    int here = 0;
-    for (; tile < open_end; ++tile) {
-        wait_loads_to_lds();
-        __syncthreads();                                       // the tile is there, and nobody reads the other one any more
-        if (tile + 1 < end_tile) stage(tile + 1, here ^ (2 * kHalf));
-        open_tile(lds + here);
-        here ^= 2 * kHalf;
-    }
-    for (; tile < end_tile; ++tile) {
-        wait_loads_to_lds();
-        __syncthreads();
-        if (tile + 1 < end_tile) stage(tile + 1, here ^ (2 * kHalf));
-        masked_tile(lds + here, tile);
-        here ^= 2 * kHalf;
-    }
-
-    if constexpr (kWK > 1) {
-        // the waves of a group join what they have of the same rows
-        __syncthreads();
-        float* const all = reinterpret_cast<float*>(lds);
-        constexpr int kWaveFloats = kNQ * (D / 2 + 2) * kWaveSize;
-        if (wk > 0) {
-            float* const mine = all + ((wk - 1) * kWR + wr) * kWaveFloats + lane;
-#pragma unroll
-            for (int n = 0; n < kNQ; ++n) {
-                float* const to = mine + n * (D / 2 + 2) * kWaveSize;
-                to[0] = st.m[n];
-                to[kWaveSize] = st.l[n];
-#pragma unroll
-                for (int d = 0; d < D / kTile; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) to[(2 + d * 16 + i) * kWaveSize] = st.o[n][d][i];
-            }
-        }
-        __syncthreads();
-        if (wk > 0) return;
-#pragma unroll 1
-        for (int other = 1; other < kWK; ++other) {
-#pragma unroll
-            for (int n = 0; n < kNQ; ++n) {
-                const float* const from = all + ((other - 1) * kWR + wr) * kWaveFloats + n * (D / 2 + 2) * kWaveSize + lane;
-                const float mo = from[0], m = fmaxf(st.m[n], mo);
-                const float f = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
-                const float fo = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(mo - m);
-                st.m[n] = m;
-                st.l[n] = st.l[n] * f + from[kWaveSize] * fo;
-#pragma unroll
-                for (int d = 0; d < D / kTile; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) st.o[n][d][i] = st.o[n][d][i] * f + from[(2 + d * 16 + i) * kWaveSize] * fo;
-            }
-        }
-    }
-
-#pragma unroll
-    for (int n = 0; n < kNQ; ++n) {
-        const float l = sum_of_halves(st.l[n]);
-        if (token[n] >= b.tokens) continue;
-        if (shares == 1) {
-            const float f = l == 0.f ? 0.f : 1.f / l;          // no key: zeros
-            char* const to = a.O + (((b.first_token + token[n]) * (int64_t)(a.Hkv * a.G) + head * a.G + g[n]) * D) * E::kBytes;
-#pragma unroll
-            for (int d = 0; d < D / kTile; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float v[4] = {st.o[n][d][4 * i] * f, st.o[n][d][4 * i + 1] * f, st.o[n][d][4 * i + 2] * f, st.o[n][d][4 * i + 3] * f};
-                    store_four<E>(to + (d * kTile + 8 * i + 4 * half) * E::kBytes, v);
+        auto stage = [&](int32_t tile, int where) {
+            const bool nodes = kTree && tile >= row_tiles;
+            const int64_t k0 = (int64_t)(nodes ? tile - row_tiles : tile) * kTileKeys;
+            const int64_t rows = nodes ? it.q.n_q : it.q.n_rows;
+            stage_rows<E, D, kTileKeys, kWaves, false>(nodes ? a.Kt + node_base : K, k0, rows, lds_at + where, wave, lane);
+            stage_rows<E, D, kTileKeys, kWaves, true>(nodes ? a.Vt + node_base : V, k0, rows, lds_at + where + kHalf, wave, lane);
+        };
+        // Which of the 32 keys from k0 on the lane's row sees.
+        auto seen = [&](bool nodes, int64_t k0) -> uint32_t {
+            int64_t bound = (nodes ? it.q.n_q : it.q.n_rows) - k0;
+            if constexpr (!kTree) bound = (int64_t)first_in_seq + t + 1 + it.q.n_rows - it.q.n_q - k0;
+            uint32_t bits = bound >= kTile ? ~0u : (bound <= 0 ? 0u : (1u << bound) - 1u);
+            if constexpr (kTree) {
+                if (nodes) {
+                    const int64_t word = k0 / kTile;
+                    bits &= word < a.mask_words ? a.mask[(first_token + t) * a.mask_words + word] : 0u;
                 }
-        } else {
-            const int64_t row = (((int64_t)id * a.Hkv + head) * a.max_shares + share) * a.block_rows + token[n] * a.G + g[n];
-            float* const to = a.partial + row * (D + 2);
-            // rows of D + 2 floats: eight bytes are what they are aligned to
+            }
+            return bits;
+        };
+        // Tiles of which every row sees every key come first: no masks, and nothing that only masks need.
+        const int64_t open_keys = kTree ? it.q.n_rows : (int64_t)first_in_seq + 1 + it.q.n_rows - it.q.n_q;
+        int32_t open_end = open_keys < kTileKeys ? 0 : (int32_t)(open_keys / kTileKeys);
+        open_end = open_end < end_tile ? open_end : end_tile;
+
+        RowState<E, D> st;
+        st.clear();
+        TileAddress<E, D> at = place;
+        auto open_tile = [&](const char* here) {
 #pragma unroll
-            for (int d = 0; d < D / kTile; ++d)
+            for (int j = 0; j < kNK; ++j) {
+                const char* const k = here + (wk * kNK + j) * kTile * R::kBytes;
+                if constexpr (R::kBytes == 512) at.forget();
+                f32x16_t s[1];
+                Weights<E> p[1];
+                scores<E, D>(k, at, q, s[0]);
+                softmax_step<E, D>(st, s, p, a.scale);
+                weighted_values<E, D>(k + kHalf, at, p[0], st.o);
+            }
+        };
+        auto masked_tile = [&](const char* here, int32_t tile) {
+            const bool nodes = kTree && tile >= row_tiles;
+            const int64_t k0 = (int64_t)(nodes ? tile - row_tiles : tile) * kTileKeys;
+#pragma unroll 1
+            for (int j = 0; j < kNK; ++j) {
+                const int sub = (wk * kNK + j) * kTile;
+                const char* const k = here + sub * R::kBytes;
+                const uint32_t bits = seen(nodes, k0 + sub);
+                if (__ballot(bits != 0) == 0) continue;
+                TileAddress<E, D> at = place;
+                if constexpr (R::kBytes == 512) {
+                    // queries are read again and places worked out again instead of held: registers, for the few tiles with masks
+                    int32_t again = row;
+                    asm volatile("" : "+v"(again));
+                    load_queries(again);
+                    at.forget();
+                }
+                f32x16_t s[1];
+                Weights<E> p[1];
+                scores<E, D>(k, at, q, s[0]);
+                const uint32_t mine = bits >> (4 * half);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 16; ++i) s[0][i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[0][i] : -__builtin_inff();
+                softmax_step<E, D>(st, s, p, a.scale);
+                // Long rows have no registers for two ways of adding the same products: they take the careful one always.
+                if (R::kBytes == 512 || values_not_finite<E, D>(k + kHalf, lane)) {
+                    if (finite_values<E, D>(k + kHalf, at, p[0], st.o)) other_values<E, D>(k + kHalf, at, p[0], bits, st.o, lane);
+                } else {
+                    weighted_values<E, D>(k + kHalf, at, p[0], st.o);
+                }
+            }
+        };
+        int32_t tile = first_tile, staged = first_tile;
+        int here = 0, there = 0;                               // where the tile is, and where the next one goes
+        auto after = [&](int slot_at) { return slot_at + 2 * kHalf < kStages * 2 * kHalf ? slot_at + 2 * kHalf : 0; };
+        auto stage_next = [&] {
+            if (staged < end_tile) {
+                stage(staged++, there);
+                there = after(there);
+            }
+        };
+        // The tile is there for all waves, and the one before it is not read any more: its place takes the next.
+        auto next_tile = [&] {
+            wait_loads_to_lds<kLoads, kStages - 2>(staged - tile - 1);
+            __syncthreads();
+            stage_next();
+        };
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        *reinterpret_cast<float2*>(to + d * kTile + 8 * i + 4 * half + 2 * j) =
-                            make_float2(st.o[n][d][4 * i + 2 * j], st.o[n][d][4 * i + 2 * j + 1]);
-            if (half == 0) *reinterpret_cast<float2*>(to + D) = make_float2(st.m[n], l);
+        for (int i = 0; i < kStages - 1; ++i) stage_next();
+        for (; tile < open_end; ++tile) {
+            next_tile();
+            if (live) open_tile(lds + here);
+            here = after(here);
         }
+        for (; tile < end_tile; ++tile) {
+            next_tile();
+            if (live) masked_tile(lds + here, tile);
+            here = after(here);
+        }
+
+        if constexpr (kWK > 1) {
+            // the waves of a group join what they have of the same rows
+            __syncthreads();
+            float* const all = reinterpret_cast<float*>(lds);
+            constexpr int kWaveFloats = (D / 2 + 2) * kWaveSize;
+            if (wk > 0) {
+                float* const to = all + ((wk - 1) * kWR + wr) * kWaveFloats + lane;
+                to[0] = st.m;
+                to[kWaveSize] = st.l;
+#pragma unroll
+                for (int d = 0; d < D / kTile; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) to[(2 + d * 16 + i) * kWaveSize] = st.o[d][i];
+            }
+            __syncthreads();
+            if (wk == 0) {
+#pragma unroll 1
+                for (int other = 1; other < kWK; ++other) {
+                    const float* const from = all + ((other - 1) * kWR + wr) * kWaveFloats + lane;
+                    const float mo = from[0], m = fmaxf(st.m, mo);
+                    const float f = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+                    const float fo = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(mo - m);
+                    st.m = m;
+                    st.l = st.l * f + from[kWaveSize] * fo;
+#pragma unroll
+                    for (int d = 0; d < D / kTile; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) st.o[d][i] = st.o[d][i] * f + from[(2 + d * 16 + i) * kWaveSize] * fo;
+                }
+            }
+        }
+
+        const float l = sum_of_halves(st.l);
+        int32_t out_row = row, out_half = half;
+        asm volatile("" : "+v"(out_row), "+v"(out_half));      // nor from its beginning to its end
+        const int32_t token = out_row / a.G;
+        if (wk == 0 && token < tokens) {
+            if (whole) {
+                const float f = l == 0.f ? 0.f : 1.f / l;      // no key: zeros
+                char* const to = a.O + (((first_token + token) * (int64_t)(a.Hkv * a.G) + it.head * a.G + out_row - token * a.G) * D) * E::kBytes;
+#pragma unroll
+                for (int d = 0; d < D / kTile; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x16_t& o = st.o[d];
+                        const float v[4] = {o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f};
+                        store_four<E>(to + (d * kTile + 8 * i + 4 * out_half) * E::kBytes, v);
+                    }
+            } else {
+                float* const to = a.partial + (((int64_t)blockIdx.x * 2 + slot) * kBlockRows + out_row) * rows_partial_floats(D);
+#pragma unroll
+                for (int d = 0; d < D / kTile; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x16_t& o = st.o[d];
+                        *reinterpret_cast<f32x4_t*>(to + d * kTile + 8 * i + 4 * out_half) = f32x4_t{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                    }
+                if (out_half == 0) *reinterpret_cast<float2*>(to + D) = make_float2(st.m, l);
+            }
+        }
+        if (item_end >= end) {
+            if (it.at == 0 && item_end > end && threadIdx.x == 0)
+                a.joins[blockIdx.x] = RowsJoin{first_token * (a.Hkv * a.G) + it.head * a.G, (int32_t)quotient(item_end - 1, stretch) - (int32_t)blockIdx.x + 1,
+                                               tokens * a.G, slot, 0};
+            return;
+        }
+        // the next item, from its beginning
+        it.start = item_end;
+        it.at = 0;
+        if (++it.block >= it.q.blocks) {
+            it.block = 0;
+            if (++it.head == a.Hkv) {
+                it.head = 0;
+                do it.q = uniform(rows_seq(a, ++it.seq));      // one with tokens follows: the stretch does not end here
+                while (it.q.blocks == 0 && it.seq + 1 < a.n_seq);
+            }
+        }
+        __syncthreads();                                       // before the first tile goes where this item's were
     }
 }
 
-// One wave per query row: the shares of the row's block, each relative to its own maximum, in the order of the keys.
-template <typename E, int D, int kTileKeys, bool kTree>
-__global__ __launch_bounds__(256)
+// Joins what several workgroups have of an item, for the workgroup in whose stretch it begins (blockIdx.y; rows come first in the launch,
+// so that those of one item are spread over all dies).  Four elements of a row a lane; the parts of a row in the order of the keys,
+// eight on their way at a time.
+constexpr int kJoinThreads = 256;
+template <typename E, int D, int kBlockRows>
+__global__ __launch_bounds__(kJoinThreads)
 void rows_join_kernel(const RowsArgs a) {
-    constexpr int kPer = D / kWaveSize;                        // elements of a lane: consecutive
-    const int lane = threadIdx.x % kWaveSize;
-    const int32_t head = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
-    const RowsBlock b = rows_block<kTree, kTileKeys>(a, id, lane);
-    if (b.tokens == 0) return;
-    const int32_t shares = rows_shares(a, b);
-    if (shares == 1) return;
-    for (int32_t row = blockIdx.y * 4 + threadIdx.x / kWaveSize; row < b.tokens * a.G; row += gridDim.y * 4) {
-        const float* const first = a.partial + ((((int64_t)id * a.Hkv + head) * a.max_shares) * a.block_rows + row) * (D + 2);
-        const int64_t step = (int64_t)a.block_rows * (D + 2);
-        float m = -__builtin_inff();
-        for (int32_t s = 0; s < shares; ++s) m = fmaxf(m, first[s * step + D]);
-        float l = 0.f, o[kPer] = {};
-        for (int32_t s = 0; s < shares; ++s) {
-            const float ms = first[s * step + D], f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ms - m);
-            if (ms == -__builtin_inff()) continue;             // a share without a key that the row sees
-            l += first[s * step + D + 1] * f;
+    constexpr int64_t kPart = (int64_t)kBlockRows * rows_partial_floats(D);
+    constexpr int kLanes = D / 4, kAhead = 8;
+    const RowsJoin join = a.joins[blockIdx.y];
+    const int32_t row = blockIdx.x * (kJoinThreads / kLanes) + threadIdx.x / kLanes, parts = join.parts;
+    if (row >= join.rows || parts == 0) return;
+    const int c = threadIdx.x % kLanes;
+    const float* const mine = a.partial + ((int64_t)blockIdx.y * 2 * kBlockRows + row) * rows_partial_floats(D);
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int32_t p = 0; p < parts; p += kAhead) {
+        f32x4_t x[kAhead];
+        float2 ml[kAhead];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) o[i] += first[s * step + lane * kPer + i] * f;
+        for (int u = 0; u < kAhead; ++u) {
+            if (p + u < parts) {
+                // two parts for each workgroup; the first may be its second, where another item ends before it
+                const float* const from = mine + (p + u == 0 ? join.slot : 2 * (p + u)) * kPart;
+                x[u] = *reinterpret_cast<const f32x4_t*>(from + 4 * c);
+                ml[u] = *reinterpret_cast<const float2*>(from + D);
+            }
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        const int32_t token = row / a.G, g = row % a.G;
-        char* const at = a.O + (((b.first_token + token) * (int64_t)(a.Hkv * a.G) + head * a.G + g) * D + lane * kPer) * E::kBytes;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if constexpr (E::kBytes == 4) reinterpret_cast<float*>(at)[i] = o[i] * f;
-            else reinterpret_cast<__bf16*>(at)[i] = (__bf16)(o[i] * f);
+        for (int u = 0; u < kAhead; ++u) {
+            if (p + u < parts && ml[u].x != -__builtin_inff()) {       // a part with a key that the row sees
+                const float top = fmaxf(m, ml[u].x), old = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml[u].x - top);
+                m = top;
+                l = l * old + ml[u].y * f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = o[i] * old + x[u][i] * f;
+            }
         }
     }
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    const int32_t token = row / a.G, g = row - token * a.G;
+    const float v[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
+    store_four<E>(a.O + ((join.first_row + (int64_t)token * (a.Hkv * a.G) + g) * D + 4 * c) * E::kBytes, v);
 }
 
-// The two shapes of workgroup a row type has.  wide: many rows, the keys of a tile seen by all waves; narrow: 32 rows, the keys of a
-// tile divided among the waves.
-template <typename E, int D> struct RowsShapes {
-    static constexpr bool kLong = AttnRow<E, D>::kBytes == 512;
-    static constexpr int kWideNQ = 1, kWideWR = kLong ? 4 : 8, kWideNK = kLong ? 1 : 2;
-    static constexpr int kNarrowWK = kLong ? 2 : 4;
-    static constexpr int kWideRows = kWideNQ * kWideWR * kTile, kWideKeys = kWideNK * kTile, kNarrowKeys = kNarrowWK * kTile;
-};
+// The shapes of workgroup a row type has: rows of a block (32 * kWR) and keys of a tile (32 * kWK * kNK).  One workgroup to a compute unit: of
+// two, the younger gets the memory that the older leaves (122 us instead of 94 for equal stretches of a batch of trees).
+template <int kRowBytes, int kShape> struct RowsShape;
+template <int kRowBytes> struct RowsShape<kRowBytes, 0> { static constexpr int kWR = 8, kWK = 1, kNK = 2, kStages = 2; };
+template <int kRowBytes> struct RowsShape<kRowBytes, 1> { static constexpr int kWR = 4, kWK = 2, kNK = 2, kStages = 2; };
+template <int kRowBytes> struct RowsShape<kRowBytes, 2> { static constexpr int kWR = 2, kWK = 2, kNK = 1, kStages = 4; };
+template <int kRowBytes> struct RowsShape<kRowBytes, 3> { static constexpr int kWR = 1, kWK = 4, kNK = 1, kStages = 2; };
+template <> struct RowsShape<512, 0> { static constexpr int kWR = 8, kWK = 1, kNK = 1, kStages = 4; };
+template <> struct RowsShape<512, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 1, kStages = 4; };
+template <> struct RowsShape<512, 2> { static constexpr int kWR = 2, kWK = 1, kNK = 1, kStages = 4; };
+template <> struct RowsShape<512, 3> { static constexpr int kWR = 1, kWK = 2, kNK = 1, kStages = 2; };
 
-template <typename E, int D, bool kTree>
-l2kv_status rows_attn_launch(const RowsArgs& a, bool wide, hipStream_t stream) {
-    using S = RowsShapes<E, D>;
-    const dim3 grid((unsigned)(a.n_blocks * a.Hkv), (unsigned)a.max_shares);
-    if (wide)
-        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWideNQ, S::kWideWR, 1, S::kWideNK, kTree>), grid, dim3(S::kWideWR * kWaveSize), 0, stream, a);
-    else
-        hipLaunchKernelGGL((rows_attn_kernel<E, D, 1, 1, S::kNarrowWK, 1, kTree>), grid, dim3(S::kNarrowWK * kWaveSize), 0, stream, a);
-    if (a.max_shares > 1) {
+template <typename E, int D, int kShape, bool kTree>
+l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
+    using S = RowsShape<AttnRow<E, D>::kBytes, kShape>;
+    constexpr int kRows = S::kWR * kTile;
+    constexpr unsigned kLds = S::kStages * 2 * S::kWK * S::kNK * kTile * AttnRow<E, D>::kBytes;
+    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+    const dim3 grid((unsigned)(a.workgroups == 0 ? a.n_blocks * a.Hkv : a.workgroups));
+    hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree>), grid, dim3(S::kWR * S::kWK * kWaveSize), kLds, stream, a);
+    if (a.workgroups > 1) {
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
-        const dim3 join((unsigned)(a.n_blocks * a.Hkv), (unsigned)((a.block_rows + 3) / 4));
-        if (wide) hipLaunchKernelGGL((rows_join_kernel<E, D, S::kWideKeys, kTree>), join, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((rows_join_kernel<E, D, S::kNarrowKeys, kTree>), join, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((rows_join_kernel<E, D, kRows>), dim3(kRows * (D / 4) / kJoinThreads, (unsigned)a.workgroups), dim3(kJoinThreads), 0, stream, a);
     }
     return launch_status();
+}
+
+template <typename E, int D, bool kTree>
+l2kv_status rows_attn_launch(const RowsArgs& a, int shape, hipStream_t stream) {
+    switch (shape) {
+        case 0: return rows_attn_launch_shape<E, D, 0, kTree>(a, stream);
+        case 1: return rows_attn_launch_shape<E, D, 1, kTree>(a, stream);
+        case 2: return rows_attn_launch_shape<E, D, 2, kTree>(a, stream);
+        default: return rows_attn_launch_shape<E, D, 3, kTree>(a, stream);
+    }
 }
 
 }  // namespace l2kv
