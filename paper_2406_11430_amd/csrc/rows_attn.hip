@@ -40,7 +40,9 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     const int64_t tiles = max_kv / s.keys + 2;                     // of an item, at most (its nodes in one)
     // Many items, or items that are not worth cutting: a workgroup each.
     p.workgroups = 0;
-    p.least_tiles = dt == L2KV_F32 ? 3 : 5;                        // one is what an item counts for by itself
+    // Two tiles of keys and the one that an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 18.3 us, 23.0 with
+    // four tiles.
+    p.least_tiles = 3;
     if (items < 4 * slots && tiles > 6 && n_seq <= 1024) {
         const int64_t most = items * tiles / (p.least_tiles - 1);
         p.workgroups = (int32_t)(most < slots ? most : slots);
