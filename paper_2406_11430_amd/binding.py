@@ -1,5 +1,5 @@
 """Binding of libl2kv.so: one Python function per C entry point, same
-names, argument marshalling only (ctypes; the calls of a decode step and the compression also natively, csrc/calls.cpp).  Tensors are torch CUDA(HIP) tensors used as
+names, argument marshalling only (ctypes; the calls of a decode step, plain or drafted, of prompts and the compression also natively, csrc/calls.cpp).  Tensors are torch CUDA(HIP) tensors used as
 device memory; every step of the path runs inside the library's kernels.
 
 The library must already be built (``python -m paper_2406_11430_amd.build``);
@@ -125,7 +125,7 @@ _calls = None
 
 class _PythonCalls:
     """In place of the native calls: leaves every call to the checks and the marshalling in this file."""
-    decode_attn = decode_attn_out = compress = staticmethod(lambda *args: None)
+    decode_attn = decode_attn_out = compress = rotary_append = prompt_attn = tree_attn = append_path = staticmethod(lambda *args: None)
 
 
 def _load_calls():
@@ -147,8 +147,9 @@ def calls():
         handle = lib()
         try:
             module = _load_calls()
-            module.bind(*(C.cast(f, C.c_void_p).value for f in (handle.l2kv_decode_attn, handle.l2kv_decode_attn_out,
-                                                               handle.l2kv_compress, handle.l2kv_keep_count)))
+            module.bind(*(C.cast(f, C.c_void_p).value for f in (
+                handle.l2kv_decode_attn, handle.l2kv_decode_attn_out, handle.l2kv_compress, handle.l2kv_keep_count,
+                handle.l2kv_rotary_append, handle.l2kv_prompt_attn, handle.l2kv_tree_attn, handle.l2kv_stream_append_path)))
         except ImportError as e:
             warnings.warn("%s; calls go through ctypes (build with `python -m paper_2406_11430_amd.build`)" % e, RuntimeWarning)
             module = _PythonCalls
@@ -542,6 +543,10 @@ def l2kv_rotary_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tens
                        amplitude: float = 1.0, stream=None) -> None:
     """Q ``[tokens, Hq, D]`` -> Qr (same shape, dense); K, V ``[tokens, Hkv, D]`` -> Kc, Vc ``[Hkv, total_slots, D]``,
     norms_c, pos_c ``[Hkv, total_slots]``.  The tokens of Q, K and V may be any distance apart (parts of one projection)."""
+    st = (_calls or calls()).rotary_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, slot_offsets, lens_in,
+                                         lens_out, layout, amplitude, stream, _stream)
+    if st is not None:
+        return _check("l2kv_rotary_append", st)
     _dev(positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, slot_offsets, lens_in, lens_out)
     total, Hkv, D = K.shape
     k_stride, v_stride = _tokens(K), _tokens(V)
@@ -597,6 +602,9 @@ def l2kv_prompt_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, q_offset
                      workspace: Optional[torch.Tensor], scale: float = 0.0, stream=None) -> None:
     """Q ``[total_q, Hq, D]`` (tokens any distance apart), K/V ``[Hkv, rows, D]`` or ``[B, Hkv, T, D]`` -> O ``[total_q, Hq, D]``
     of Q's type.  Offsets are device int64 ``[n_seq + 1]`` (in rows; of a ``[B, Hkv, T, D]`` cache b*Hkv*T), kv_lens int32 or None."""
+    st = (_calls or calls()).prompt_attn(Q, K, V, q_offsets, kv_offsets, kv_lens, max_kv, O, workspace, scale, stream, _stream)
+    if st is not None:
+        return _check("l2kv_prompt_attn", st)
     _dev(q_offsets, kv_offsets, kv_lens, O, workspace)
     total_q, Hq, D = Q.shape
     q_stride = _tokens(Q)
@@ -617,6 +625,9 @@ def l2kv_tree_attn(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, lens: to
                    O: torch.Tensor, workspace: Optional[torch.Tensor], scale: float = 0.0, stream=None) -> None:
     """Q ``[nodes, Hq, D]``, Kc/Vc ``[Hkv, total_slots, D]`` or ``[B, Hkv, T, D]``, Kt/Vt ``[Hkv, nodes, D]``, mask
     ``[nodes, words]`` int32 (bit j of a row: its node sees node j of its sequence) -> O ``[nodes, Hq, D]`` of Q's type."""
+    st = (_calls or calls()).tree_attn(Q, Kc, Vc, lens, slot_offsets, max_len, Kt, Vt, node_offsets, mask, O, workspace, scale, stream, _stream)
+    if st is not None:
+        return _check("l2kv_tree_attn", st)
     _dev(lens, slot_offsets, Kt, Vt, node_offsets, mask, O, workspace)
     total, Hq, D = Q.shape
     q_stride = _tokens(Q)
@@ -639,6 +650,10 @@ def l2kv_stream_append_path(Kt: torch.Tensor, Vt: torch.Tensor, norms_t: torch.T
                             Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor,
                             stream=None) -> None:
     """Rows path ``[n_seq, max_path]`` (path_lens of each) of the nodes ``[n_planes, total_nodes, D]`` -> the next free slots."""
+    st = (_calls or calls()).append_path(Kt, Vt, norms_t, pos_t, node_offsets, path, path_lens, slot_offsets, lens_in, lens_out,
+                                       Kc, Vc, norms_c, pos_c, stream, _stream)
+    if st is not None:
+        return _check("l2kv_stream_append_path", st)
     _dev(Kt, Vt, norms_t, pos_t, node_offsets, path, path_lens, slot_offsets, lens_in, lens_out, Kc, Vc, norms_c, pos_c)
     n_planes, total, D = Kt.shape
     n_seq, max_path = path.shape
