@@ -14,38 +14,69 @@ extern template l2kv_status rows_attn_launch<F32, 64, true>(const RowsArgs&, int
 extern template l2kv_status rows_attn_launch<F32, 128, false>(const RowsArgs&, int, hipStream_t);
 extern template l2kv_status rows_attn_launch<F32, 128, true>(const RowsArgs&, int, hipStream_t);
 
+constexpr int kNarrowest = 2;              // of the shapes; 0 is the widest
 struct ShapeSizes { int32_t rows, keys; };
 template <int kRowBytes, int kShape> static constexpr ShapeSizes sizes_of() {
     using S = RowsShape<kRowBytes, kShape>;
     return {S::kWR * kTile, S::kWK * S::kNK * kTile};
 }
 template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
-    constexpr ShapeSizes all[4] = {sizes_of<kRowBytes, 0>(), sizes_of<kRowBytes, 1>(), sizes_of<kRowBytes, 2>(), sizes_of<kRowBytes, 3>()};
+    constexpr ShapeSizes all[3] = {sizes_of<kRowBytes, 0>(), sizes_of<kRowBytes, 1>(), sizes_of<kRowBytes, 2>()};
     return all[shape];
 }
 
-RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
+// Which block of rows a launch takes and whether a workgroup has an item for itself or an equal stretch of all of them.  Wide blocks read
+// K and V least often; two workgroups of a narrow one share a compute unit, so that one computes while the other begins or ends an item, and
+// there are more of them.  Measured (bf16, D 128, 8 KV heads of 4 query heads, us):
+//                                         256 rows  128 rows  64 rows  stretches
+//   1 prompt of 8192 tokens                    544       570      638        652    (most work: the widest block)
+//   64 prompts of 64                          36.7      31.4     38.7       39.2    (two and more 128-row workgroups for each compute unit)
+//   1 prompt of 512                           23.3      20.5     14.7       23.7    (few: the narrowest)
+//   32 trees of 4 nodes over 1024 rows each: as many bytes in either, 57
+//   4 prompts' next 64 tokens over 16000       421       368      240         94    (few and long: stretches, of the block that takes the rows)
+//   1 tree of 64 nodes over 8192               220       192      108       30.8    (K and V are in the caches: stretches of the narrowest)
+// Over 90 sizes of all row types what this chooses takes 3 % longer than the best of the six, and no fixed choice of one less than 40 %.
+RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree) {
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
+    const int64_t units = device_compute_units(), mean = (total_q + n_seq - 1) / n_seq;
     auto sizes = [&](int shape) { return row_bytes == 128 ? shape_sizes<128>(shape) : (row_bytes == 256 ? shape_sizes<256>(shape) : shape_sizes<512>(shape)); };
-    RowsPlan p;
+    auto items = [&](int shape) {
+        const int64_t tokens = sizes(shape).rows / G;
+        return (mean + tokens - 1) / tokens * n_seq * Hkv;
+    };
     // the smallest block that takes the rows of a sequence, somewhat more than the average where there are several
-    const int64_t rows = total_q * G / n_seq, room = n_seq == 1 ? rows : rows + rows / 4;
-    p.shape = 3;
+    const int64_t rows = mean * G, room = n_seq == 1 ? rows : rows + rows / 4;
+    RowsPlan p;
+    p.shape = kNarrowest;
     while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
+    const int64_t longest = max_kv + (tree ? mean : 0);            // keys of an item
+    bool stretches = false;
+    if (p.shape == 0 && longest >= 2048 && items(0) >= 2 * units) {
+    } else if (p.shape < kNarrowest && items(1) >= 2 * units) {
+        p.shape = 1;
+    } else {
+        // Of the narrowest block: the keys of the longest item, with something for two in a compute unit, against those of a stretch, with
+        // 8 tiles' time for its beginning and the join.  Stretches of the widest block take 0.6 of the time for the same keys.
+        const int64_t n = items(kNarrowest), tile = sizes(kNarrowest).keys;
+        const bool cached = (double)max_kv * n_seq * Hkv * row_bytes * 2 <= 40e6;          // a little more than the L2s hold
+        if (p.shape == 0 && cached) p.shape = kNarrowest;
+        const double own = (double)longest * (n > units ? 1.3 : 1.0);
+        const double keys = (double)longest - (tree ? 0.0 : 0.5 * (double)(mean < longest ? mean : longest));
+        const double even = (double)(8 * tile) + (double)n * keys / (double)units * (p.shape == 0 ? 0.6 : 1.0);
+        stretches = n < 2 * units && own > even && n_seq <= 1024;      // the search for a stretch's beginning goes over all sequences
+        if (!stretches) p.shape = kNarrowest;
+    }
     const ShapeSizes s = sizes(p.shape);
     p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
     p.n_blocks = (int32_t)blocks;
-    const int64_t items = blocks * Hkv, slots = device_compute_units();
-    const int64_t tiles = max_kv / s.keys + 2;                     // of an item, at most (its nodes in one)
-    // Many items, or items that are not worth cutting: a workgroup each.
-    p.workgroups = 0;
     // Two tiles of keys and the one that an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 18.3 us, 23.0 with
     // four tiles.
     p.least_tiles = 3;
-    if (items < 4 * slots && tiles > 6 && n_seq <= 1024) {
-        const int64_t most = items * tiles / (p.least_tiles - 1);
-        p.workgroups = (int32_t)(most < slots ? most : slots);
+    p.workgroups = 0;
+    if (stretches) {
+        const int64_t most = blocks * Hkv * (max_kv / s.keys + 2) / (p.least_tiles - 1);
+        p.workgroups = (int32_t)(most < units ? most : units);
     }
     p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * s.rows * rows_partial_floats(D) * sizeof(float);
     p.bytes = p.workgroups < 2 ? 0 : p.partial_bytes + (size_t)p.workgroups * sizeof(RowsJoin);

@@ -82,6 +82,11 @@ __device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
 }
 
+__device__ __forceinline__ RowsSeq of_lane(const RowsSeq& q, int lane) {
+    return RowsSeq{of_lane(q.q_first, lane), of_lane(q.row_first, lane), __builtin_amdgcn_readlane(q.n_q, lane),
+                   __builtin_amdgcn_readlane(q.n_rows, lane), __builtin_amdgcn_readlane(q.blocks, lane)};
+}
+
 // Keys of a stretch where all items count for `total`: the same for every workgroup, but at least some tiles, so that short problems are
 // not cut to pieces.
 template <int kTileKeys> __device__ __forceinline__ int64_t rows_stretch(const RowsArgs& a, int64_t total) {
@@ -122,8 +127,7 @@ __device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& i
     }
     const int which = __builtin_ctzll(behind);
     it.seq = s0 + which;
-    it.q = RowsSeq{of_lane(q.q_first, which), of_lane(q.row_first, which), __builtin_amdgcn_readlane(q.n_q, which),
-                   __builtin_amdgcn_readlane(q.n_rows, which), __builtin_amdgcn_readlane(q.blocks, which)};
+    it.q = of_lane(q, which);
     int64_t rest = begin - base - of_lane(upto - mine, which);
     const int64_t head_keys = L::before(a, it.q, it.q.blocks);
     it.head = (int32_t)quotient(rest, head_keys);
@@ -144,32 +148,43 @@ __device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& i
     return true;
 }
 
-// The item of a workgroup of its own.  Blocks are counted so that sequence s has ids from q_off[s] / tokens_per_block + s on: room for all
-// its blocks, and which sequence an id belongs to is found among the offsets alone, 64 at a time.
+// The item of a workgroup of its own: blocks are numbered over the sequences without gaps, found by a sum over the offsets, a part of the
+// sequences for each lane (more than 64 in two rounds).  (Workgroups without a block behind those that have one do no harm; between
+// them they did, as the hardware deals workgroups out in turn: a batch whose every other number was empty ran on half of the device.)
 template <bool kTree, int kTileKeys>
 __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, int lane) {
     it.head = (int32_t)(blockIdx.x % (uint32_t)a.Hkv);
-    const int32_t id = a.n_blocks - 1 - (int32_t)(blockIdx.x / (uint32_t)a.Hkv);      // the last tokens of a sequence see most: they go first
+    int32_t block = -1 - (int32_t)(blockIdx.x / (uint32_t)a.Hkv);      // from the end: the last tokens of a sequence see most, they go first
     int32_t lo = 0, count = a.n_seq;
-    while (count > 1) {
+    for (bool all = true;; all = false) {
         const int32_t step = (count + kWaveSize - 1) / kWaveSize;
-        const int32_t mine = lo + lane * step;
-        bool at_or_before = false;
-        if ((int64_t)lane * step < count) {
-            const int64_t off = a.q_off[mine], inside = off < 0 ? 0 : (off < a.total_q ? off : a.total_q);
-            at_or_before = (int64_t)((uint32_t)inside / (uint32_t)a.tokens_per_block) + mine <= id;
+        RowsSeq q = {};
+        uint32_t mine = 0;
+        if (step <= 1) {
+            if (lane < count) q = rows_seq(a, lo + lane);
+            mine = (uint32_t)q.blocks;
+        } else {
+            for (int32_t n = 0; n < step; ++n) {
+                const int32_t s = lane * step + n;
+                if (s < count) mine += ((uint32_t)clamped_range(a.q_off, lo + s, a.total_q).count + (uint32_t)a.tokens_per_block - 1) / (uint32_t)a.tokens_per_block;
+            }
         }
-        const uint64_t found = __ballot(at_or_before);
-        const int32_t last = found == 0 ? 0 : 63 - __builtin_clzll(found);
-        lo += last * step;
-        count = count - last * step < step ? count - last * step : step;
+        const uint32_t upto = wave_inclusive_sum(mine);
+        if (all) block += __builtin_amdgcn_readlane((int)upto, kWaveSize - 1);
+        const uint64_t behind = __ballot((int32_t)upto > block);
+        if (block < 0 || behind == 0) return false;
+        const int which = __builtin_ctzll(behind);
+        block -= __builtin_amdgcn_readlane((int)(upto - mine), which);
+        if (step <= 1) {
+            it.seq = lo + which;
+            it.q = of_lane(q, which);
+            it.block = block;
+            it.start = it.at = 0;
+            return block >= 0 && block < it.q.blocks;
+        }
+        lo += which * step;
+        count = count - which * step < step ? count - which * step : step;
     }
-    it.seq = __builtin_amdgcn_readfirstlane(lo);
-    it.q = uniform(rows_seq(a, it.seq));
-    const int64_t block = uniform(id - ((int64_t)((uint32_t)it.q.q_first / (uint32_t)a.tokens_per_block) + it.seq));
-    it.block = (int32_t)block;
-    it.start = it.at = 0;
-    return block >= 0 && block < it.q.blocks;
 }
 
 template <typename E> __device__ __forceinline__ void store_four(char* at, const float (&v)[4]) {
@@ -191,7 +206,6 @@ void rows_attn_kernel(const RowsArgs a) {
     using R = AttnRow<E, D>;
     constexpr int kWaves = kWR * kWK, kTileKeys = kWK * kNK * kTile, kBlockRows = kWR * kTile;
     constexpr int kHalf = kTileKeys * R::kBytes;               // bytes of a tile of K, and of one of V
-    constexpr int kJoinFloats = (kWK - 1) * kWR * (D / 2 + 2) * kWaveSize;
     constexpr int kLoads = 2 * kHalf / 1024 / kWaves;          // of a wave, for a tile
     using L = RowsLength<kTree, kTileKeys>;
     // Sized at the launch: the compiler takes a workgroup that fills the LDS for one wave per SIMD whatever else it is told, and spreads its
@@ -470,13 +484,11 @@ void rows_join_kernel(const RowsArgs a) {
 // two, the younger gets the memory that the older leaves (122 us instead of 94 for equal stretches of a batch of trees).
 template <int kRowBytes, int kShape> struct RowsShape;
 template <int kRowBytes> struct RowsShape<kRowBytes, 0> { static constexpr int kWR = 8, kWK = 1, kNK = 2, kStages = 2; };
-template <int kRowBytes> struct RowsShape<kRowBytes, 1> { static constexpr int kWR = 4, kWK = 2, kNK = 2, kStages = 2; };
-template <int kRowBytes> struct RowsShape<kRowBytes, 2> { static constexpr int kWR = 2, kWK = 2, kNK = 1, kStages = 4; };
-template <int kRowBytes> struct RowsShape<kRowBytes, 3> { static constexpr int kWR = 1, kWK = 4, kNK = 1, kStages = 2; };
+template <int kRowBytes> struct RowsShape<kRowBytes, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 2, kStages = 2; };
+template <int kRowBytes> struct RowsShape<kRowBytes, 2> { static constexpr int kWR = 2, kWK = 2, kNK = 1, kStages = 2; };
 template <> struct RowsShape<512, 0> { static constexpr int kWR = 8, kWK = 1, kNK = 1, kStages = 4; };
-template <> struct RowsShape<512, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 1, kStages = 4; };
-template <> struct RowsShape<512, 2> { static constexpr int kWR = 2, kWK = 1, kNK = 1, kStages = 4; };
-template <> struct RowsShape<512, 3> { static constexpr int kWR = 1, kWK = 2, kNK = 1, kStages = 2; };
+template <> struct RowsShape<512, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 1, kStages = 2; };
+template <> struct RowsShape<512, 2> { static constexpr int kWR = 2, kWK = 2, kNK = 1, kStages = 2; };
 
 template <typename E, int D, int kShape, bool kTree>
 l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
@@ -484,6 +496,7 @@ l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     constexpr int kRows = S::kWR * kTile;
     constexpr unsigned kLds = S::kStages * 2 * S::kWK * S::kNK * kTile * AttnRow<E, D>::kBytes;
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+    static_assert((S::kWK - 1) * S::kWR * (D / 2 + 2) * kWaveSize * sizeof(float) <= kLds, "room for what the waves of a group join");
     const dim3 grid((unsigned)(a.workgroups == 0 ? a.n_blocks * a.Hkv : a.workgroups));
     hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree>), grid, dim3(S::kWR * S::kWK * kWaveSize), kLds, stream, a);
     if (a.workgroups > 1) {
@@ -498,8 +511,7 @@ l2kv_status rows_attn_launch(const RowsArgs& a, int shape, hipStream_t stream) {
     switch (shape) {
         case 0: return rows_attn_launch_shape<E, D, 0, kTree>(a, stream);
         case 1: return rows_attn_launch_shape<E, D, 1, kTree>(a, stream);
-        case 2: return rows_attn_launch_shape<E, D, 2, kTree>(a, stream);
-        default: return rows_attn_launch_shape<E, D, 3, kTree>(a, stream);
+        default: return rows_attn_launch_shape<E, D, 2, kTree>(a, stream);
     }
 }
 
