@@ -501,7 +501,10 @@ l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree>), grid, dim3(S::kWR * S::kWK * kWaveSize), kLds, stream, a);
     if (a.workgroups > 1) {
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
-        hipLaunchKernelGGL((rows_join_kernel<E, D, kRows>), dim3(kRows * (D / 4) / kJoinThreads, (unsigned)a.workgroups), dim3(kJoinThreads), 0, stream, a);
+        // (of a few tokens not all rows of a block: 7 nodes take 2.8 us, the 64 rows of a block 5.8)
+        const int64_t rows = a.total_q * a.G < kRows ? a.total_q * a.G : kRows;
+        const dim3 join_grid((unsigned)((rows * (D / 4) + kJoinThreads - 1) / kJoinThreads), (unsigned)a.workgroups);
+        hipLaunchKernelGGL((rows_join_kernel<E, D, kRows>), join_grid, dim3(kJoinThreads), 0, stream, a);
     }
     return launch_status();
 }
