@@ -70,12 +70,11 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
     p.n_blocks = (int32_t)blocks;
-    // Two tiles of keys and the one that an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 18.3 us, 23.0 with
-    // four tiles.
-    p.least_tiles = 3;
+    // Two tiles of keys and what an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 18.3 us, 23.0 with four tiles.
+    p.least_tiles = rows_item_tiles(tree) + 2;
     p.workgroups = 0;
     if (stretches) {
-        const int64_t most = blocks * Hkv * (max_kv / s.keys + 2) / (p.least_tiles - 1);
+        const int64_t most = blocks * Hkv * (max_kv / s.keys + 2) / 2;
         p.workgroups = (int32_t)(most < units ? most : units);
     }
     p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * s.rows * rows_partial_floats(D) * sizeof(float);

@@ -42,8 +42,9 @@ __device__ __forceinline__ RowsSeq uniform(const RowsSeq& q) {
 }
 
 // Lengths of items, in keys.  A block of a prompt sees the rows up to its last token's limit; a block of a tree all cached rows and all
-// nodes, in whole tiles each.  An item counts for one tile more than it has, so that none is empty.
+// nodes, in whole tiles each.  An item counts for some tiles more than it has: what its beginning and its end take, and so that none is empty.
 template <bool kTree, int kTileKeys> struct RowsLength {
+    static constexpr int kExtra = rows_item_tiles(kTree) * kTileKeys;
     static __device__ __forceinline__ int64_t keys(const RowsArgs& a, const RowsSeq& q, int64_t block) {
         if constexpr (kTree) {
             return (((int64_t)q.n_rows + kTileKeys - 1) / kTileKeys + ((int64_t)q.n_q + kTileKeys - 1) / kTileKeys) * kTileKeys;
@@ -55,11 +56,11 @@ template <bool kTree, int kTileKeys> struct RowsLength {
     // of the blocks before `block`, together
     static __device__ __forceinline__ int64_t before(const RowsArgs& a, const RowsSeq& q, int64_t block) {
         if constexpr (kTree) {
-            return block * (kTileKeys + keys(a, q, 0));
+            return block * (kExtra + keys(a, q, 0));
         } else {
             const int64_t step = a.tokens_per_block, more = (int64_t)q.n_rows - q.n_q;
             const int64_t none = more >= 0 ? 0 : (uint32_t)-more / (uint32_t)step;            // blocks that see nothing
-            int64_t sum = block * kTileKeys;
+            int64_t sum = block * kExtra;
             if (block > none) sum += step * (block * (block + 1) - none * (none + 1)) / 2 + more * (block - none);
             if (block == q.blocks && block > none) sum -= block * step - q.n_q;
             return sum;
@@ -222,7 +223,7 @@ void rows_attn_kernel(const RowsArgs a) {
     int64_t end, stretch = 0;                                  // of this workgroup's stretch
     if (a.workgroups == 0) {
         if (!rows_own_item<kTree, kTileKeys>(a, it, lane)) return;
-        end = kTileKeys + L::keys(a, it.q, it.block);
+        end = L::kExtra + L::keys(a, it.q, it.block);
     } else {
         if (threadIdx.x == 0) a.joins[blockIdx.x].parts = 0;   // until an item begins here that ends elsewhere
         if (!rows_stretch_item<kTree, kTileKeys>(a, it, stretch, end, lane)) return;
@@ -230,11 +231,11 @@ void rows_attn_kernel(const RowsArgs a) {
     for (int slot = 0;; slot = 1) {                            // one item after the other
         int row = wr * kTile + lane % kTile, half = lane / kTile;
         asm volatile("" : "+v"(row), "+v"(half));              // what follows from them is not held from item to item: registers
-        const int64_t keys = L::keys(a, it.q, it.block), item_end = it.start + kTileKeys + keys;
+        const int64_t keys = L::keys(a, it.q, it.block), item_end = it.start + L::kExtra + keys;
         const int64_t here_end = (end < item_end ? end : item_end) - it.start;
-        // tile t stands at (t + 1) * kTileKeys of its item
-        const int32_t first_tile = it.at <= kTileKeys ? 0 : (int32_t)((it.at - 1) / kTileKeys);
-        const int32_t end_tile = here_end <= kTileKeys ? 0 : (int32_t)((here_end - 1) / kTileKeys);
+        // tile t stands at kExtra + t * kTileKeys of its item
+        const int32_t first_tile = it.at <= L::kExtra ? 0 : (int32_t)((it.at - L::kExtra + kTileKeys - 1) / kTileKeys);
+        const int32_t end_tile = here_end <= L::kExtra ? 0 : (int32_t)((here_end - L::kExtra + kTileKeys - 1) / kTileKeys);
         const bool whole = it.at == 0 && item_end <= end;
         const int32_t first_in_seq = it.block * a.tokens_per_block;
         const int64_t first_token = it.q.q_first + first_in_seq;
