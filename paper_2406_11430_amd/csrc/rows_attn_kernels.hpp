@@ -149,14 +149,40 @@ __device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& i
     return true;
 }
 
-// The item of a workgroup of its own: blocks are numbered over the sequences without gaps, found by a sum over the offsets, a part of the
-// sequences for each lane (more than 64 in two rounds).  (Workgroups without a block behind those that have one do no harm; between
-// them they did, as the hardware deals workgroups out in turn: a batch whose every other number was empty ran on half of the device.)
+// The item of a workgroup of its own; the last tokens of a sequence see most, so they go first.  Blocks are numbered over the sequences
+// without gaps, found by a sum over the offsets, a part of the sequences for each lane (more than 64 in two rounds).  (Workgroups
+// without a block behind those that have one do no harm; between them they did, as the hardware deals workgroups out in turn: a batch
+// whose every other number was empty ran on half of the device.)
+constexpr int32_t kSummedSequences = kWaveSize * kWaveSize;
 template <bool kTree, int kTileKeys>
 __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, int lane) {
     it.head = (int32_t)(blockIdx.x % (uint32_t)a.Hkv);
-    int32_t block = -1 - (int32_t)(blockIdx.x / (uint32_t)a.Hkv);      // from the end: the last tokens of a sequence see most, they go first
-    int32_t lo = 0, count = a.n_seq;
+    it.start = it.at = 0;
+    const int32_t number = (int32_t)(blockIdx.x / (uint32_t)a.Hkv);
+    int32_t block = 0, lo = 0, count = a.n_seq;
+    if (count > kSummedSequences) {
+        // Very many, where a sum would be longer than the work: sequence s has the numbers from q_off[s] / tokens_per_block + s on, room for
+        // all its blocks, and a search among 64 candidates a round finds the last that begins at or before a number.
+        const int32_t id = a.n_blocks - 1 - number;
+        while (count > 1) {
+            const int32_t step = (count + kWaveSize - 1) / kWaveSize;
+            const int64_t mine = lo + (int64_t)lane * step;
+            bool at_or_before = false;
+            if ((int64_t)lane * step < count) {
+                const int64_t first = clamped_range(a.q_off, mine, a.total_q).first;
+                at_or_before = (int64_t)((uint32_t)first / (uint32_t)a.tokens_per_block) + mine <= id;
+            }
+            const uint64_t found = __ballot(at_or_before);
+            const int32_t last = found == 0 ? 0 : 63 - __builtin_clzll(found);
+            lo += last * step;
+            count = count - last * step < step ? count - last * step : step;
+        }
+        it.seq = __builtin_amdgcn_readfirstlane(lo);
+        it.q = uniform(rows_seq(a, it.seq));
+        block = id - (int32_t)((uint32_t)it.q.q_first / (uint32_t)a.tokens_per_block) - it.seq;
+        it.block = block;
+        return block >= 0 && block < it.q.blocks;
+    }
     for (bool all = true;; all = false) {
         const int32_t step = (count + kWaveSize - 1) / kWaveSize;
         RowsSeq q = {};
@@ -171,7 +197,7 @@ __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, i
             }
         }
         const uint32_t upto = wave_inclusive_sum(mine);
-        if (all) block += __builtin_amdgcn_readlane((int)upto, kWaveSize - 1);
+        if (all) block = __builtin_amdgcn_readlane((int)upto, kWaveSize - 1) - 1 - number;
         const uint64_t behind = __ballot((int32_t)upto > block);
         if (block < 0 || behind == 0) return false;
         const int which = __builtin_ctzll(behind);
@@ -180,7 +206,6 @@ __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, i
             it.seq = lo + which;
             it.q = of_lane(q, which);
             it.block = block;
-            it.start = it.at = 0;
             return block >= 0 && block < it.q.blocks;
         }
         lo += which * step;
