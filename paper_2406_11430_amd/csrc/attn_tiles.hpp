@@ -47,9 +47,12 @@ template <typename E, int D> struct AttnRow {
 
 // 16 bytes per lane from base + offset to LDS, lane after lane from `lds` on, not waited for.  (Written out because the compiler waits for
 // loads of this kind in front of every transposing read, also of the other tile; no register is written, so
-// nothing but the wait below depends on when it is done.)
-__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+// nothing but the wait below depends on when it is done.)  kOnce: what is not read again soon passes the caches by.
+template <bool kOnce> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+    if constexpr (kOnce)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 // This wave's loads to LDS are done, but for the last `tiles` tiles of kLoads each (at most kMost of them stay on their way).
 template <int kLoads, int kMost>
@@ -64,7 +67,7 @@ __device__ __forceinline__ void wait_loads_to_lds(int32_t tiles) {
 }
 
 // Rows [k0, k0 + kRows) of a matrix of `rows` rows to LDS, by kWaves waves; rows behind the end are copies of the last.
-template <typename E, int D, int kRows, int kWaves, bool kIsV>
+template <typename E, int D, int kRows, int kWaves, bool kIsV, bool kOnce>
 __device__ __forceinline__ void stage_rows(const char* base, int64_t k0, int64_t rows, uint32_t lds, int wave, int lane) {
     using R = AttnRow<E, D>;
     constexpr int kRowsPerChunk = 1024 / R::kBytes, kLanesPerRow = R::kPieces;
@@ -80,7 +83,7 @@ __device__ __forceinline__ void stage_rows(const char* base, int64_t k0, int64_t
         const int r = chunk * kRowsPerChunk + lane / kLanesPerRow;
         const int piece = (lane % kLanesPerRow) ^ (kIsV ? R::v_swizzle(r) : R::k_swizzle(r));
         const int src = r < last ? r : last;
-        load_to_lds(from, (uint32_t)(src * R::kBytes + piece * 16), lds + chunk * 1024);
+        load_to_lds<kOnce>(from, (uint32_t)(src * R::kBytes + piece * 16), lds + chunk * 1024);
     }
 }
 

@@ -50,6 +50,7 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     p.shape = kNarrowest;
     while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
     const int64_t longest = max_kv + (tree ? mean : 0);            // keys of an item
+    const double bytes = 2.0 * (double)max_kv * n_seq * Hkv * row_bytes;     // of K and V, at most
     bool stretches = false;
     if (p.shape == 0 && longest >= 2048 && items(0) >= 2 * units) {
     } else if (p.shape < kNarrowest && items(1) >= 2 * units) {
@@ -58,14 +59,17 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
         // Of the narrowest block: the keys of the longest item, with something for two in a compute unit, against those of a stretch, with
         // 8 tiles' time for its beginning and the join.  Stretches of the widest block take 0.6 of the time for the same keys.
         const int64_t n = items(kNarrowest), tile = sizes(kNarrowest).keys;
-        const bool cached = (double)max_kv * n_seq * Hkv * row_bytes * 2 <= 40e6;          // a little more than the L2s hold
-        if (p.shape == 0 && cached) p.shape = kNarrowest;
+        if (p.shape == 0 && bytes <= 40e6) p.shape = kNarrowest;           // a little more than the L2s hold
         const double own = (double)longest * (n > units ? 1.3 : 1.0);
         const double keys = (double)longest - (tree ? 0.0 : 0.5 * (double)(mean < longest ? mean : longest));
         const double even = (double)(8 * tile) + (double)n * keys / (double)units * (p.shape == 0 ? 0.6 : 1.0);
         stretches = n < 2 * units && own > even && n_seq <= 1024;      // the search for a stretch's beginning goes over all sequences
         if (!stretches) p.shape = kNarrowest;
     }
+    // A tree's cached rows are read once (or by a few workgroups at about the same time), and more of them than the memory-side cache holds
+    // are not there when the next call comes: 64 trees over 500 to 4000 rows 126 us, 138 through the caches; 64 over 1000 61 and 67.  16
+    // over 1000 rows, which stay there from call to call, would take 28 us instead of 24.
+    p.once = tree && bytes > 256e6;
     const ShapeSizes s = sizes(p.shape);
     p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
@@ -87,6 +91,7 @@ l2kv_status rows_attn_dispatch(RowsArgs a, const RowsPlan& p, int32_t D, l2kv_dt
     a.n_blocks = p.n_blocks;
     a.workgroups = p.workgroups < 2 ? 0 : p.workgroups;
     a.least_tiles = p.least_tiles;
+    a.once = p.once;
     a.joins = reinterpret_cast<RowsJoin*>(reinterpret_cast<char*>(a.partial) + p.partial_bytes);
 #define L2KV_ROWS(E, D_) return tree ? rows_attn_launch<E, D_, true>(a, p.shape, stream) : rows_attn_launch<E, D_, false>(a, p.shape, stream)
     if (dt == L2KV_F32) {

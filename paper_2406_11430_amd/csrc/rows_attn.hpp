@@ -24,6 +24,7 @@ struct RowsArgs {
     int32_t n_seq, Hkv, G, mask_words;
     int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
     float scale;                                                // softmax scale times log2(e)
+    bool once;                                                  // trees: cached rows pass the caches by
 };
 
 // What an item counts for besides its keys, in tiles of them: of a prompt one for its beginning and its end and one because its
@@ -35,6 +36,7 @@ constexpr int rows_item_tiles(bool tree) { return tree ? 1 : 2; }
 struct RowsPlan {
     int shape;
     int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
+    bool once;
     size_t partial_bytes, bytes;       // of the parts, and of the joins behind them as well
 };
 

@@ -226,7 +226,7 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
 
 // kWR x kWK waves: kWR groups of 32 rows each, the keys of a tile shared among kWK waves of a group.  A tile has kWK * kNK * 32 keys;
 // kStages of them have room in LDS, all but one on their way while that one is worked on.
-template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree>
+template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree, bool kOnce>
 __global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {
     using R = AttnRow<E, D>;
@@ -284,8 +284,8 @@ void rows_attn_kernel(const RowsArgs a) {
             const bool nodes = kTree && tile >= row_tiles;
             const int64_t k0 = (int64_t)(nodes ? tile - row_tiles : tile) * kTileKeys;
             const int64_t rows = nodes ? it.q.n_q : it.q.n_rows;
-            stage_rows<E, D, kTileKeys, kWaves, false>(nodes ? a.Kt + node_base : K, k0, rows, lds_at + where, wave, lane);
-            stage_rows<E, D, kTileKeys, kWaves, true>(nodes ? a.Vt + node_base : V, k0, rows, lds_at + where + kHalf, wave, lane);
+            stage_rows<E, D, kTileKeys, kWaves, false, kOnce>(nodes ? a.Kt + node_base : K, k0, rows, lds_at + where, wave, lane);
+            stage_rows<E, D, kTileKeys, kWaves, true, kOnce>(nodes ? a.Vt + node_base : V, k0, rows, lds_at + where + kHalf, wave, lane);
         };
         // Which of the 32 keys from k0 on the lane's row sees.
         auto seen = [&](bool nodes, int64_t k0) -> uint32_t {
@@ -524,7 +524,11 @@ l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
     static_assert((S::kWK - 1) * S::kWR * (D / 2 + 2) * kWaveSize * sizeof(float) <= kLds, "room for what the waves of a group join");
     const dim3 grid((unsigned)(a.workgroups == 0 ? a.n_blocks * a.Hkv : a.workgroups));
-    hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree>), grid, dim3(S::kWR * S::kWK * kWaveSize), kLds, stream, a);
+    const dim3 block(S::kWR * S::kWK * kWaveSize);
+    if (kTree && a.once)
+        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree, kTree>), grid, block, kLds, stream, a);
+    else
+        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree, false>), grid, block, kLds, stream, a);
     if (a.workgroups > 1) {
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
         // (of a few tokens not all rows of a block: 7 nodes take 2.8 us, the 64 rows of a block 5.8)

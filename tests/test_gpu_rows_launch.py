@@ -182,3 +182,18 @@ def test_stretches_of_the_widest_block(dtype, D):
     assert torch.equal(O, run(Q, K, V, new, rows))
     c = Case(D, new, rows, 16, 4, D, dtype)
     c.verify(c.run())
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("top,G", [(2, 4), (30, 4), (60, 4), (9, 1)])
+def test_trees_over_more_than_the_caches_hold(dtype, D, top, G):
+    """Bounds for which rows of the cache are read past the caches, with workgroups for each item; the same bits as with a bound for which
+    they are not, where the work is cut alike."""
+    nodes = [1 + (5 * s) % top for s in range(64)]
+    lens = [(37 * s) % 300 for s in range(64)]
+    c = Case(top + D, nodes, lens, 8 * G, 8, D, dtype)
+    bound = 256_000_000 // (2 * 64 * 8 * D * (2 if dtype == torch.bfloat16 else 4)) + 1
+    assert bound <= sum(c.room)
+    O = c.run(bound=bound)
+    c.verify(O)
+    assert torch.equal(O, c.run(bound=bound - 2))
