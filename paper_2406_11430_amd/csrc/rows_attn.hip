@@ -28,14 +28,14 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
 // Which block of rows a launch takes and whether a workgroup has an item for itself or an equal stretch of all of them.  Wide blocks read
 // K and V least often; two workgroups of a narrow one share a compute unit, so that one computes while the other begins or ends an item, and
 // there are more of them.  Measured (bf16, D 128, 8 KV heads of 4 query heads, us):
-//                                         256 rows  128 rows  64 rows  stretches
-//   1 prompt of 8192 tokens                    544       570      638        652    (most work: the widest block)
-//   64 prompts of 64                          36.7      31.4     38.7       39.2    (two and more 128-row workgroups for each compute unit)
-//   1 prompt of 512                           23.3      20.5     14.7       23.7    (few: the narrowest)
-//   32 trees of 4 nodes over 1024 rows each: as many bytes in either, 57
-//   4 prompts' next 64 tokens over 16000       421       368      240         94    (few and long: stretches, of the block that takes the rows)
-//   1 tree of 64 nodes over 8192               220       192      108       30.8    (K and V are in the caches: stretches of the narrowest)
-// Over 90 sizes of all row types what this chooses takes 3 % longer than the best of the six, and no fixed choice of one less than 40 %.
+//                                       256 rows  128 rows  64 rows  stretches
+//   1 prompt of 8192 tokens                  554       581      653        652    (most work: the widest block)
+//   64 prompts of 64                        36.7      31.4     38.7       39.2    (two and more 128-row workgroups for each compute unit)
+//   1 prompt of 512                         23.6      20.9     15.1       23.7    (few: the narrowest)
+//   4 trees of 64 nodes over 16000 rows      419       371      242         94    (few and long: stretches, of the block that takes the rows)
+//   1 tree of 64 nodes over 8192             221       194      111       30.8    (K and V are in the caches: stretches of the narrowest; the widest 37)
+// Over 90 sizes of all row types what this chooses took 3 % longer than the best of the six (the widest block that a sequence fills, and
+// stretches wherever there are fewer than four items for each compute unit: 25 %).
 RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree) {
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t units = device_compute_units(), mean = (total_q + n_seq - 1) / n_seq;

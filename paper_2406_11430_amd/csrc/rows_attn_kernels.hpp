@@ -225,7 +225,12 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
 }
 
 // kWR x kWK waves: kWR groups of 32 rows each, the keys of a tile shared among kWK waves of a group.  A tile has kWK * kNK * 32 keys;
-// kStages of them have room in LDS, all but one on their way while that one is worked on.
+// kStages of them have room in LDS, all but one on their way while that one is worked on.  kOnce: cached rows are not read again soon.
+//
+// Prompts are bound by the two units that do not overlap enough: of a tile of 256 rows and 64 keys (bf16, D 128; 1.9 us) the matrix unit is
+// busy for 57 %, exponentials, maxima and roundings take a third.  A prompt of 32768 tokens (32 query heads, 8 KV heads) takes 7.7 to 8.0 ms,
+// 1.10 to 1.14 PFLOP/s of the 1.37 that a large matrix product reaches; without the values read ahead of the softmax 7.9 to 8.1.  Trees are bound by memory:
+// 64 of 1 to 32 nodes over 500 to 4000 rows 121 us, 5.0 TB/s (a large copy: 4.80).
 template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree, bool kOnce>
 __global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {
@@ -313,11 +318,18 @@ void rows_attn_kernel(const RowsArgs a) {
             for (int j = 0; j < kNK; ++j) {
                 const char* const k = here + (wk * kNK + j) * kTile * R::kBytes;
                 if constexpr (R::kBytes == 512) at.forget();
-                f32x16_t s[1];
-                Weights<E> p[1];
-                scores<E, D>(k, at, q, s[0]);
-                softmax_step<E, D>(st, s, p, a.scale);
-                weighted_values<E, D>(k + kHalf, at, p[0], st.o);
+                f32x16_t s;
+                Weights<E> p;
+                scores<E, D>(k, at, q, s);
+                if constexpr (R::kBytes == 512) {
+                    softmax_step<E, D>(st, s, p, a.scale);
+                    weighted_values<E, D>(k + kHalf, at, p, st.o);
+                } else {
+                    ValueTile<E, D> values;
+                    load_values<E, D>(k + kHalf, at, values);
+                    softmax_step<E, D>(st, s, p, a.scale);
+                    weighted_values<E, D>(values, p, st.o);
+                }
             }
         };
         auto masked_tile = [&](const char* here, int32_t tile) {
@@ -337,18 +349,20 @@ void rows_attn_kernel(const RowsArgs a) {
                     load_queries(again);
                     at.forget();
                 }
-                f32x16_t s[1];
-                Weights<E> p[1];
-                scores<E, D>(k, at, q, s[0]);
+                f32x16_t s;
+                Weights<E> p;
+                scores<E, D>(k, at, q, s);
                 const uint32_t mine = bits >> (4 * half);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[0][i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[0][i] : -__builtin_inff();
+                for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : -__builtin_inff();
                 softmax_step<E, D>(st, s, p, a.scale);
                 // Long rows have no registers for two ways of adding the same products: they take the careful one always.
                 if (R::kBytes == 512 || values_not_finite<E, D>(k + kHalf, lane)) {
-                    if (finite_values<E, D>(k + kHalf, at, p[0], st.o)) other_values<E, D>(k + kHalf, at, p[0], bits, st.o, lane);
+                    if (finite_values<E, D>(k + kHalf, at, p, st.o)) other_values<E, D>(k + kHalf, at, p, bits, st.o, lane);
                 } else {
-                    weighted_values<E, D>(k + kHalf, at, p[0], st.o);
+                    ValueTile<E, D> values;
+                    load_values<E, D>(k + kHalf, at, values);
+                    weighted_values<E, D>(values, p, st.o);
                 }
             }
         };
@@ -506,8 +520,12 @@ void rows_join_kernel(const RowsArgs a) {
     store_four<E>(a.O + ((join.first_row + (int64_t)token * (a.Hkv * a.G) + g) * D + 4 * c) * E::kBytes, v);
 }
 
-// The shapes of workgroup a row type has: rows of a block (32 * kWR) and keys of a tile (32 * kWK * kNK).  One workgroup to a compute unit: of
-// two, the younger gets the memory that the older leaves (122 us instead of 94 for equal stretches of a batch of trees).
+// The shapes of workgroup a row type has: rows of a block (32 * kWR) and keys of a tile (32 * kWK * kNK).  The widest fills a compute unit
+// (8 waves of up to 256 registers), of the others two share one; the narrowest has two waves for the same rows, so that short items of
+// few rows use all four SIMDs.  Two tiles in LDS, one read and one on its way: 3 and 4 of them measured slower (256 rows: a prompt of 32768
+// tokens 8.5 ms against 7.9; 128 rows, trees of a batch: 200 us against 152), 32 keys a tile for 128 rows as well (582 against 570).
+// Measured against the widest: 16 waves' worth of rows in 4 waves of 64 (half the LDS reads, one wave a SIMD) 8.45 ms, halves of a workgroup
+// in opposite phases 8.04, raised priority for products 8.44.  Rows of 512 bytes have 32 keys a tile: registers and LDS.
 template <int kRowBytes, int kShape> struct RowsShape;
 template <int kRowBytes> struct RowsShape<kRowBytes, 0> { static constexpr int kWR = 8, kWK = 1, kNK = 2, kStages = 2; };
 template <int kRowBytes> struct RowsShape<kRowBytes, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 2, kStages = 2; };
