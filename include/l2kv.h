@@ -431,6 +431,7 @@ size_t l2kv_decode_ragged_workspace_bytes(int32_t n_seq, int32_t Hq, int64_t max
  * Q, K and V of a token are heads of D contiguous elements, a token's heads side by
  * side; the *_stride arguments are the ELEMENTS between two tokens (>= heads*D,
  * a multiple of 16 bytes), so the three may be parts of one projection's output.
+ * What a call writes must not overlap what it reads.
  * ------------------------------------------------------------------------ */
 
 /* Which two elements of a head are turned together, of the first rot_dim = R:
@@ -512,7 +513,8 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  *             decomposition; rows beyond it are still attended to)
  *   O   out : [total_q][Hq][D], dense, of type dt
  *   workspace: l2kv_prompt_attn_workspace_bytes(...) bytes, 16-aligned; contents
- *             irrelevant before and after.  May be NULL where that is 0.
+ *             irrelevant before and after, one per call that may run at the same
+ *             time.  May be NULL where that is 0.
  * Arithmetic: fp32 scores, softmax and sums; for bf16, products on the matrix unit
  * with the softmax weights rounded to bf16 (their sum is that of the rounded ones) and O
  * rounded once.
