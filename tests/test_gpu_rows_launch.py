@@ -197,3 +197,42 @@ def test_trees_over_more_than_the_caches_hold(dtype, D, top, G):
     O = c.run(bound=bound)
     c.verify(O)
     assert torch.equal(O, c.run(bound=bound - 2))
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("new,have", [([17000], 0), ([90] * 80, 0), ([70] * 90, 11), ([45, 80], 4000), ([5], 9000), ([100, 60], 40000)])
+def test_hidden_rows_have_no_effect_however_the_work_is_cut(dtype, D, new, have):
+    """The last row of every sequence, which only its last token sees, holds anything; all other tokens keep their bits."""
+    rows = [n + have for n in new]
+    Q, K, V = make(len(new), new, rows, 8, 2, D, dtype)
+    clean = run(Q, K, V, new, rows)
+    last = torch.tensor(starts(rows)[1:], device=DEV) - 1
+    K[:, last], V[:, last[0::2]], V[:, last[1::2]] = float("nan"), float("inf"), float("nan")
+    O = run(Q, K, V, new, rows)
+    own = torch.tensor(starts(new)[1:], device=DEV) - 1
+    others = torch.ones(sum(new), dtype=torch.bool, device=DEV)
+    others[own] = False
+    assert torch.equal(O[others], clean[others]) and not torch.isfinite(O[own]).any()
+
+
+def test_another_stream():
+    """Every call on a stream that is not the current one, behind work of that stream which its inputs come from."""
+    from test_binding_calls_rows import CALLS
+    side = torch.cuda.Stream()
+    for name, (build, entry) in CALLS.items():
+        a, outs = build()
+        entry(**a)
+        want = [a[o].clone() for o in outs]
+        b, _ = build()
+        inputs = {k: v for k, v in b.items() if isinstance(v, torch.Tensor) and k not in outs}
+        late = {k: torch.zeros_like(v) for k, v in inputs.items()}
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000)
+            for k, v in inputs.items():
+                late[k].copy_(v)
+        b.update(late)
+        entry(**b, stream=side)
+        side.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(b[o], w), (name, o)
