@@ -240,6 +240,26 @@ template <typename E, int D> __device__ __forceinline__ bool values_not_finite(c
     return __ballot(bad) != 0;
 }
 
+// The same of values in registers: an exponent of all ones and one more is the sign bit.  (bf16 rows of 256 bytes have none left for it.)
+template <typename E, int D> __device__ __forceinline__ bool values_not_finite(const ValueTile<E, D>& x) {
+    uint32_t any = 0;
+    if constexpr (E::kBytes == 2) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int d = 0; d < D / kTile; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) any |= (x.v[t][d][i] & 0x7f807f80u) + 0x00800080u;
+        return __ballot((any & 0x80008000u) != 0) != 0;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < D / kTile; ++d) any |= (__builtin_bit_cast(uint32_t, x.v[i][d]) & 0x7f800000u) + 0x00800000u;
+        return __ballot((any & 0x80000000u) != 0) != 0;
+    }
+}
+
 // For a tile with hidden keys, where 0 times an infinity is not zero: the operand of 16 keys (bf16: t = 0, 1) or two (fp32: t = 0..15) with
 // the finite values of the keys to keep, or the others; and the weights that go with it.
 template <typename E, int D>

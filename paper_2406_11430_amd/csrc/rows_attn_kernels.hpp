@@ -356,12 +356,17 @@ void rows_attn_kernel(const RowsArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : -__builtin_inff();
                 softmax_step<E, D>(st, s, p, a.scale);
+                ValueTile<E, D> values;
+                constexpr bool kLook = R::kBytes == 128 || (R::kBytes == 256 && E::kBytes == 4);
+                if constexpr (kLook) load_values<E, D>(k + kHalf, at, values);
                 // Long rows have no registers for two ways of adding the same products: they take the careful one always.
-                if (R::kBytes == 512 || values_not_finite<E, D>(k + kHalf, lane)) {
+                bool careful = R::kBytes == 512;
+                if constexpr (kLook) careful = values_not_finite<E, D>(values);
+                else if constexpr (R::kBytes < 512) careful = values_not_finite<E, D>(k + kHalf, lane);
+                if (careful) {
                     if (finite_values<E, D>(k + kHalf, at, p, st.o)) other_values<E, D>(k + kHalf, at, p, bits, st.o, lane);
                 } else {
-                    ValueTile<E, D> values;
-                    load_values<E, D>(k + kHalf, at, values);
+                    if constexpr (!kLook) load_values<E, D>(k + kHalf, at, values);
                     weighted_values<E, D>(values, p, st.o);
                 }
             }
