@@ -7,10 +7,12 @@
 // is that of the row as stored, and four fp64 operations an element hide behind the memory (two bytes in, two out).
 //
 // A workgroup takes up to four tokens: their angles once into LDS, for all heads; then rows of Q, K and V, 16 elements a lane in two pieces
-// of 8 that belong together (half layout: pieces u and u + rot/16, interleaved: 2u and 2u + 1; what is not rotated is copied).
+// of 8, neighbouring lanes side by side: of what is turned pieces u and u + rot/16 (the two halves belong together; interleaved pairs
+// lie in one piece), of the rest, which is copied, and of V the same behind it.  (Two pieces side by side a lane, where nothing belongs
+// together: 3.4 TB/s instead of 4.2 for fp32 rows of 128 of which 16 elements are turned.)
 //
-// Bound by memory: 36768 bf16 tokens of 32 + 8 + 8 heads of 128 take 179 us, 5.06 TB/s in and out (a large copy: 4.80), 183 without the rows
-// that are on their way ahead; 64 fp32 tokens of 8 + 4 + 4 heads of 64 take 4.4 us, a launch and three loads that wait for one another.
+// Bound by memory: 36768 bf16 tokens of 32 + 8 + 8 heads of 128 take 173 to 179 us, 5.05 to 5.25 TB/s in and out (a large copy: 4.80), 183 without the
+// rows that are on their way ahead; 64 fp32 tokens of 8 + 4 + 4 heads of 64 take 4.4 us, a launch and three loads that wait for one another.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 #include "row_norm.hpp"
@@ -96,9 +98,9 @@ void rotary_kernel(const RotaryArgs a) {
         at.t = at.row / heads, at.h = at.row - at.t * heads;
         at.is_q = at.h < a.Hq, at.is_k = !at.is_q && at.h < a.Hq + a.Hkv;
         at.kv = at.is_q ? 0 : (at.is_k ? at.h - a.Hq : at.h - a.Hq - a.Hkv);
-        at.turn = (at.is_q || at.is_k) && u < a.rot / 16;
-        const bool apart = at.turn ? !kInterleaved : !(at.is_q || at.is_k);
-        at.p0 = apart ? u : 2 * u, at.p1 = apart ? u + (at.turn ? a.rot / 16 : kLanes) : 2 * u + 1;
+        const int turned = at.is_q || at.is_k ? a.rot / 16 : 0;                            // lanes, of two pieces each
+        at.turn = u < turned;
+        at.p0 = at.turn ? u : u + turned, at.p1 = at.turn ? u + turned : u + kLanes;
         return at;
     };
     Piece<E> next0, next1;
@@ -141,7 +143,8 @@ void rotary_kernel(const RotaryArgs a) {
             float r0[8], r1[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double c = angle[t][8 * u + i][0], s = angle[t][8 * u + i][1];
+                const int pair = !kInterleaved ? 8 * u + i : (i < 4 ? 4 * p0 + i : 4 * p1 + i - 4);
+                const double c = angle[t][pair][0], s = angle[t][pair][1];
                 double x1, x2;
                 if constexpr (kInterleaved) {
                     x1 = piece_element<E>(i < 4 ? x : y, 2 * i % 8);
