@@ -482,7 +482,7 @@ l2kv_status l2kv_rotary_freqs(int32_t rot_dim, double base, l2kv_rotary_scaling 
  *                   plane (prompts, packed as they are; nodes of drafted trees).
  * Errors: NULL (also for one of the three arrays without the others), SHAPE
  * (rot_dim not a multiple of 16 or above D, layout, total_slots < total_tokens
- * without offsets, amplitude not finite, more than 2^24-1 workgroups of four tokens, ...), DTYPE, ALIGN, LAUNCH.
+ * without offsets, amplitude not finite, more than 2^24-1 workgroups of four tokens or more, ...), DTYPE, ALIGN, LAUNCH.
  */
 l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
                                int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,

@@ -6,7 +6,7 @@
 // before sine and cosine.  The turn itself is done in fp64 as well and rounded once: the key's norm, which decides whether it is kept,
 // is that of the row as stored, and four fp64 operations an element hide behind the memory (two bytes in, two out).
 //
-// A workgroup takes up to four tokens: their angles once into LDS, for all heads; then rows of Q, K and V, 16 elements a lane in two pieces
+// A workgroup takes some tokens: their angles once into LDS, for all heads; then rows of Q, K and V, 16 elements a lane in two pieces
 // of 8, neighbouring lanes side by side: of what is turned pieces u and u + rot/16 (the two halves belong together; interleaved pairs
 // lie in one piece), of the rest, which is copied, and of V the same behind it.  (Two pieces side by side a lane, where nothing belongs
 // together: 3.4 TB/s instead of 4.2 for fp32 rows of 128 of which 16 elements are turned.)
@@ -21,7 +21,11 @@ namespace l2kv {
 namespace {
 
 constexpr int kRotThreads = 256, kRotWaves = kRotThreads / kWaveSize;
-constexpr int kRotTokens = 4;                 // most tokens of a workgroup
+// Most tokens of a workgroup, and most rows from more than 4 of them: heads are few where 4 tokens leave lanes idle (32768 fp32 tokens of 1 + 1 + 1
+// heads of 64 21.4 us, 17.0 with 16 of them; 8 + 8 + 8 heads 91 and, with 8, 95).  Rows of 512 bytes fill the lanes, and the LDS of more
+// angles costs workgroups (bf16, D 256, 4 + 1 + 1 heads: 41 us, 51 with 16).
+constexpr int rot_tokens(int row_bytes) { return row_bytes <= 256 ? 16 : 4; }
+constexpr int kRotRows = 96;
 constexpr int64_t kNoSlot = -1, kNoSequence = -2;
 
 // Slot of token t: its place among its sequence's tokens behind the occupied slots; kNoSlot where they are full, kNoSequence for a token
@@ -71,8 +75,9 @@ __global__ __launch_bounds__(kRotThreads)
 void rotary_kernel(const RotaryArgs a) {
     constexpr int kLanes = D / 16, kRows = kWaveSize / kLanes;     // lanes of a row, rows of a wave
     constexpr int kRowBytes = D * E::kBytes, kPiece = 8 * E::kBytes;
-    __shared__ __attribute__((aligned(16))) double angle[kRotTokens][D / 2][2];
-    __shared__ int64_t slot_of[kRotTokens];
+    constexpr int kTokens = rot_tokens(kRowBytes);
+    __shared__ __attribute__((aligned(16))) double angle[kTokens][D / 2][2];
+    __shared__ int64_t slot_of[kTokens];
     __shared__ __attribute__((aligned(16))) char key_rows[kRotWaves][kRows * kRowBytes];
 
     const int lane = threadIdx.x % kWaveSize;
@@ -211,8 +216,11 @@ void rotary_kernel(const RotaryArgs a) {
 }  // namespace
 
 l2kv_status rotary_dispatch(RotaryArgs a, l2kv_dtype dt, int32_t D, bool interleaved, hipStream_t stream) {
-    // few tokens: one to a workgroup, so that they are spread over the chip
-    a.tokens_per_block = a.total_tokens >= 4 * (int64_t)device_compute_units() ? kRotTokens : 1;
+    // Enough tokens for some rows a lane group, but workgroups for the whole chip: few tokens one to each.
+    const int heads = a.Hq + 2 * a.Hkv;
+    a.tokens_per_block = rot_tokens(D * (dt == L2KV_F32 ? 4 : 2));
+    while (a.tokens_per_block > 4 && a.tokens_per_block * heads > kRotRows) a.tokens_per_block /= 2;
+    while (a.tokens_per_block > 1 && a.total_tokens < a.tokens_per_block * (int64_t)device_compute_units()) a.tokens_per_block /= 2;
     const int64_t blocks = (a.total_tokens + a.tokens_per_block - 1) / a.tokens_per_block;
     if (blocks > (1 << 24) - 1) return L2KV_ERR_SHAPE;             // a launch has fewer than 2^32 lanes
     const dim3 grid((unsigned)blocks);
