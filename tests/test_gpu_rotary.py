@@ -155,3 +155,35 @@ def test_many_tokens_and_a_graph():
         torch.cuda.synchronize()
         close(Qr, turned(Q, positions, freqs, 1, 1.0))
         close(c[0].transpose(0, 1), turned(K, positions, freqs, 1, 1.0))
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("Hq,Hkv,total", [(1, 1, 4099), (4, 1, 4111), (2, 2, 4096), (6, 3, 2051), (1, 1, 1029)])
+@pytest.mark.parametrize("layout", [0, 1])
+def test_many_tokens_of_few_heads(dtype, D, Hq, Hkv, total, layout):
+    """Workgroups of 16, 8 and 4 tokens, the last one not full; into rows as they are, and into the slots of many sequences."""
+    Q, K, V = inputs(total, total, Hq, Hkv, D, dtype)
+    positions = (torch.arange(total, dtype=torch.int32) % 1000 * 77).to(DEV)
+    rot = 32
+    freqs = l2kv.l2kv_rotary_freqs(rot, 10000.0).to(DEV)
+    Qr = torch.empty((total, Hq, D), dtype=dtype, device=DEV)
+    Kc, Vc, norms, pos = cache(Hkv, total, D, dtype)
+    l2kv.l2kv_rotary_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms, pos, layout=layout)
+    close(Qr, turned(Q, positions, freqs, layout, 1.0))
+    close(Kc.transpose(0, 1), turned(K, positions, freqs, layout, 1.0))
+    assert torch.equal(Vc, V.transpose(0, 1)) and torch.equal(pos, positions.expand(Hkv, total))
+    again = torch.empty_like(norms)
+    l2kv.l2kv_norms(Kc, again)
+    assert torch.equal(norms, again)
+    new = [7] * (total // 7) + [total % 7]
+    slots = [n + 3 for n in new]
+    Ks, Vs, norms_s, pos_s = cache(Hkv, sum(slots), D, dtype)
+    lens_in = torch.full((len(new),), 2, dtype=torch.int32, device=DEV)
+    lens_out = torch.empty_like(lens_in)
+    l2kv.l2kv_rotary_append(Q, K, V, positions, freqs, Qr, Ks, Vs, norms_s, pos_s, offsets(new), offsets(slots), lens_in, lens_out, layout=layout)
+    assert lens_out.tolist() == [n + 2 for n in new]
+    to = torch.cat([torch.arange(n) + 2 + c for n, c in zip(new, starts(slots))]).to(DEV)
+    assert torch.equal(Ks[:, to], Kc) and torch.equal(Vs[:, to], Vc) and torch.equal(norms_s[:, to], norms) and torch.equal(pos_s[:, to], pos)
+    free = torch.ones(sum(slots), dtype=torch.bool, device=DEV)
+    free[to] = False
+    assert (Ks[:, free] == 9).all() and (Vs[:, free] == 9).all() and (norms_s[:, free] == 9).all() and (pos_s[:, free] == 9).all()
