@@ -510,8 +510,12 @@ void rows_join_kernel(const RowsArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (p + u < parts && ml[u].x != -__builtin_inff()) {       // a part with a key that the row sees
-                const float top = fmaxf(m, ml[u].x), old = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml[u].x - top);
+            if (p + u < parts) {
+                // A maximum of minus infinity says that no score of the part is above it, not that the row sees no key there: NaN of such a
+                // part (scores that are all NaN, values that are not finite under a weight of zero) is in its sums, and goes on.
+                const float top = fmaxf(m, ml[u].x);
+                const float old = top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - top);
+                const float f = top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - top);
                 m = top;
                 l = l * old + ml[u].y * f;
 #pragma unroll
