@@ -508,7 +508,9 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  *             total_rows: rows that can be read from the start of every head.
  *             Planes [Hkv][total_rows][D]: kv_head_stride = total_rows * D.
  *             Caches [B][Hkv][T][D]: kv_head_stride = T*D, kv_offsets[b] = b*Hkv*T,
- *             kv_lens[b] <= T, total_rows = ((B-1)*Hkv + 1) * T.
+ *             kv_lens[b] <= T or NULL (all T), total_rows = ((B-1)*Hkv + 1) * T.
+ *             With several KV heads a sequence has at most kv_head_stride / D rows,
+ *             whatever offsets and lengths say: its rows of the next head follow.
  *   max_kv  : an upper bound of all n_kv (sizes the workspace and the
  *             decomposition; rows beyond it are still attended to)
  *   O   out : [total_q][Hq][D], dense, of type dt
@@ -542,7 +544,7 @@ size_t l2kv_prompt_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, 
  *   Q      in : [total_nodes] x Hq heads, node_offsets DEVICE int64 [n_seq+1]
  *   Kc, Vc in : one layer's planes, kv_head_stride, total_slots, slot_offsets as
  *               kv_head_stride, total_rows, kv_offsets of l2kv_prompt_attn
- *   lens   in : DEVICE int32 [n_seq], at most as many as the sequence has slots; 0 allowed
+ *   lens   in : DEVICE int32 [n_seq], at most as many as the sequence has slots (forced to that); 0 allowed
  *   max_len   : an upper bound of all lens (as max_kv of l2kv_prompt_attn; 0 allowed)
  *   Kt, Vt in : [Hkv][total_nodes][D]
  *   mask   in : DEVICE uint32 [total_nodes][mask_words], mask_words >= 1; nodes of a

@@ -601,7 +601,8 @@ def l2kv_prompt_attn(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, q_offset
                      kv_offsets: torch.Tensor, kv_lens: Optional[torch.Tensor], max_kv: int, O: torch.Tensor,
                      workspace: Optional[torch.Tensor], scale: float = 0.0, stream=None) -> None:
     """Q ``[total_q, Hq, D]`` (tokens any distance apart), K/V ``[Hkv, rows, D]`` or ``[B, Hkv, T, D]`` -> O ``[total_q, Hq, D]``
-    of Q's type.  Offsets are device int64 ``[n_seq + 1]`` (in rows; of a ``[B, Hkv, T, D]`` cache b*Hkv*T), kv_lens int32 or None."""
+    of Q's type.  Offsets are device int64 ``[n_seq + 1]`` (in rows; of a ``[B, Hkv, T, D]`` cache b*Hkv*T), kv_lens int32 or None
+    (all rows up to the next offset; of a ``[B, Hkv, T, D]`` cache all T)."""
     st = (_calls or calls()).prompt_attn(Q, K, V, q_offsets, kv_offsets, kv_lens, max_kv, O, workspace, scale, stream, _stream)
     if st is not None:
         return _check("l2kv_prompt_attn", st)

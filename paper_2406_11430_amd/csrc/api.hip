@@ -537,6 +537,7 @@ static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, i
     if (a.total_rows <= 0 || a.total_rows > kMaxTokens || max_kv > a.total_rows || (!tree && max_kv == 0)) return L2KV_ERR_SHAPE;
     // a head may start inside the rows of another ([B][Hkv][T][D] caches), but not at the same place
     if (a.kv_head_stride < (a.Hkv > 1 ? D : 0) || a.kv_head_stride > (int64_t{1} << 58) / a.Hkv) return L2KV_ERR_SHAPE;
+    a.most_rows = a.Hkv > 1 ? a.kv_head_stride / D : a.total_rows;
     l2kv_status st = check_token_stride(a.q_stride, a.total_q, Hq, D, dt);
     if (st == L2KV_ERR_SHAPE) return st;
     a.G = Hq / a.Hkv;

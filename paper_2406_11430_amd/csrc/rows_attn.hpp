@@ -21,6 +21,7 @@ struct RowsArgs {
     const int32_t* kv_lens;
     const uint32_t* mask;
     int64_t total_q, total_rows, kv_head_stride, q_stride;      // strides in elements
+    int64_t most_rows;                                          // of a sequence: where the next head begins
     int32_t n_seq, Hkv, G, mask_words;
     int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
     float scale;                                                // softmax scale times log2(e)

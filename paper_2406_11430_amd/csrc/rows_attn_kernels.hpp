@@ -26,7 +26,7 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
 
 __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int32_t s) {
     const Range q = clamped_range(a.q_off, s, a.total_q), kv = clamped_range(a.kv_off, s, a.total_rows);
-    int64_t rows = kv.count;
+    int64_t rows = kv.count < a.most_rows ? kv.count : a.most_rows;
     if (a.kv_lens != nullptr) {
         const int64_t len = a.kv_lens[s];
         rows = len < 0 ? 0 : (len < rows ? len : rows);
