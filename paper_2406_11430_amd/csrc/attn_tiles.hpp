@@ -48,12 +48,18 @@ template <typename E, int D> struct AttnRow {
 
 // 16 bytes per lane from base + offset to LDS, lane after lane from `lds` on, not waited for.  (Written out because the compiler waits for
 // loads of this kind in front of every transposing read, also of the other tile; no register is written, so
-// nothing but the wait below depends on when it is done.)  kOnce: what is not read again soon passes the caches by.
+// nothing but the wait below depends on when it is done.)  m0, which says where in LDS, has its old content again behind it: it is reserved, so
+// that the compiler cannot be told that it changes.  The pause makes five wait states, which a vector load wants behind a vector
+// instruction that wrote its scalar address (a reload of a spilled one, say) and which the compiler does not see to in here.
+// kOnce: what is not read again soon passes the caches by.
 template <bool kOnce> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+    uint32_t m0;
     if constexpr (kOnce)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %2, %3 nt\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "s"(lds), "v"(offset), "s"(base) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 // This wave's loads to LDS are done, but for the last `tiles` tiles of kLoads each (at most kMost of them stay on their way).
 template <int kLoads, int kMost>
