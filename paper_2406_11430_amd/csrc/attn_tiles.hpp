@@ -26,10 +26,14 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_char_t;
 
 constexpr int kTile = 32;                    // query rows and keys of one matrix instruction
-// Scores may rise this far (in powers of two) above the maximum that weights are relative to before it is moved: weights stay
-// below 2^16, in fp32 sums and bf16 weights without any loss (a sum of 2^31 of them below 2^47; what rounds to zero beside a largest weight of
-// 1 or more is below 2^-126 of it), and most tiles leave the accumulators alone (8 instead of 16: 1.3 % longer).
-constexpr float kRiseAllowed = 16.0f;
+// Weights are relative to a reference that lies this far (in powers of two) above a row's largest score at the time, and that is moved when a
+// score passes it: they are at most 1, as are the factors of a move, so sums of weights times values leave the range of fp32 only where those of a
+// plain softmax do, and most tiles leave the accumulators alone.  bf16: 16, so that a row's largest weight is between 2^-16 and 1 (8 instead of
+// 16: 1.3 % longer); weights are rounded relative to themselves, wherever they lie, the exponent's argument, of up to 32 near the top, is off by 2^-20 at
+// most beside their 2^-8, and what falls below 2^-126 is below 2^-110 of the largest.  fp32, where the argument's bits are
+// the weight's: 0, the largest score itself; products take so long there that moving the accumulators costs little (three prompts of 511 to
+// 1533 tokens, 4 heads of 64: 35.9 -> 36.7 us).
+template <typename E> constexpr float kHeadroom = E::kBytes == 2 ? 16.0f : 0.0f;
 
 template <typename E, int D> struct AttnRow {
     static constexpr int kBytes = D * E::kBytes;                     // 128, 256 or 512
@@ -362,7 +366,7 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 // Running softmax of a wave's 32 query rows.
 template <typename E, int D> struct RowState {
     f32x16_t o[D / kTile];
-    float m;               // what weights are relative to, in powers of two; the same in both halves
+    float m;               // what weights are relative to, in powers of two (see kHeadroom); the same in both halves
     float l;               // sum of the weights of this lane's keys
     __device__ __forceinline__ void clear() {
         m = -__builtin_inff();
@@ -372,7 +376,7 @@ template <typename E, int D> struct RowState {
     }
 };
 
-// Scores of a tile of keys (hidden ones -inf) to weights, moving the maximum where scores rise too far above it.  scale: softmax scale
+// Scores of a tile of keys (hidden ones -inf) to weights, moving the reference where a score passes it.  scale: softmax scale
 // times log2(e).  bf16 weights are rounded for the matrix unit, and the sum is taken over the ROUNDED ones, so the weights of a row sum
 // to one exactly as they are applied: rounding one key that outweighs the rest has no effect at all.
 template <typename E, int D>
@@ -381,9 +385,9 @@ __device__ __forceinline__ void softmax_step(RowState<E, D>& st, const f32x16_t&
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top *= scale;
-    if (__ballot(top > st.m + kRiseAllowed) != 0) {
+    if (__ballot(top > st.m) != 0) {
         // each row by its own scores: what another row of the wave sees does not change its bits
-        const float both = max_of_halves(top), m = both > st.m + kRiseAllowed ? both : st.m;
+        const float both = max_of_halves(top), m = both > st.m ? both + kHeadroom<E> : st.m;
         const float f = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
         st.m = m;
         st.l *= f;
