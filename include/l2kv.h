@@ -518,6 +518,10 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  *   workspace: l2kv_prompt_attn_workspace_bytes(...) bytes, 16-aligned; contents
  *             irrelevant before and after, one per call that may run at the same
  *             time.  May be NULL where that is 0.
+ *             The size does NOT grow with the arguments: few tokens over many rows need
+ *             room for parts, many of them none.  A buffer for calls of several sizes
+ *             has the largest of theirs, or, for any sizes of one D,
+ *             compute units (l2kv_device_info) * (2048 * (D + 4) + 24) bytes.
  * Arithmetic: fp32 scores, softmax and sums; for bf16, products on the matrix unit
  * with the softmax weights rounded to bf16 (their sum is that of the rounded ones) and O
  * rounded once.
