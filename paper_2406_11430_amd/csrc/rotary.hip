@@ -70,18 +70,6 @@ template <typename E> __device__ __forceinline__ Piece<E> make_piece(const float
     return p;
 }
 
-// A turned element for make_piece, rounded to nearest from the fp64 result on.  bf16 goes by way of fp32, which on the way to a middle between two
-// bf16 numbers would lose on which side of it the result lies: of the lower 32 of the 52 bits only whether one is set is kept, as the last of the
-// upper 20, which fp32 has room for as they are (but below 2^-126, where it has fewer).
-template <typename E> __device__ __forceinline__ float turned_element(double x) {
-    if constexpr (E::kBytes == 2) {
-        const uint64_t bits = __builtin_bit_cast(uint64_t, x);
-        const uint32_t lower = (uint32_t)bits;
-        x = __builtin_bit_cast(double, (bits >> 32 | (lower < 1u ? lower : 1u)) << 32);
-    }
-    return (float)x;
-}
-
 template <typename E, int D, bool kInterleaved>
 __global__ __launch_bounds__(kRotThreads)
 void rotary_kernel(const RotaryArgs a) {
@@ -170,7 +158,7 @@ void rotary_kernel(const RotaryArgs a) {
                     x1 = piece_element<E>(x, i);
                     x2 = piece_element<E>(y, i);
                 }
-                const float a1 = turned_element<E>(x1 * c - x2 * s), a2 = turned_element<E>(x2 * c + x1 * s);
+                const float a1 = (float)(x1 * c - x2 * s), a2 = (float)(x2 * c + x1 * s);
                 if constexpr (kInterleaved) {
                     (i < 4 ? r0 : r1)[2 * i % 8] = a1;
                     (i < 4 ? r0 : r1)[2 * i % 8 + 1] = a2;
