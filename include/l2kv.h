@@ -464,7 +464,8 @@ l2kv_status l2kv_rotary_freqs(int32_t rot_dim, double base, l2kv_rotary_scaling 
  * turned by theta = p * freqs[i]:
  *     x1' = amplitude * (x1 cos theta - x2 sin theta)
  *     x2' = amplitude * (x2 cos theta + x1 sin theta)
- * in fp64, rounded once; elements from rot_dim on, and V, are copied.
+ * in fp64, rounded to fp32 and for bf16 from there (as a conversion by way of float
+ * does); elements from rot_dim on, and V, are copied.
  *   Q, K, V    in : [total_tokens] x Hq, Hkv, Hkv heads; Q may be NULL together
  *                   with Qr (keys and values only; Hq and q_stride are not read)
  *   positions  in : DEVICE int32 [total_tokens], of either sign

@@ -3,8 +3,10 @@
 //
 // Pair i of a token at position p is turned by the angle p * freq[i]: (x1, x2) -> a (x1 cos - x2 sin, x2 cos + x1 sin).  Angles reach a
 // million radians at long contexts, where an fp32 angle is off by a twentieth of a radian, so they are formed in fp64 and reduced to one turn
-// before sine and cosine.  The turn itself is done in fp64 as well and rounded once: the key's norm, which decides whether it is kept,
-// is that of the row as stored, and four fp64 operations an element hide behind the memory (two bytes in, two out).
+// before sine and cosine.  The turn itself is done in fp64 as well and rounded to fp32, and for bf16 from there, which is how frameworks
+// convert doubles (one rounding in its place, by a bit that says whether anything lies below: 0 to 7 % longer, and one element in 65536
+// that lies beside a middle on the other side of it than theirs); the key's norm, which decides whether it is kept, is that of the row as
+// stored, and four fp64 operations an element hide behind the memory (two bytes in, two out).
 //
 // A workgroup takes some tokens: their angles once into LDS, for all heads; then rows of Q, K and V, 16 elements a lane in two pieces
 // of 8, neighbouring lanes side by side: of what is turned pieces u and u + rot/16 (the two halves belong together; interleaved pairs
