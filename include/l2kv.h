@@ -425,8 +425,8 @@ size_t l2kv_decode_ragged_workspace_bytes(int32_t n_seq, int32_t Hq, int64_t max
  *
  * Tokens of several sequences are packed: sequence s = tokens
  * offsets[s] .. offsets[s+1]-1 of every tensor (DEVICE int64 [n_seq+1],
- * ascending, first entry 0; sequences may be empty; tokens behind the last one are
- * neither read nor written).  As above, contents of device arrays cannot be
+ * ascending, first entry 0; sequences may be empty; tokens behind the last one have
+ * no effect and nothing is written for them).  As above, contents of device arrays cannot be
  * checked on the host: the kernels force what they read into the buffers.
  * Q, K and V of a token are heads of D contiguous elements, a token's heads side by
  * side; the *_stride arguments are the ELEMENTS between two tokens (>= heads*D,
@@ -512,8 +512,9 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  *             kv_lens[b] <= T or NULL (all T), total_rows = ((B-1)*Hkv + 1) * T.
  *             With several KV heads a sequence has at most kv_head_stride / D rows,
  *             whatever offsets and lengths say: its rows of the next head follow.
- *   max_kv  : an upper bound of all n_kv (sizes the workspace and the
+ *   max_kv  : an upper bound of all n_kv, at least 1 (sizes the workspace and the
  *             decomposition; rows beyond it are still attended to)
+ *   scale   : softmax scale; <= 0 selects 1/sqrt(D)
  *   O   out : [total_q][Hq][D], dense, of type dt
  *   workspace: l2kv_prompt_attn_workspace_bytes(...) bytes, 16-aligned; contents
  *             irrelevant before and after, one per call that may run at the same
@@ -523,8 +524,11 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  *             has the largest of theirs, or, for any sizes of one D,
  *             compute units (l2kv_device_info) * (2048 * (D + 4) + 24) bytes.
  * Arithmetic: fp32 scores, softmax and sums; for bf16, products on the matrix unit
- * with the softmax weights rounded to bf16 (their sum is that of the rounded ones) and O
- * rounded once.
+ * with the softmax weights rounded to bf16 (their sum is that of the rounded ones; O is
+ * off by about a tenth more than by its own rounding, and differs by that much from
+ * l2kv_decode_attn*, which hold weights in fp32) and O rounded once.  Weights are at
+ * most 1: sums leave the range of fp32 only where those of a plain softmax do.
+ * NaN and infinities reach the results of the queries that see them.
  * Errors: NULL, SHAPE (Hq % Hkv != 0, Hq/Hkv > 8 -- > 4 for D = 256 --, ...), DTYPE, WORKSPACE, ALIGN, LAUNCH.
  */
 l2kv_status l2kv_prompt_attn(const void* Q, const void* K, const void* V, l2kv_dtype dt, int32_t n_seq, int32_t Hq,

@@ -510,7 +510,8 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
 static bool rows_sizes_ok(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt) {
     if (!dtype_ok(dt) || !dim_ok(D, dt) || n_seq <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || Hq / Hkv > max_group(D)) return false;
     if (total_q <= 0 || total_q > kMaxTokens || max_kv < 0 || max_kv > kMaxTokens) return false;
-    // at most 2^24 workgroups of 256 lanes: a block has at least 8 tokens (64 rows, groups of 8)
+    // Fewer than 2^24 workgroups of 256 lanes, whose blocks have at least 8 tokens (64 rows, groups of 8), and fewer than 2^23 of 512, whose blocks
+    // have at least 32 and sequences more than 12: 4 tokens a block are counted, with which both hold.
     return (total_q / 4 + n_seq) <= ((int64_t{1} << 24) - 1) / Hkv;
 }
 

@@ -14,7 +14,7 @@
 // together: 3.4 TB/s instead of 4.2 for fp32 rows of 128 of which 16 elements are turned.)
 //
 // Bound by memory: 36768 bf16 tokens of 32 + 8 + 8 heads of 128 take 173 to 179 us, 5.05 to 5.25 TB/s in and out (a large copy: 4.80), 183 without the
-// rows that are on their way ahead; 64 fp32 tokens of 8 + 4 + 4 heads of 64 take 4.4 us, a launch and three loads that wait for one another.
+// rows that are on their way ahead; 64 fp32 tokens of 8 + 4 + 4 heads of 64 take 4.4 to 4.8 us, a launch and three loads that wait for one another.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 #include "row_norm.hpp"
@@ -24,8 +24,8 @@ namespace {
 
 constexpr int kRotThreads = 256, kRotWaves = kRotThreads / kWaveSize;
 // Most tokens of a workgroup, and most rows from more than 4 of them: heads are few where 4 tokens leave lanes idle (32768 fp32 tokens of 1 + 1 + 1
-// heads of 64 21.4 us, 17.0 with 16 of them; 8 + 8 + 8 heads 91 and, with 8, 95).  Rows of 512 bytes fill the lanes, and the LDS of more
-// angles costs workgroups (bf16, D 256, 4 + 1 + 1 heads: 41 us, 51 with 16).
+// heads of 64 21.7 us, 17.3 with 16 of them; 8 + 8 + 8 heads 92 and, with 8, 98).  Rows of 512 bytes fill the lanes, and the LDS of more
+// angles costs workgroups (bf16, D 256, 4 + 1 + 1 heads: 47 us, 55 with 16).
 constexpr int rot_tokens(int row_bytes) { return row_bytes <= 256 ? 16 : 4; }
 constexpr int kRotRows = 96;
 constexpr int64_t kNoSlot = -1, kNoSequence = -2;

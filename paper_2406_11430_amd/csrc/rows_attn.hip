@@ -29,13 +29,14 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
 // K and V least often; two workgroups of a narrow one share a compute unit, so that one computes while the other begins or ends an item, and
 // there are more of them.  Measured (bf16, D 128, 8 KV heads of 4 query heads, us):
 //                                       256 rows  128 rows  64 rows  stretches
-//   1 prompt of 8192 tokens                  554       581      653        652    (most work: the widest block)
-//   64 prompts of 64                        36.7      31.4     38.7       39.2    (two and more 128-row workgroups for each compute unit)
-//   1 prompt of 512                         23.6      20.9     15.1       23.7    (few: the narrowest)
-//   4 trees of 64 nodes over 16000 rows      419       371      242         94    (few and long: stretches, of the block that takes the rows)
-//   1 tree of 64 nodes over 8192             221       194      111       30.8    (K and V are in the caches: stretches of the narrowest; the widest 37)
-// Over 90 sizes of all row types what this chooses took 3 % longer than the best of the six (the widest block that a sequence fills, and
-// stretches wherever there are fewer than four items for each compute unit: 25 %).
+//   1 prompt of 8192 tokens                  510       529      603        595    (most work: the widest block)
+//   64 prompts of 64                        35.5      30.3     37.9       38.6    (two and more 128-row workgroups for each compute unit)
+//   1 prompt of 512                         22.2      19.2     14.3       24.4    (few: the narrowest)
+//   4 trees of 64 nodes over 16000 rows      389       328      244         92    (few and long: stretches, of the block that takes the rows)
+//   1 tree of 64 nodes over 8192             204       172      106       29.9    (K and V are in the caches: stretches of the narrowest; the widest 36)
+// Over 90 sizes of all row types what this chooses took 3 % longer than the best of the six (the best single one, stretches of 128 rows: 33 %).
+// It knows the longest sequence and not the sum: a batch with one that is much longer than the others may get workgroups of their own where
+// stretches are far better (64 trees of 8 nodes, one over 131072 rows and the others over 2000: 2006 us, stretches 197).
 RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree) {
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t units = device_compute_units(), mean = (total_q + n_seq - 1) / n_seq;
@@ -67,14 +68,14 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
         if (!stretches) p.shape = kNarrowest;
     }
     // A tree's cached rows are read once (or by a few workgroups at about the same time), and more of them than the memory-side cache holds
-    // are not there when the next call comes: 64 trees over 500 to 4000 rows 126 us, 138 through the caches; 64 over 1000 61 and 67.  16
-    // over 1000 rows, which stay there from call to call, would take 28 us instead of 24.
+    // are not there when the next call comes: 64 trees over 500 to 4000 rows 124 us, 135 through the caches; 64 over 1000 56 and 63.  16
+    // over 1000 rows, which stay there from call to call, would take 28 us instead of 23.
     p.once = tree && bytes > 256e6;
     const ShapeSizes s = sizes(p.shape);
     p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
     p.n_blocks = (int32_t)blocks;
-    // Two tiles of keys and what an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 18.3 us, 23.0 with four tiles.
+    // Two tiles of keys and what an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 15.0 us, 17.0 with four tiles.
     p.least_tiles = rows_item_tiles(tree) + 2;
     p.workgroups = 0;
     if (stretches) {

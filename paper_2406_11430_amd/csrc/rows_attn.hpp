@@ -29,7 +29,7 @@ struct RowsArgs {
 };
 
 // What an item counts for besides its keys, in tiles of them: of a prompt one for its beginning and its end and one because its
-// diagonal may lie in a tile more (fp32, odd lengths: 38 us, 43 with one tile), of a tree one (7 fp32 nodes over 4000 rows: 35 us, 39 with two).
+// diagonal may lie in a tile more (fp32, odd lengths: 34.9 us, 35.7 with one tile), of a tree one (7 fp32 nodes over 4000 rows: 35.5 us, 38.9 with two).
 constexpr int rows_item_tiles(bool tree) { return tree ? 1 : 2; }
 
 // How a launch is cut: the shape of its workgroups, which takes blocks of so many tokens, and the number of workgroups that take equal

@@ -228,9 +228,9 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
 // kStages of them have room in LDS, all but one on their way while that one is worked on.  kOnce: cached rows are not read again soon.
 //
 // Prompts are bound by the two units that do not overlap enough: of a tile of 256 rows and 64 keys (bf16, D 128; 1.9 us) the matrix unit is
-// busy for 55 % of the cycles, exponentials, maxima and roundings for 47, and the clock falls as they are busier.  A prompt of 32768 tokens (32 query heads, 8 KV heads) takes 7.6 to 8.2 ms,
-// 1.07 to 1.16 PFLOP/s of the 1.37 that a large matrix product reaches.  Trees are bound by memory:
-// 64 of 1 to 32 nodes over 500 to 4000 rows 121 us, 5.0 TB/s (a large copy: 4.80).
+// busy for 55 % of the cycles, exponentials, maxima and roundings for 46, and the clock falls as they are busier.  A prompt of 32768 tokens (32 query heads, 8 KV heads) takes 7.7 to 8.4 ms
+// from card to card, 1.05 to 1.14 PFLOP/s of the 1.37 that a large matrix product reaches.  Batches of trees are bound by memory:
+// 64 of 1 to 32 nodes over 500 to 4000 rows 119 to 121 us, 5.1 TB/s (a large copy: 4.80).
 template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree, bool kOnce>
 __global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {
