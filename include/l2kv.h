@@ -527,7 +527,8 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
  * with the softmax weights rounded to bf16 (their sum is that of the rounded ones; O is
  * off by about a tenth more than by its own rounding, and differs by that much from
  * l2kv_decode_attn*, which hold weights in fp32) and O rounded once.  Weights are at
- * most 1: sums leave the range of fp32 only where those of a plain softmax do.
+ * most 1: sums leave the range of fp32 only where those of a plain softmax do
+ * (bf16 values below 2^-110 in size may count as zero).
  * NaN and infinities reach the results of the queries that see them.
  * Errors: NULL, SHAPE (Hq % Hkv != 0, Hq/Hkv > 8 -- > 4 for D = 256 --, ...), DTYPE, WORKSPACE, ALIGN, LAUNCH.
  */

@@ -30,7 +30,8 @@ constexpr int kTile = 32;                    // query rows and keys of one matri
 // score passes it: they are at most 1, as are the factors of a move, so sums of weights times values leave the range of fp32 only where those of a
 // plain softmax do, and most tiles leave the accumulators alone.  bf16: 16, so that a row's largest weight is between 2^-16 and 1 (8 instead of
 // 16: 1.3 % longer); weights are rounded relative to themselves, wherever they lie, the exponent's argument, of up to 32 near the top, is off by 2^-20 at
-// most beside their 2^-8, and what falls below 2^-126 is below 2^-110 of the largest.  fp32, where the argument's bits are
+// most beside their 2^-8, and what falls below 2^-126 is below 2^-110 of the largest (at the other end, products of values below 2^-110 may be
+// lost, an error below any result's use).  fp32, where the argument's bits are
 // the weight's: 0, the largest score itself; products take so long there that moving the accumulators costs little (three prompts of 511 to
 // 1533 tokens, 4 heads of 64: 35.9 -> 36.7 us).
 template <typename E> constexpr float kHeadroom = E::kBytes == 2 ? 16.0f : 0.0f;
