@@ -592,6 +592,157 @@ l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float*
                                     float* norms_c, int32_t* pos_c, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The cache in pages.
+ *
+ * A slot cache [planes][total_slots][D] with norms_c, pos_c [planes][total_slots] whose slots are handed out in pages
+ * of page_size (16, 32, 64, 128 or 256): page p = slots p*page_size .. of every plane, total_slots = n_pages *
+ * page_size.  Row r of sequence s lies at slot
+ *     page_table[s][r / page_size] * page_size + r % page_size
+ * page_table: DEVICE int32 [n_seq][max_pages], the same for all planes (layers and KV heads); -1 where there is no page.
+ * A sequence has at most max_pages * page_size rows (at most 2^31-1).  An entry that is no page's number is forced into
+ * them where rows are read, and takes no row where they are written.  Several sequences may hold the same page: who
+ * writes rows first asks l2kv_pages_reserve for them.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * l2kv_rotary_append with norms of the heads before the rotation.  Every query head (where q_weight is given) and every
+ * key head (k_weight) is divided by the root of its mean square and multiplied by the weights, one for each element:
+ *     y[d] = x[d] / sqrt( sum_e x[e]^2 / D + eps ) * weight[d]
+ * and then turned as in l2kv_rotary_append; elements from rot_dim on are normed alike.  All of it in fp64, rounded to
+ * fp32 and for bf16 from there.  norms_c are those of the keys as stored.
+ *   q_weight, k_weight in: DEVICE fp32 [D], NULL: heads of that kind are not normed
+ *   eps   : >= 0, finite (0 and a head of zeros give NaN)
+ * Everything else as l2kv_rotary_append, which both NULL makes it.
+ * Errors: as l2kv_rotary_append; SHAPE for eps.
+ */
+l2kv_status l2kv_norm_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                                    int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                                    int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                                    const int32_t* positions, const double* freqs, int32_t rot_dim,
+                                    l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                                    const int64_t* token_offsets, const int64_t* slot_offsets,
+                                    const int32_t* lens_in, int32_t* lens_out, int64_t total_slots, void* Qr,
+                                    void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream);
+
+/*
+ * The same into pages: the j-th token of sequence s becomes row lens_in[s] + j of it.  A token whose row has no page is
+ * not stored (its queries are turned all the same).  lens_out[s] = lens_in[s] + the tokens stored before the first such
+ * one; may be NULL (calls for further layers), must not be lens_in.
+ *   Kc, Vc out: one layer's planes [Hkv][n_pages*page_size][D]; norms_c, pos_c likewise
+ * Errors: as l2kv_norm_rotary_append; SHAPE for page_size, max_pages, n_pages.
+ */
+l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                              int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                              int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                              const int32_t* positions, const double* freqs, int32_t rot_dim,
+                              l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                              const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
+                              int32_t page_size, int32_t n_pages, const int32_t* lens_in, int32_t* lens_out,
+                              void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream);
+
+/*
+ * Attention of the last tokens of every sequence, one or many, over all its rows in pages: l2kv_prompt_attn with the
+ * rows found by the page table.  Query i of the n_q of sequence s attends to its rows j <= i + n_kv - n_q; a single
+ * token (a decode step) sees all n_kv.  The rows of the new tokens themselves are in the cache already
+ * (l2kv_paged_append).  Rows of a page behind the last are not seen, whatever they hold.
+ *   Q      in : [total_q] x Hq heads, q_offsets DEVICE int64 [n_seq+1]
+ *   Kc, Vc in : one layer's planes [Hkv][n_pages*page_size][D]
+ *   kv_lens in: DEVICE int32 [n_seq], rows of every sequence (0 allowed)
+ *   max_kv    : an upper bound of all of them, at least 1 (sizes the workspace and the decomposition; rows beyond it
+ *               are still attended to)
+ *   O     out : [total_q][Hq][D], dense, of type dt
+ *   workspace : l2kv_paged_attn_workspace_bytes(...), as for l2kv_prompt_attn, with the same bound for all sizes
+ * Arithmetic and errors: as l2kv_prompt_attn; SHAPE for page_size, max_pages, n_pages and where n_seq * max_pages exceeds 2^31-1.
+ */
+l2kv_status l2kv_paged_attn(const void* Q, const void* Kc, const void* Vc, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
+                            int32_t Hkv, int32_t D, int64_t total_q, int64_t q_stride, const int64_t* q_offsets,
+                            const int32_t* page_table, int32_t max_pages, int32_t page_size, int32_t n_pages,
+                            const int32_t* kv_lens, int64_t max_kv, float scale, void* O, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+size_t l2kv_paged_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
+                                       l2kv_dtype dt);
+
+/*
+ * The pages' bookkeeping, in device memory, so that a serving loop needs no word from the device:
+ *   refs       DEVICE int32 [n_pages]: holders of every page (entries of page tables that name it)
+ *   free_pages DEVICE int32 [n_pages]: the first free_count[0] are the pages without holders, the last of them the next
+ *              to be handed out; free_count DEVICE int32 [1]
+ * l2kv_pages_init makes all pages free and every entry of a table -1 (several tables: -1 in the others is the caller's
+ * to write).  Which page goes where depends on nothing but the order of the entries: sequence after sequence, page
+ * after page.  Calls that share refs, free_pages or a workspace must not overlap in time.  n_seq <= 65535.
+ * Errors of the four calls: NULL, SHAPE (also n_seq * max_pages or n_pages * page_size beyond 2^31-1), ALIGN, LAUNCH;
+ * of those with a workspace, l2kv_pages_workspace_bytes(n_pages) bytes, 16-aligned, contents irrelevant before
+ * and after, WORKSPACE.
+ */
+l2kv_status l2kv_pages_init(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t* refs, int32_t* free_pages,
+                            int32_t* free_count, int32_t n_pages, void* stream);
+
+/*
+ * Sequences that go on from others: sequence i of table_out has the pages and the length of sequence parents[i] of
+ * table_in (a number outside 0..n_in-1: none), each page held once more.  A parent may have any number of children.
+ * What table_out named before is written over, not released (l2kv_pages_release).
+ *   table_in  in : [n_in][max_pages], lens_in [n_in]; pages up to lens_in are taken over
+ *   parents   in : DEVICE int32 [n_out]
+ *   table_out out: [n_out][max_pages], lens_out [n_out]; neither may be an input
+ */
+l2kv_status l2kv_pages_fork(const int32_t* table_in, const int32_t* lens_in, int32_t n_in, const int32_t* parents,
+                            int32_t n_out, int32_t max_pages, int32_t page_size, int32_t n_pages, int32_t* table_out,
+                            int32_t* lens_out, int32_t* refs, void* stream);
+
+/*
+ * Room for rows from[s] .. to[s]-1 of every sequence, to be written by it alone: entries of these rows that are -1 get a
+ * free page; a page that others hold as well is copied, all planes with norms and ids, and the copy takes its
+ * place (where all holders of a page ask for it in the same call the last keeps it).
+ *   from, to in : DEVICE int32 [n_seq]; from >= to, from < 0 or to > max_pages * page_size asks for nothing
+ *   ends    out : [n_seq], to[s] where the sequence has its room, else from[s]: nothing was asked for, or the free pages do not
+ *                 suffice and nothing of it was changed.  Sequences are served in order: behind one that does not fit
+ *                 only those that need no page get theirs.  Must not be an input.
+ *   Kc, Vc, norms_c, pos_c: all planes of the cache, [n_planes][n_pages*page_size]
+ * Errors: also DTYPE.
+ */
+l2kv_status l2kv_pages_reserve(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t page_size,
+                               const int32_t* from, const int32_t* to, int32_t* ends, int32_t* refs, int32_t* free_pages,
+                               int32_t* free_count, int32_t n_pages, l2kv_dtype dt, int32_t n_planes, int32_t D, void* Kc,
+                               void* Vc, float* norms_c, int32_t* pos_c, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * Sequences give up their pages behind the first keep_lens[s] rows (0: all): the entries become -1, each page has a holder
+ * less, and those without any are free again (released and reserved once more in the same order, the same ones come
+ * back).  keep_lens DEVICE int32 [n_seq].
+ */
+l2kv_status l2kv_pages_release(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t page_size,
+                               const int32_t* keep_lens, int32_t* refs, int32_t* free_pages, int32_t* free_count,
+                               int32_t n_pages, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t l2kv_pages_workspace_bytes(int64_t n_pages);
+
+/*
+ * Compaction in pages (the rule of Sec. 1 on a paged cache): of every plane and sequence the min(keep[s], lens_in[s]) rows
+ * with the lowest (norm bits, row), in the order of the rows, become rows 0, 1, ... of the sequence in table_out;
+ * K, V, norm and token id.  As many in every plane, other ones in each.  Rows are appended behind one another, so the
+ * lower row is the earlier token and ties go to it, as in l2kv_select.
+ *   Kc, Vc, norms_c, pos_c: [n_planes][n_pages*page_size], read and written; the pages of table_out must not be those of
+ *             table_in (l2kv_pages_reserve before, l2kv_pages_release behind); pages that several sequences hold are only read
+ *   table_in [n_seq][max_in], lens_in, keep [n_seq]; table_out [n_seq][max_out], lens_out [n_seq] = rows kept (capped at the
+ *             pages' room; rows whose entry is no page are not written).  lens_out must not be an input.
+ *   total_rows, total_kept: upper bounds of the sums of lens_in and of the rows kept (size the workspace and the launches;
+ *             what goes beyond them is left out); total_kept < 2^29
+ *   max_len : an upper bound of lens_in (chooses the kernel variant; rows beyond it are left out)
+ *   workspace: l2kv_paged_compress_workspace_bytes(...) bytes, 16-aligned; contents irrelevant before and after, one per call
+ *             that may run at the same time
+ * Errors: NULL, DTYPE, SHAPE, WORKSPACE, ALIGN, LAUNCH.
+ */
+l2kv_status l2kv_paged_compress(void* Kc, void* Vc, float* norms_c, int32_t* pos_c, l2kv_dtype dt, int32_t n_planes,
+                                int32_t n_seq, int32_t D, int32_t page_size, int32_t n_pages, const int32_t* table_in,
+                                int32_t max_in, const int32_t* lens_in, const int32_t* keep, const int32_t* table_out,
+                                int32_t max_out, int32_t* lens_out, int64_t total_rows, int64_t total_kept,
+                                int64_t max_len, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t l2kv_paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept);
+
+/* ---------------------------------------------------------------------------
  * Attention-loss analysis (Sec. 3, Eq. 5-7)
  *
  * When m of the T cached pairs of a head are dropped, the attention loss L^m is

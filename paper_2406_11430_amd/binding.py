@@ -1,5 +1,5 @@
 """Binding of libl2kv.so: one Python function per C entry point, same
-names, argument marshalling only (ctypes; the calls of a decode step, plain or drafted, of prompts and the compression also natively, csrc/calls.cpp).  Tensors are torch CUDA(HIP) tensors used as
+names, argument marshalling only (ctypes; the calls of a decode step, plain, drafted or in pages, of prompts and the compression also natively, csrc/calls.cpp).  Tensors are torch CUDA(HIP) tensors used as
 device memory; every step of the path runs inside the library's kernels.
 
 The library must already be built (``python -m paper_2406_11430_amd.build``);
@@ -99,6 +99,40 @@ SIGNATURES = {
                                           C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
                                           C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "l2kv_norm_rotary_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32,
+                                          C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                          C.c_void_p, C.c_double, C.c_void_p, C.c_void_p, C.c_int32, C.c_int,
+                                          C.c_double, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p]),
+    "l2kv_paged_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32,
+                                    C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                    C.c_void_p, C.c_double, C.c_void_p, C.c_void_p, C.c_int32, C.c_int,
+                                    C.c_double, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                    C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p]),
+    "l2kv_paged_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int32,
+                                  C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                  C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
+                                  C.c_size_t, C.c_void_p]),
+    "l2kv_pages_init": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_int32, C.c_void_p]),
+    "l2kv_pages_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+                                  C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "l2kv_pages_reserve": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int,
+                                     C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]),
+    "l2kv_pages_release": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "l2kv_paged_compress": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32,
+                                      C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
+                                      C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "l2kv_paged_attn_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                                                     C.c_int32, C.c_int]),
+    "l2kv_pages_workspace_bytes": (C.c_size_t, [C.c_int64]),
+    "l2kv_paged_compress_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64, C.c_int64]),
     "l2kv_norm_ranks": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t,
                                   C.c_void_p]),
     "l2kv_norm_ranks_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64]),
@@ -126,6 +160,7 @@ _calls = None
 class _PythonCalls:
     """In place of the native calls: leaves every call to the checks and the marshalling in this file."""
     decode_attn = decode_attn_out = compress = rotary_append = prompt_attn = tree_attn = append_path = staticmethod(lambda *args: None)
+    paged_append = paged_attn = pages_fork = pages_reserve = pages_release = paged_compress = staticmethod(lambda *args: None)
 
 
 def _load_calls():
@@ -149,7 +184,9 @@ def calls():
             module = _load_calls()
             module.bind(*(C.cast(f, C.c_void_p).value for f in (
                 handle.l2kv_decode_attn, handle.l2kv_decode_attn_out, handle.l2kv_compress, handle.l2kv_keep_count,
-                handle.l2kv_rotary_append, handle.l2kv_prompt_attn, handle.l2kv_tree_attn, handle.l2kv_stream_append_path)))
+                handle.l2kv_rotary_append, handle.l2kv_prompt_attn, handle.l2kv_tree_attn, handle.l2kv_stream_append_path,
+                handle.l2kv_paged_append, handle.l2kv_paged_attn, handle.l2kv_pages_fork, handle.l2kv_pages_reserve,
+                handle.l2kv_pages_release, handle.l2kv_paged_compress)))
         except ImportError as e:
             warnings.warn("%s; calls go through ctypes (build with `python -m paper_2406_11430_amd.build`)" % e, RuntimeWarning)
             module = _PythonCalls
@@ -670,6 +707,206 @@ def l2kv_stream_append_path(Kt: torch.Tensor, Vt: torch.Tensor, norms_t: torch.T
         _ptr(Kt), _ptr(Vt), _ptr(norms_t), _ptr(pos_t), _dtype_code(Kt), n_planes, n_seq, D, total, _ptr(node_offsets),
         _ptr(path), max_path, _ptr(path_lens), _ptr(slot_offsets), total_slots, _ptr(lens_in), _ptr(lens_out), _ptr(Kc),
         _ptr(Vc), _ptr(norms_c), _ptr(pos_c), _stream(stream)))
+
+
+# ------------------------------------------------------------ the cache in pages
+def l2kv_norm_rotary_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, q_weight: Optional[torch.Tensor],
+                            k_weight: Optional[torch.Tensor], eps: float, positions: torch.Tensor, freqs: torch.Tensor,
+                            Qr: Optional[torch.Tensor], Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor,
+                            token_offsets: Optional[torch.Tensor] = None, slot_offsets: Optional[torch.Tensor] = None,
+                            lens_in: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+                            layout: int = L2KV_ROTARY_HALF, amplitude: float = 1.0, stream=None) -> None:
+    """l2kv_rotary_append with norms of the query and key heads before the rotation; weights are float32 ``[D]`` or None."""
+    total, Hkv, D, Hq, strides, total_slots = _append_shapes(Q, K, V, q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)
+    _dev(token_offsets, slot_offsets, lens_in, lens_out)
+    n_seq = 0
+    if token_offsets is not None:
+        n_seq = token_offsets.numel() - 1
+        _i64(token_offsets, n_seq + 1)
+        for t, check in ((slot_offsets, _i64), (lens_in, _i32), (lens_out, _i32)):
+            if t is not None:
+                check(t, n_seq + (check is _i64))
+    _check("l2kv_norm_rotary_append", lib().l2kv_norm_rotary_append(
+        _ptr(Q), _ptr(K), _ptr(V), _dtype_code(K), total, Hq, Hkv, D, *strides, _ptr(q_weight), _ptr(k_weight), float(eps),
+        _ptr(positions), _ptr(freqs), 2 * freqs.numel(), int(layout), float(amplitude), n_seq, _ptr(token_offsets), _ptr(slot_offsets),
+        _ptr(lens_in), _ptr(lens_out), total_slots, _ptr(Qr), _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c), _stream(stream)))
+
+
+def _append_shapes(Q, K, V, q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c):
+    """What the calls that append check alike -> (tokens, Hkv, D, Hq, strides of tokens, slots)."""
+    _dev(q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)
+    total, Hkv, D = K.shape
+    k_stride, v_stride = _tokens(K), _tokens(V)
+    Hq, q_stride = (0, 0) if Q is None else (Q.shape[1], _tokens(Q))
+    planes, total_slots, Dc = Kc.shape
+    assert V.shape == K.shape and V.dtype == K.dtype == Kc.dtype == Vc.dtype and Vc.shape == Kc.shape
+    assert (planes, Dc) == (Hkv, D) and norms_c.shape == (Hkv, total_slots) and norms_c.dtype == torch.float32
+    assert pos_c.shape == (Hkv, total_slots) and pos_c.dtype == torch.int32
+    if Q is not None:
+        assert Q.shape == (total, Hq, D) and Q.dtype == K.dtype
+        assert Qr is None or (Qr.shape == Q.shape and Qr.dtype == Q.dtype)
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.numel() == D)
+    assert freqs.dtype == torch.float64
+    _i32(positions, total)
+    return total, Hkv, D, Hq, (q_stride, k_stride, v_stride), total_slots
+
+
+def _page_table(page_table: torch.Tensor, page_size: int, slots: Optional[int] = None):
+    """-> (n_seq, max_pages, n_pages of a cache of so many slots)."""
+    _dev(page_table)
+    assert page_table.dtype == torch.int32 and page_table.dim() == 2
+    if slots is not None and (page_size <= 0 or slots % page_size != 0):
+        raise ValueError("l2kv needs whole pages: %d slots in pages of %d" % (slots, page_size))
+    return (*page_table.shape, 0 if slots is None else slots // page_size)
+
+
+def l2kv_paged_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor,
+                      Qr: Optional[torch.Tensor], Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor,
+                      token_offsets: torch.Tensor, page_table: torch.Tensor, page_size: int, lens_in: torch.Tensor,
+                      lens_out: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, layout: int = L2KV_ROTARY_HALF,
+                      amplitude: float = 1.0, stream=None) -> None:
+    """Q ``[tokens, Hq, D]`` -> Qr; K, V ``[tokens, Hkv, D]`` -> the pages of Kc, Vc ``[Hkv, n_pages * page_size, D]`` that
+    page_table ``[n_seq, max_pages]`` int32 names.  Heads are normed where there are weights (float32 ``[D]``)."""
+    st = (_calls or calls()).paged_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size, lens_in,
+                                        lens_out, q_weight, k_weight, eps, layout, amplitude, stream, _stream)
+    if st is not None:
+        return _check("l2kv_paged_append", st)
+    total, Hkv, D, Hq, strides, slots = _append_shapes(Q, K, V, q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)
+    _dev(token_offsets, lens_in, lens_out)
+    n_seq, max_pages, n_pages = _page_table(page_table, page_size, slots)
+    _i64(token_offsets, n_seq + 1), _i32(lens_in, n_seq)
+    if lens_out is not None:
+        _i32(lens_out, n_seq)
+    _check("l2kv_paged_append", lib().l2kv_paged_append(
+        _ptr(Q), _ptr(K), _ptr(V), _dtype_code(K), total, Hq, Hkv, D, *strides, _ptr(q_weight), _ptr(k_weight), float(eps),
+        _ptr(positions), _ptr(freqs), 2 * freqs.numel(), int(layout), float(amplitude), n_seq, _ptr(token_offsets), _ptr(page_table),
+        max_pages, int(page_size), n_pages, _ptr(lens_in), _ptr(lens_out), _ptr(Qr), _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c),
+        _stream(stream)))
+
+
+def l2kv_paged_attn_workspace_bytes(n_seq: int, Hq: int, Hkv: int, total_q: int, max_kv: int, D: int, dtype) -> int:
+    return int(lib().l2kv_paged_attn_workspace_bytes(int(n_seq), int(Hq), int(Hkv), int(total_q), int(max_kv), int(D), _code(dtype)))
+
+
+def l2kv_paged_attn(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, q_offsets: torch.Tensor, page_table: torch.Tensor,
+                    page_size: int, kv_lens: torch.Tensor, max_kv: int, O: torch.Tensor, workspace: Optional[torch.Tensor],
+                    scale: float = 0.0, stream=None) -> None:
+    """Q ``[total_q, Hq, D]`` (the last tokens of every sequence, any distance apart), Kc/Vc ``[Hkv, n_pages * page_size, D]`` (one
+    layer), kv_lens ``[n_seq]`` int32 -> O ``[total_q, Hq, D]`` of Q's type."""
+    st = (_calls or calls()).paged_attn(Q, Kc, Vc, q_offsets, page_table, page_size, kv_lens, max_kv, O, workspace, scale, stream, _stream)
+    if st is not None:
+        return _check("l2kv_paged_attn", st)
+    _dev(Kc, Vc, q_offsets, kv_lens, O, workspace)
+    total_q, Hq, D = Q.shape
+    q_stride = _tokens(Q)
+    Hkv, slots, Dc = Kc.shape
+    n_seq, max_pages, n_pages = _page_table(page_table, page_size, slots)
+    assert Dc == D and Vc.shape == Kc.shape and Kc.dtype == Vc.dtype == Q.dtype == O.dtype and O.shape == Q.shape
+    _i64(q_offsets, n_seq + 1), _i32(kv_lens, n_seq)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check("l2kv_paged_attn", lib().l2kv_paged_attn(
+        _ptr(Q), _ptr(Kc), _ptr(Vc), _dtype_code(Q), n_seq, Hq, Hkv, D, total_q, q_stride, _ptr(q_offsets), _ptr(page_table), max_pages,
+        int(page_size), n_pages, _ptr(kv_lens), int(max_kv), float(scale), _ptr(O), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def _holders(refs: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor) -> int:
+    _dev(refs, free_pages, free_count)
+    n_pages = refs.numel()
+    _i32(refs, n_pages), _i32(free_pages, n_pages), _i32(free_count, 1)
+    return n_pages
+
+
+def l2kv_pages_init(page_table: torch.Tensor, refs: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, stream=None) -> None:
+    """All pages free, every entry of page_table ``[n_seq, max_pages]`` -1; refs, free_pages ``[n_pages]``, free_count ``[1]``, all int32."""
+    n_pages = _holders(refs, free_pages, free_count)
+    n_seq, max_pages, _ = _page_table(page_table, 1)
+    _check("l2kv_pages_init", lib().l2kv_pages_init(_ptr(page_table), n_seq, max_pages, _ptr(refs), _ptr(free_pages), _ptr(free_count),
+                                                  n_pages, _stream(stream)))
+
+
+def l2kv_pages_fork(table_in: torch.Tensor, lens_in: torch.Tensor, parents: torch.Tensor, table_out: torch.Tensor, lens_out: torch.Tensor,
+                    refs: torch.Tensor, page_size: int, stream=None) -> None:
+    """Sequence i of table_out ``[n_out, max_pages]`` goes on from sequence parents[i] of table_in ``[n_in, max_pages]``."""
+    st = (_calls or calls()).pages_fork(table_in, lens_in, parents, table_out, lens_out, refs, page_size, stream, _stream)
+    if st is not None:
+        return _check("l2kv_pages_fork", st)
+    _dev(lens_in, parents, lens_out, refs)
+    n_in, max_pages, _ = _page_table(table_in, page_size)
+    n_out, max_out, _ = _page_table(table_out, page_size)
+    assert max_out == max_pages and refs.dtype == torch.int32
+    _i32(lens_in, n_in), _i32(parents, n_out), _i32(lens_out, n_out)
+    _check("l2kv_pages_fork", lib().l2kv_pages_fork(
+        _ptr(table_in), _ptr(lens_in), n_in, _ptr(parents), n_out, max_pages, int(page_size), refs.numel(), _ptr(table_out),
+        _ptr(lens_out), _ptr(refs), _stream(stream)))
+
+
+def l2kv_pages_workspace_bytes(n_pages: int) -> int:
+    return int(lib().l2kv_pages_workspace_bytes(int(n_pages)))
+
+
+def l2kv_pages_reserve(page_table: torch.Tensor, first: torch.Tensor, to: torch.Tensor, ends: torch.Tensor, refs: torch.Tensor,
+                       free_pages: torch.Tensor, free_count: torch.Tensor, page_size: int, Kc: torch.Tensor, Vc: torch.Tensor,
+                       norms_c: torch.Tensor, pos_c: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Room for rows first[s] .. to[s]-1 of every sequence; Kc, Vc ``[n_planes, n_pages * page_size, D]`` with norms and ids are all planes."""
+    st = (_calls or calls()).pages_reserve(page_table, first, to, ends, refs, free_pages, free_count, page_size, Kc, Vc, norms_c, pos_c,
+                                         workspace, stream, _stream)
+    if st is not None:
+        return _check("l2kv_pages_reserve", st)
+    _dev(first, to, ends, Kc, Vc, norms_c, pos_c, workspace)
+    n_pages = _holders(refs, free_pages, free_count)
+    n_planes, slots, D = Kc.shape
+    n_seq, max_pages, _ = _page_table(page_table, page_size, slots)
+    _i32(first, n_seq), _i32(to, n_seq), _i32(ends, n_seq)
+    assert Vc.shape == Kc.shape and Vc.dtype == Kc.dtype and slots == n_pages * page_size
+    assert norms_c.shape == (n_planes, slots) == pos_c.shape and norms_c.dtype == torch.float32 and pos_c.dtype == torch.int32
+    _check("l2kv_pages_reserve", lib().l2kv_pages_reserve(
+        _ptr(page_table), n_seq, max_pages, int(page_size), _ptr(first), _ptr(to), _ptr(ends), _ptr(refs), _ptr(free_pages),
+        _ptr(free_count), n_pages, _dtype_code(Kc), n_planes, D, _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def l2kv_pages_release(page_table: torch.Tensor, keep_lens: torch.Tensor, refs: torch.Tensor, free_pages: torch.Tensor,
+                       free_count: torch.Tensor, page_size: int, workspace: torch.Tensor, stream=None) -> None:
+    """Sequences give up their pages behind the first keep_lens[s] rows."""
+    st = (_calls or calls()).pages_release(page_table, keep_lens, refs, free_pages, free_count, page_size, workspace, stream, _stream)
+    if st is not None:
+        return _check("l2kv_pages_release", st)
+    _dev(keep_lens, workspace)
+    n_pages = _holders(refs, free_pages, free_count)
+    n_seq, max_pages, _ = _page_table(page_table, page_size)
+    _i32(keep_lens, n_seq)
+    _check("l2kv_pages_release", lib().l2kv_pages_release(
+        _ptr(page_table), n_seq, max_pages, int(page_size), _ptr(keep_lens), _ptr(refs), _ptr(free_pages), _ptr(free_count), n_pages,
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def l2kv_paged_compress_workspace_bytes(n_planes: int, n_seq: int, total_rows: int, total_kept: int) -> int:
+    return int(lib().l2kv_paged_compress_workspace_bytes(int(n_planes), int(n_seq), int(total_rows), int(total_kept)))
+
+
+def l2kv_paged_compress(Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor, table_in: torch.Tensor,
+                        lens_in: torch.Tensor, keep: torch.Tensor, table_out: torch.Tensor, lens_out: torch.Tensor, page_size: int,
+                        total_rows: int, total_kept: int, max_len: int, workspace: torch.Tensor, stream=None) -> None:
+    """The keep[s] lowest-norm rows of every sequence and plane of Kc, Vc ``[n_planes, n_pages * page_size, D]``, from the pages of
+    table_in ``[n_seq, max_in]`` into those of table_out ``[n_seq, max_out]``; total_rows, total_kept, max_len are bounds of the sums
+    of lens_in and keep and of lens_in."""
+    st = (_calls or calls()).paged_compress(Kc, Vc, norms_c, pos_c, table_in, lens_in, keep, table_out, lens_out, page_size, total_rows,
+                                          total_kept, max_len, workspace, stream, _stream)
+    if st is not None:
+        return _check("l2kv_paged_compress", st)
+    _dev(Kc, Vc, norms_c, pos_c, lens_in, keep, lens_out, workspace)
+    n_planes, slots, D = Kc.shape
+    n_seq, max_in, n_pages = _page_table(table_in, page_size, slots)
+    n_out, max_out, _ = _page_table(table_out, page_size, slots)
+    assert n_out == n_seq and Vc.shape == Kc.shape and Vc.dtype == Kc.dtype
+    assert norms_c.shape == (n_planes, slots) == pos_c.shape and norms_c.dtype == torch.float32 and pos_c.dtype == torch.int32
+    _i32(lens_in, n_seq), _i32(keep, n_seq), _i32(lens_out, n_seq)
+    _check("l2kv_paged_compress", lib().l2kv_paged_compress(
+        _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c), _dtype_code(Kc), n_planes, n_seq, D, int(page_size), n_pages, _ptr(table_in),
+        max_in, _ptr(lens_in), _ptr(keep), _ptr(table_out), max_out, _ptr(lens_out), int(total_rows), int(total_kept), int(max_len),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 # ------------------------------------------------------------ attention-loss analysis

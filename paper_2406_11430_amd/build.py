@@ -20,7 +20,9 @@ OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["decode_attn_bf16_128.hip", "decode_attn_bf16_256.hip", "decode_attn_bf16_64.hip",
            "decode_attn_f32_128.hip", "decode_attn_f32_64.hip", "api.hip", "norms.hip", "select.hip", "compact.hip", "decode_attn.hip", "decode_plan.hip",
            "stream.hip", "alr.hip", "rows_attn_bf16_128.hip", "rows_attn_bf16_256.hip", "rows_attn_bf16_64.hip",
-           "rows_attn_f32_128.hip", "rows_attn_f32_64.hip", "rows_attn.hip", "rotary.hip", "append_path.hip"]
+           "rows_attn_f32_128.hip", "rows_attn_f32_64.hip", "rows_attn_paged_bf16_128.hip",
+           "rows_attn_paged_bf16_256.hip", "rows_attn_paged_bf16_64.hip", "rows_attn_paged_f32_128.hip", "rows_attn_paged_f32_64.hip",
+           "rows_attn.hip", "rotary.hip", "append_path.hip", "pages.hip", "paged_compress.hip"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops is switched off on purpose: the compiler must not form

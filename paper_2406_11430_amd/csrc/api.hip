@@ -465,6 +465,80 @@ static l2kv_status check_token_stride(int64_t stride, int64_t tokens, int32_t he
     return (stride * elem_bytes(dt)) % 16 != 0 ? L2KV_ERR_ALIGN : L2KV_OK;
 }
 
+// Pages: size a power of two, all slots and all entries of a table numbered in 31 bits.
+static bool pages_ok(int32_t n_seq, int32_t max_pages, int32_t page_size, int32_t n_pages) {
+    return n_seq > 0 && max_pages > 0 && n_pages > 0 && page_size >= 16 && page_size <= 256 && (page_size & (page_size - 1)) == 0 &&
+           static_cast<int64_t>(n_seq) * max_pages <= kMaxTokens && static_cast<int64_t>(max_pages) * page_size <= kMaxTokens &&
+           static_cast<int64_t>(n_pages) * page_size <= kMaxTokens;
+}
+static int32_t page_shift_of(int32_t page_size) { return __builtin_ctz(static_cast<unsigned>(page_size)); }
+
+// The calls that append: what they share beyond pointers, offsets and places, from the checks to the launch.
+static l2kv_status rotary_append(RotaryArgs a, l2kv_dtype dt, int32_t D, l2kv_rotary_layout layout, void* stream) {
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (a.Q == nullptr) a.Hq = 0;
+    if (a.total_tokens <= 0 || a.total_tokens > kMaxTokens || a.Hkv <= 0 || a.Hkv > 65535 || a.Hq < 0 || a.Hq > 65535 ||
+        (a.Q != nullptr && a.Hq == 0) || !dim_ok(D, dt) || a.total_slots <= 0 || a.total_slots > kMaxTokens)
+        return L2KV_ERR_SHAPE;
+    if (!rot_dim_ok(a.rot, D) || (layout != L2KV_ROTARY_HALF && layout != L2KV_ROTARY_INTERLEAVED) || !std::isfinite(a.amplitude))
+        return L2KV_ERR_SHAPE;
+    if (!(a.eps >= 0.0) || !std::isfinite(a.eps)) return L2KV_ERR_SHAPE;
+    if (a.token_off == nullptr ? a.total_slots < a.total_tokens : (a.n_seq <= 0 || a.lens_in == a.lens_out)) return L2KV_ERR_SHAPE;
+    if (a.Q != nullptr)
+        if (l2kv_status st = check_token_stride(a.q_stride, a.total_tokens, a.Hq, D, dt); st != L2KV_OK) return st;
+    if (l2kv_status st = check_token_stride(a.k_stride, a.total_tokens, a.Hkv, D, dt); st != L2KV_OK) return st;
+    if (l2kv_status st = check_token_stride(a.v_stride, a.total_tokens, a.Hkv, D, dt); st != L2KV_OK) return st;
+    if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Qr, 16) || !aligned(a.Kc, 16) || !aligned(a.Vc, 16) ||
+        !aligned(a.norms_c, 4) || !aligned(a.pos_c, 4) || !aligned(a.positions, 4) || !aligned(a.freqs, 8) || !aligned(a.token_off, 8) ||
+        !aligned(a.slot_off, 8) || !aligned(a.lens_in, 4) || !aligned(a.lens_out, 4) || !aligned(a.q_weight, 4) || !aligned(a.k_weight, 4) ||
+        !aligned(a.page_table, 4))
+        return L2KV_ERR_ALIGN;
+    return rotary_dispatch(a, dt, D, layout == L2KV_ROTARY_INTERLEAVED, static_cast<hipStream_t>(stream));
+}
+
+static RotaryArgs rotary_args(const void* Q, const void* K, const void* V, int64_t total_tokens, int32_t Hq, int32_t Hkv, int64_t q_stride,
+                              int64_t k_stride, int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                              const int32_t* positions, const double* freqs, int32_t rot_dim, double amplitude, int32_t n_seq,
+                              const int64_t* token_offsets, const int32_t* lens_in, int32_t* lens_out, void* Qr, void* Kc, void* Vc,
+                              float* norms_c, int32_t* pos_c) {
+    RotaryArgs a = {};
+    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(K), a.V = static_cast<const char*>(V);
+    a.positions = positions, a.freqs = freqs;
+    a.token_off = token_offsets, a.lens_in = lens_in, a.lens_out = lens_out;
+    a.Qr = static_cast<char*>(Qr), a.Kc = static_cast<char*>(Kc), a.Vc = static_cast<char*>(Vc);
+    a.norms_c = norms_c, a.pos_c = pos_c;
+    a.total_tokens = total_tokens;
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.amplitude = amplitude, a.n_seq = n_seq, a.Hq = Hq, a.Hkv = Hkv, a.rot = rot_dim;
+    a.q_weight = q_weight, a.k_weight = k_weight, a.eps = eps;
+    return a;
+}
+
+// What none of them does without.
+static bool rotary_null(const void* Q, const void* K, const void* V, const int32_t* positions, const double* freqs, const void* Qr,
+                        const void* Kc, const void* Vc, const float* norms_c, const int32_t* pos_c) {
+    return K == nullptr || V == nullptr || positions == nullptr || freqs == nullptr || Kc == nullptr || Vc == nullptr ||
+           norms_c == nullptr || pos_c == nullptr || (Q == nullptr) != (Qr == nullptr);
+}
+
+l2kv_status l2kv_norm_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                                    int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                                    int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                                    const int32_t* positions, const double* freqs, int32_t rot_dim,
+                                    l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                                    const int64_t* token_offsets, const int64_t* slot_offsets,
+                                    const int32_t* lens_in, int32_t* lens_out, int64_t total_slots, void* Qr,
+                                    void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
+    if (rotary_null(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)) return L2KV_ERR_NULL;
+    const bool packed = token_offsets == nullptr;
+    if ((slot_offsets == nullptr) != packed || (lens_in == nullptr) != packed || (packed && lens_out != nullptr))
+        return L2KV_ERR_NULL;
+    RotaryArgs a = rotary_args(Q, K, V, total_tokens, Hq, Hkv, q_stride, k_stride, v_stride, q_weight, k_weight, eps, positions, freqs, rot_dim,
+                               amplitude, n_seq, token_offsets, lens_in, lens_out, Qr, Kc, Vc, norms_c, pos_c);
+    a.slot_off = slot_offsets, a.total_slots = total_slots;
+    return rotary_append(a, dt, D, layout, stream);
+}
+
 l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
                                int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
                                int64_t v_stride, const int32_t* positions, const double* freqs, int32_t rot_dim,
@@ -472,38 +546,28 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
                                const int64_t* token_offsets, const int64_t* slot_offsets,
                                const int32_t* lens_in, int32_t* lens_out, int64_t total_slots, void* Qr,
                                void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
-    if (K == nullptr || V == nullptr || positions == nullptr || freqs == nullptr || Kc == nullptr || Vc == nullptr ||
-        norms_c == nullptr || pos_c == nullptr || (Q == nullptr) != (Qr == nullptr))
+    return l2kv_norm_rotary_append(Q, K, V, dt, total_tokens, Hq, Hkv, D, q_stride, k_stride, v_stride, nullptr, nullptr, 0.0, positions, freqs,
+                                   rot_dim, layout, amplitude, n_seq, token_offsets, slot_offsets, lens_in, lens_out, total_slots, Qr, Kc, Vc,
+                                   norms_c, pos_c, stream);
+}
+
+l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                              int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                              int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                              const int32_t* positions, const double* freqs, int32_t rot_dim,
+                              l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                              const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
+                              int32_t page_size, int32_t n_pages, const int32_t* lens_in, int32_t* lens_out,
+                              void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
+    if (rotary_null(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c) || token_offsets == nullptr || page_table == nullptr ||
+        lens_in == nullptr)
         return L2KV_ERR_NULL;
-    const bool packed = token_offsets == nullptr;
-    if ((slot_offsets == nullptr) != packed || (lens_in == nullptr) != packed || (packed && lens_out != nullptr))
-        return L2KV_ERR_NULL;
-    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
-    if (Q == nullptr) Hq = 0;
-    if (total_tokens <= 0 || total_tokens > kMaxTokens || Hkv <= 0 || Hkv > 65535 || Hq < 0 || Hq > 65535 || (Q != nullptr && Hq == 0) ||
-        !dim_ok(D, dt) || total_slots <= 0 || total_slots > kMaxTokens)
-        return L2KV_ERR_SHAPE;
-    if (!rot_dim_ok(rot_dim, D) || (layout != L2KV_ROTARY_HALF && layout != L2KV_ROTARY_INTERLEAVED) || !std::isfinite(amplitude))
-        return L2KV_ERR_SHAPE;
-    if (packed ? total_slots < total_tokens : (n_seq <= 0 || lens_in == lens_out)) return L2KV_ERR_SHAPE;
-    if (Q != nullptr)
-        if (l2kv_status st = check_token_stride(q_stride, total_tokens, Hq, D, dt); st != L2KV_OK) return st;
-    if (l2kv_status st = check_token_stride(k_stride, total_tokens, Hkv, D, dt); st != L2KV_OK) return st;
-    if (l2kv_status st = check_token_stride(v_stride, total_tokens, Hkv, D, dt); st != L2KV_OK) return st;
-    if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(Qr, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) ||
-        !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(positions, 4) || !aligned(freqs, 8) || !aligned(token_offsets, 8) ||
-        !aligned(slot_offsets, 8) || !aligned(lens_in, 4) || !aligned(lens_out, 4))
-        return L2KV_ERR_ALIGN;
-    RotaryArgs a = {};
-    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(K), a.V = static_cast<const char*>(V);
-    a.positions = positions, a.freqs = freqs;
-    a.token_off = token_offsets, a.slot_off = slot_offsets, a.lens_in = lens_in, a.lens_out = lens_out;
-    a.Qr = static_cast<char*>(Qr), a.Kc = static_cast<char*>(Kc), a.Vc = static_cast<char*>(Vc);
-    a.norms_c = norms_c, a.pos_c = pos_c;
-    a.total_tokens = total_tokens, a.total_slots = total_slots;
-    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
-    a.amplitude = amplitude, a.n_seq = n_seq, a.Hq = Hq, a.Hkv = Hkv, a.rot = rot_dim;
-    return rotary_dispatch(a, dt, D, layout == L2KV_ROTARY_INTERLEAVED, static_cast<hipStream_t>(stream));
+    if (dtype_ok(dt) && !pages_ok(n_seq, max_pages, page_size, n_pages)) return L2KV_ERR_SHAPE;
+    RotaryArgs a = rotary_args(Q, K, V, total_tokens, Hq, Hkv, q_stride, k_stride, v_stride, q_weight, k_weight, eps, positions, freqs, rot_dim,
+                               amplitude, n_seq, token_offsets, lens_in, lens_out, Qr, Kc, Vc, norms_c, pos_c);
+    a.page_table = page_table, a.max_pages = max_pages, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
+    a.total_slots = static_cast<int64_t>(n_pages) * page_size;
+    return rotary_append(a, dt, D, layout, stream);
 }
 
 // Sizes shared by the two attentions of many query rows, and by their workspaces.
@@ -530,15 +594,21 @@ size_t l2kv_tree_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, in
     return rows_workspace_bytes(n_seq, Hq, Hkv, total_nodes, max_len, D, dt, true);
 }
 
-// The rest of both calls, from the checks that they share to the launch.
+size_t l2kv_paged_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
+                                       l2kv_dtype dt) {
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt, false);
+}
+
+// The rest of the three calls, from the checks that they share to the launch.
 static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, int64_t max_kv, float scale, void* workspace,
-                             size_t workspace_bytes, bool tree, void* stream) {
+                             size_t workspace_bytes, RowsKind kind, void* stream) {
+    const bool tree = kind == kRowsTree;
     if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
     if (!rows_sizes_ok(a.n_seq, Hq, a.Hkv, a.total_q, max_kv, D, dt) || !std::isfinite(scale)) return L2KV_ERR_SHAPE;
     if (a.total_rows <= 0 || a.total_rows > kMaxTokens || max_kv > a.total_rows || (!tree && max_kv == 0)) return L2KV_ERR_SHAPE;
     // a head may start inside the rows of another ([B][Hkv][T][D] caches), but not at the same place
     if (a.kv_head_stride < (a.Hkv > 1 ? D : 0) || a.kv_head_stride > (int64_t{1} << 58) / a.Hkv) return L2KV_ERR_SHAPE;
-    a.most_rows = a.Hkv > 1 ? a.kv_head_stride / D : a.total_rows;
+    if (kind != kRowsPaged) a.most_rows = a.Hkv > 1 ? a.kv_head_stride / D : a.total_rows;
     l2kv_status st = check_token_stride(a.q_stride, a.total_q, Hq, D, dt);
     if (st == L2KV_ERR_SHAPE) return st;
     a.G = Hq / a.Hkv;
@@ -546,11 +616,12 @@ static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, i
     if (workspace_bytes < plan.bytes || (workspace == nullptr && plan.bytes > 0)) return L2KV_ERR_WORKSPACE;
     if (st != L2KV_OK || (a.kv_head_stride * elem_bytes(dt)) % 16 != 0) return L2KV_ERR_ALIGN;
     if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Kt, 16) || !aligned(a.Vt, 16) || !aligned(a.O, 16) ||
-        !aligned(a.q_off, 8) || !aligned(a.kv_off, 8) || !aligned(a.kv_lens, 4) || !aligned(a.mask, 4) || !aligned(workspace, 16))
+        !aligned(a.q_off, 8) || !aligned(a.kv_off, 8) || !aligned(a.kv_lens, 4) || !aligned(a.mask, 4) || !aligned(a.page_table, 4) ||
+        !aligned(workspace, 16))
         return L2KV_ERR_ALIGN;
     a.scale = (scale > 0.f ? scale : 1.0f / std::sqrt(static_cast<float>(D))) * 1.44269504f;      // powers of two from here on
     a.partial = static_cast<float*>(workspace);
-    return rows_attn_dispatch(a, plan, D, dt, tree, static_cast<hipStream_t>(stream));
+    return rows_attn_dispatch(a, plan, D, dt, kind, static_cast<hipStream_t>(stream));
 }
 
 l2kv_status l2kv_prompt_attn(const void* Q, const void* K, const void* V, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
@@ -565,7 +636,27 @@ l2kv_status l2kv_prompt_attn(const void* Q, const void* K, const void* V, l2kv_d
     a.q_off = q_offsets, a.kv_off = kv_offsets, a.kv_lens = kv_lens;
     a.total_q = total_q, a.total_rows = total_rows, a.kv_head_stride = kv_head_stride, a.q_stride = q_stride;
     a.n_seq = n_seq, a.Hkv = Hkv;
-    return rows_attn(a, dt, Hq, D, max_kv, scale, workspace, workspace_bytes, false, stream);
+    return rows_attn(a, dt, Hq, D, max_kv, scale, workspace, workspace_bytes, kRowsPrompt, stream);
+}
+
+l2kv_status l2kv_paged_attn(const void* Q, const void* Kc, const void* Vc, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
+                            int32_t Hkv, int32_t D, int64_t total_q, int64_t q_stride, const int64_t* q_offsets,
+                            const int32_t* page_table, int32_t max_pages, int32_t page_size, int32_t n_pages,
+                            const int32_t* kv_lens, int64_t max_kv, float scale, void* O, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (Q == nullptr || Kc == nullptr || Vc == nullptr || O == nullptr || q_offsets == nullptr || page_table == nullptr || kv_lens == nullptr)
+        return L2KV_ERR_NULL;
+    if (dtype_ok(dt) && !pages_ok(n_seq, max_pages, page_size, n_pages)) return L2KV_ERR_SHAPE;
+    RowsArgs a = {};
+    a.Q = static_cast<const char*>(Q), a.K = static_cast<const char*>(Kc), a.V = static_cast<const char*>(Vc), a.O = static_cast<char*>(O);
+    a.q_off = q_offsets, a.kv_lens = kv_lens;
+    a.page_table = page_table, a.max_pages = max_pages, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
+    // a sequence may have more rows than there are slots where its pages repeat; what its entries hold bounds it
+    a.most_rows = static_cast<int64_t>(max_pages) * page_size;
+    a.kv_head_stride = static_cast<int64_t>(n_pages) * page_size * D;
+    a.total_rows = a.most_rows;
+    a.total_q = total_q, a.q_stride = q_stride, a.n_seq = n_seq, a.Hkv = Hkv;
+    return rows_attn(a, dt, Hq, D, max_kv, scale, workspace, workspace_bytes, kRowsPaged, stream);
 }
 
 l2kv_status l2kv_tree_attn(const void* Q, const void* Kc, const void* Vc, const void* Kt, const void* Vt, l2kv_dtype dt,
@@ -584,7 +675,7 @@ l2kv_status l2kv_tree_attn(const void* Q, const void* Kc, const void* Vc, const 
     a.q_off = node_offsets, a.kv_off = slot_offsets, a.kv_lens = lens, a.mask = mask;
     a.total_q = total_nodes, a.total_rows = total_slots, a.kv_head_stride = kv_head_stride, a.q_stride = q_stride;
     a.n_seq = n_seq, a.Hkv = Hkv, a.mask_words = mask_words;
-    return rows_attn(a, dt, Hq, D, max_len, scale, workspace, workspace_bytes, true, stream);
+    return rows_attn(a, dt, Hq, D, max_len, scale, workspace, workspace_bytes, kRowsTree, stream);
 }
 
 l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t,
@@ -607,6 +698,100 @@ l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float*
         return L2KV_ERR_ALIGN;
     return append_path_dispatch(Kt, Vt, norms_t, pos_t, dt, n_planes, n_seq, D, total_nodes, node_offsets, path, max_path, path_lens,
                                 slot_offsets, total_slots, lens_in, lens_out, Kc, Vc, norms_c, pos_c, static_cast<hipStream_t>(stream));
+}
+
+/* ---- pages ------------------------------------------------------------------ */
+
+constexpr int32_t kMaxPagedSeq = 65535;
+
+l2kv_status l2kv_pages_init(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t* refs, int32_t* free_pages,
+                            int32_t* free_count, int32_t n_pages, void* stream) {
+    if (page_table == nullptr || refs == nullptr || free_pages == nullptr || free_count == nullptr) return L2KV_ERR_NULL;
+    if (!pages_ok(n_seq, max_pages, 16, n_pages) || n_seq > kMaxPagedSeq) return L2KV_ERR_SHAPE;
+    if (!aligned(page_table, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4)) return L2KV_ERR_ALIGN;
+    return pages_init_dispatch(PagesArgs{page_table, refs, free_pages, free_count, n_seq, max_pages, n_pages, 4}, static_cast<hipStream_t>(stream));
+}
+
+l2kv_status l2kv_pages_fork(const int32_t* table_in, const int32_t* lens_in, int32_t n_in, const int32_t* parents,
+                            int32_t n_out, int32_t max_pages, int32_t page_size, int32_t n_pages, int32_t* table_out,
+                            int32_t* lens_out, int32_t* refs, void* stream) {
+    if (table_in == nullptr || lens_in == nullptr || parents == nullptr || table_out == nullptr || lens_out == nullptr || refs == nullptr)
+        return L2KV_ERR_NULL;
+    if (!pages_ok(n_in, max_pages, page_size, n_pages) || !pages_ok(n_out, max_pages, page_size, n_pages) || n_in > kMaxPagedSeq ||
+        n_out > kMaxPagedSeq || table_in == table_out || lens_in == lens_out || parents == lens_out)
+        return L2KV_ERR_SHAPE;
+    if (!aligned(table_in, 4) || !aligned(lens_in, 4) || !aligned(parents, 4) || !aligned(table_out, 4) || !aligned(lens_out, 4) || !aligned(refs, 4))
+        return L2KV_ERR_ALIGN;
+    const PagesArgs out = {table_out, refs, nullptr, nullptr, n_out, max_pages, n_pages, page_shift_of(page_size)};
+    return pages_fork_dispatch(table_in, lens_in, n_in, parents, out, lens_out, static_cast<hipStream_t>(stream));
+}
+
+size_t l2kv_pages_workspace_bytes(int64_t n_pages) { return n_pages <= 0 || n_pages > kMaxTokens / 16 ? 0 : pages_workspace_bytes(n_pages); }
+
+l2kv_status l2kv_pages_reserve(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t page_size,
+                               const int32_t* from, const int32_t* to, int32_t* ends, int32_t* refs, int32_t* free_pages,
+                               int32_t* free_count, int32_t n_pages, l2kv_dtype dt, int32_t n_planes, int32_t D, void* Kc,
+                               void* Vc, float* norms_c, int32_t* pos_c, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    if (page_table == nullptr || from == nullptr || to == nullptr || ends == nullptr || refs == nullptr || free_pages == nullptr ||
+        free_count == nullptr || Kc == nullptr || Vc == nullptr || norms_c == nullptr || pos_c == nullptr)
+        return L2KV_ERR_NULL;
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || n_seq > kMaxPagedSeq || n_planes <= 0 || !dim_ok(D, dt) || from == ends || to == ends)
+        return L2KV_ERR_SHAPE;
+    if (workspace == nullptr || workspace_bytes < pages_workspace_bytes(n_pages)) return L2KV_ERR_WORKSPACE;
+    if (!aligned(page_table, 4) || !aligned(from, 4) || !aligned(to, 4) || !aligned(ends, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) ||
+        !aligned(free_count, 4) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(workspace, 16))
+        return L2KV_ERR_ALIGN;
+    const PagesArgs a = {page_table, refs, free_pages, free_count, n_seq, max_pages, n_pages, page_shift_of(page_size)};
+    return pages_reserve_dispatch(a, from, to, ends, dt, n_planes, D, Kc, Vc, norms_c, pos_c, workspace, static_cast<hipStream_t>(stream));
+}
+
+l2kv_status l2kv_pages_release(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t page_size,
+                               const int32_t* keep_lens, int32_t* refs, int32_t* free_pages, int32_t* free_count,
+                               int32_t n_pages, void* workspace, size_t workspace_bytes, void* stream) {
+    if (page_table == nullptr || keep_lens == nullptr || refs == nullptr || free_pages == nullptr || free_count == nullptr) return L2KV_ERR_NULL;
+    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || n_seq > kMaxPagedSeq) return L2KV_ERR_SHAPE;
+    if (workspace == nullptr || workspace_bytes < pages_workspace_bytes(n_pages)) return L2KV_ERR_WORKSPACE;
+    if (!aligned(page_table, 4) || !aligned(keep_lens, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4) ||
+        !aligned(workspace, 16))
+        return L2KV_ERR_ALIGN;
+    const PagesArgs a = {page_table, refs, free_pages, free_count, n_seq, max_pages, n_pages, page_shift_of(page_size)};
+    return pages_release_dispatch(a, keep_lens, workspace, static_cast<hipStream_t>(stream));
+}
+
+static bool paged_compress_ok(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
+    return n_planes > 0 && n_seq > 0 && n_seq <= kMaxPagedSeq && n_planes <= kMaxHeads / n_seq && total_rows > 0 && total_rows <= kMaxTokens &&
+           total_kept > 0 && total_kept < (int64_t{1} << 29);
+}
+
+size_t l2kv_paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
+    return paged_compress_ok(n_planes, n_seq, total_rows, total_kept) ? paged_compress_workspace_bytes(n_planes, n_seq, total_rows, total_kept) : 0;
+}
+
+l2kv_status l2kv_paged_compress(void* Kc, void* Vc, float* norms_c, int32_t* pos_c, l2kv_dtype dt, int32_t n_planes,
+                                int32_t n_seq, int32_t D, int32_t page_size, int32_t n_pages, const int32_t* table_in,
+                                int32_t max_in, const int32_t* lens_in, const int32_t* keep, const int32_t* table_out,
+                                int32_t max_out, int32_t* lens_out, int64_t total_rows, int64_t total_kept,
+                                int64_t max_len, void* workspace, size_t workspace_bytes, void* stream) {
+    if (Kc == nullptr || Vc == nullptr || norms_c == nullptr || pos_c == nullptr || table_in == nullptr || lens_in == nullptr ||
+        keep == nullptr || table_out == nullptr || lens_out == nullptr)
+        return L2KV_ERR_NULL;
+    if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
+    if (!pages_ok(n_seq, max_in, page_size, n_pages) || !pages_ok(n_seq, max_out, page_size, n_pages) || !dim_ok(D, dt) ||
+        !paged_compress_ok(n_planes, n_seq, total_rows, total_kept) || max_len <= 0 || max_len > total_rows || table_in == table_out ||
+        lens_out == lens_in || lens_out == keep)
+        return L2KV_ERR_SHAPE;
+    if (workspace == nullptr || workspace_bytes < paged_compress_workspace_bytes(n_planes, n_seq, total_rows, total_kept)) return L2KV_ERR_WORKSPACE;
+    if (!aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(table_in, 4) || !aligned(lens_in, 4) ||
+        !aligned(keep, 4) || !aligned(table_out, 4) || !aligned(lens_out, 4) || !aligned(workspace, 16))
+        return L2KV_ERR_ALIGN;
+    PagedCompressArgs a = {};
+    a.Kc = static_cast<char*>(Kc), a.Vc = static_cast<char*>(Vc), a.norms_c = norms_c, a.pos_c = pos_c;
+    a.table_in = table_in, a.lens_in = lens_in, a.keep = keep, a.table_out = table_out, a.lens_out = lens_out;
+    a.total_rows = total_rows, a.total_kept = total_kept, a.max_len = max_len;
+    a.n_planes = n_planes, a.n_seq = n_seq, a.max_in = max_in, a.max_out = max_out, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
+    return paged_compress_dispatch(a, dt, D, workspace, static_cast<hipStream_t>(stream));
 }
 
 /* ---- attention-loss analysis ---------------------------------------------- */

@@ -23,6 +23,12 @@ decltype(&l2kv_rotary_append) rotary_append_entry = nullptr;
 decltype(&l2kv_prompt_attn) prompt_attn_entry = nullptr;
 decltype(&l2kv_tree_attn) tree_attn_entry = nullptr;
 decltype(&l2kv_stream_append_path) append_path_entry = nullptr;
+decltype(&l2kv_paged_append) paged_append_entry = nullptr;
+decltype(&l2kv_paged_attn) paged_attn_entry = nullptr;
+decltype(&l2kv_pages_fork) pages_fork_entry = nullptr;
+decltype(&l2kv_pages_reserve) pages_reserve_entry = nullptr;
+decltype(&l2kv_pages_release) pages_release_entry = nullptr;
+decltype(&l2kv_paged_compress) paged_compress_entry = nullptr;
 
 // A plain contiguous device tensor, else nullptr.  (Subclasses of torch.Tensor take the way through Python.)
 const at::Tensor* device_tensor(PyObject* o) {
@@ -407,14 +413,268 @@ PyObject* append_path_checked(PyObject* const* args, Py_ssize_t n_args) {
     });
 }
 
+// A table of pages [n_seq, max_pages].
+struct PageTable {
+    int32_t* pages = nullptr;
+    int64_t n_seq = 0, max_pages = 0;
+};
+PageTable page_table_of(Arguments& a) {
+    const at::Tensor* const t = a.dense();
+    a.require(t != nullptr && t->dim() == 2 && t->scalar_type() == at::kInt);
+    return a.good ? PageTable{static_cast<int32_t*>(t->data_ptr()), t->size(0), t->size(1)} : PageTable{};
+}
+// Size of the pages that a cache of so many slots has, and their number.
+int64_t page_size_of(Arguments& a, int64_t slots, int64_t* n_pages) {
+    const int64_t size = a.integer();
+    a.require(size > 0 && size <= INT32_MAX && slots % size == 0);
+    *n_pages = a.good ? slots / size : 0;
+    return size;
+}
+// All planes of a cache: Kc, Vc, norms, token ids.
+struct Cache {
+    l2kv_dtype dt = L2KV_F32;
+    void *Kc = nullptr, *Vc = nullptr;
+    float* norms = nullptr;
+    int32_t* pos = nullptr;
+    int64_t planes = 0, slots = 0, D = 0;
+};
+Cache cache_of(Arguments& a) {
+    Cache c;
+    const at::Tensor* const K = a.dense();
+    a.require(K != nullptr && K->dim() == 3 && element_type(*K, &c.dt));
+    if (!a.good) return c;
+    c.Kc = K->data_ptr();
+    c.planes = K->size(0), c.slots = K->size(1), c.D = K->size(2);
+    const int64_t rows[2] = {c.planes, c.slots};
+    c.Vc = a.data<void>(K->scalar_type(), K->sizes());
+    c.norms = a.data<float>(at::kFloat, at::IntArrayRef(rows));
+    c.pos = a.data<int32_t>(at::kInt, at::IntArrayRef(rows));
+    return c;
+}
+
+// (Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size, lens_in, lens_out, q_weight, k_weight, eps,
+// layout, amplitude, stream, stream's handle)
+PyObject* paged_append_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 22) Py_RETURN_NONE;
+    Arguments a{args};
+    int64_t q_stride = 0, k_stride = 0, v_stride = 0, Hq = 0;
+    l2kv_dtype dt;
+    const at::Tensor* const Q = a.none() ? nullptr : a.tokens(&q_stride);
+    const at::Tensor *const K = a.tokens(&k_stride), *const V = a.tokens(&v_stride);
+    if (!a.good || !element_type(*K, &dt)) Py_RETURN_NONE;
+    const auto type = K->scalar_type();
+    const int64_t total = K->size(0), Hkv = K->size(1), D = K->size(2);
+    a.require(V->sizes() == K->sizes() && V->scalar_type() == type);
+    if (Q != nullptr) {
+        Hq = Q->size(1);
+        a.require(Q->size(0) == total && Q->size(2) == D && Q->scalar_type() == type);
+    }
+    const int32_t* const positions = a.ints(total);
+    const at::Tensor* const freqs = a.dense();
+    if (!a.good || freqs->scalar_type() != at::kDouble) Py_RETURN_NONE;
+    void* Qr = nullptr;
+    if (!a.none()) {
+        if (Q == nullptr) Py_RETURN_NONE;
+        Qr = a.data<void>(type, Q->sizes());
+    }
+    const Cache c = cache_of(a);
+    a.require(c.planes == Hkv && c.D == D && c.dt == dt);
+    const at::Tensor* const offsets = a.dense();
+    const PageTable table = page_table_of(a);
+    if (!a.good || offsets->scalar_type() != at::kLong || offsets->numel() != table.n_seq + 1) Py_RETURN_NONE;
+    int64_t n_pages;
+    const int64_t size = page_size_of(a, c.slots, &n_pages);
+    const int32_t* const lens_in = a.ints(table.n_seq);
+    int32_t* const lens_out = a.none() ? nullptr : a.ints(table.n_seq);
+    const float* const q_weight = a.none() ? nullptr : a.data<float>(at::kFloat, D);
+    const float* const k_weight = a.none() ? nullptr : a.data<float>(at::kFloat, D);
+    const double eps = a.number();
+    const int64_t layout = a.integer();
+    const double amplitude = a.number();
+    a.require(all_int32({table.n_seq, table.max_pages, n_pages, Hq, Hkv, D, 2 * freqs->numel()}) &&
+              (layout == L2KV_ROTARY_HALF || layout == L2KV_ROTARY_INTERLEAVED));
+    if (!a.good) Py_RETURN_NONE;
+    const void *const q = Q == nullptr ? nullptr : Q->data_ptr(), *const k = K->data_ptr(), *const v = V->data_ptr();
+    const double* const f = static_cast<const double*>(freqs->data_ptr());
+    const int32_t rot_dim = (int32_t)(2 * freqs->numel());
+    const int64_t* const token_off = static_cast<const int64_t*>(offsets->data_ptr());
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return paged_append_entry(q, k, v, dt, total, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, q_stride, k_stride, v_stride, q_weight, k_weight, eps,
+                                  positions, f, rot_dim, (l2kv_rotary_layout)layout, amplitude, (int32_t)table.n_seq, token_off, table.pages,
+                                  (int32_t)table.max_pages, (int32_t)size, (int32_t)n_pages, lens_in, lens_out, Qr, c.Kc, c.Vc, c.norms, c.pos, s);
+    });
+}
+
+// (Q, Kc, Vc, q_offsets, page_table, page_size, kv_lens, max_kv, O, workspace, scale, stream, stream's handle)
+PyObject* paged_attn_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 13) Py_RETURN_NONE;
+    Arguments a{args};
+    int64_t q_stride = 0;
+    l2kv_dtype dt;
+    const at::Tensor* const Q = a.tokens(&q_stride);
+    if (!a.good || !element_type(*Q, &dt)) Py_RETURN_NONE;
+    const auto type = Q->scalar_type();
+    const int64_t total = Q->size(0), Hq = Q->size(1), D = Q->size(2);
+    const at::Tensor* const Kc = a.dense();
+    if (!a.good || Kc->dim() != 3 || Kc->size(2) != D || Kc->scalar_type() != type) Py_RETURN_NONE;
+    const int64_t Hkv = Kc->size(0);
+    const void* const Vc = a.data<void>(type, Kc->sizes());
+    const at::Tensor* const offsets = a.dense();
+    const PageTable table = page_table_of(a);
+    if (!a.good || offsets->scalar_type() != at::kLong || offsets->numel() != table.n_seq + 1) Py_RETURN_NONE;
+    int64_t n_pages;
+    const int64_t size = page_size_of(a, Kc->size(1), &n_pages);
+    const int32_t* const lens = a.ints(table.n_seq);
+    const int64_t max_kv = a.integer();
+    void* const O = a.data<void>(type, Q->sizes());
+    size_t bytes;
+    void* const ws = a.workspace(&bytes);
+    const double scale = a.number();
+    a.require(all_int32({table.n_seq, table.max_pages, n_pages, Hq, Hkv, D}));
+    if (!a.good) Py_RETURN_NONE;
+    const void *const q = Q->data_ptr(), *const k = Kc->data_ptr();
+    const int64_t* const q_off = static_cast<const int64_t*>(offsets->data_ptr());
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return paged_attn_entry(q, k, Vc, dt, (int32_t)table.n_seq, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, total, q_stride, q_off, table.pages,
+                                (int32_t)table.max_pages, (int32_t)size, (int32_t)n_pages, lens, max_kv, (float)scale, O, ws, bytes, s);
+    });
+}
+
+// (table_in, lens_in, parents, table_out, lens_out, refs, page_size, stream, stream's handle)
+PyObject* pages_fork_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 9) Py_RETURN_NONE;
+    Arguments a{args};
+    const PageTable in = page_table_of(a);
+    const int32_t* const lens_in = a.ints(in.n_seq);
+    const at::Tensor* const parents = a.dense();
+    const PageTable out = page_table_of(a);
+    if (!a.good || parents->scalar_type() != at::kInt || parents->numel() != out.n_seq) Py_RETURN_NONE;
+    int32_t* const lens_out = a.ints(out.n_seq);
+    const at::Tensor* const refs = a.dense();
+    const int64_t size = a.integer();
+    a.require(in.max_pages == out.max_pages && all_int32({in.n_seq, out.n_seq, in.max_pages, size}));
+    if (!a.good || refs->scalar_type() != at::kInt || refs->numel() > INT32_MAX) Py_RETURN_NONE;
+    const int32_t* const from = static_cast<const int32_t*>(parents->data_ptr());
+    int32_t* const holders = static_cast<int32_t*>(refs->data_ptr());
+    const int32_t n_pages = (int32_t)refs->numel();
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return pages_fork_entry(in.pages, lens_in, (int32_t)in.n_seq, from, (int32_t)out.n_seq, (int32_t)in.max_pages, (int32_t)size, n_pages, out.pages,
+                                lens_out, holders, s);
+    });
+}
+
+// Holders of pages and free ones.
+struct Holders {
+    int32_t *refs = nullptr, *free_pages = nullptr, *free_count = nullptr;
+    int64_t n_pages = 0;
+};
+Holders holders_of(Arguments& a) {
+    Holders h;
+    const at::Tensor* const refs = a.dense();
+    a.require(refs != nullptr && refs->scalar_type() == at::kInt && refs->numel() <= INT32_MAX);
+    if (!a.good) return h;
+    h.refs = static_cast<int32_t*>(refs->data_ptr());
+    h.n_pages = refs->numel();
+    h.free_pages = a.ints(h.n_pages);
+    h.free_count = a.ints(1);
+    return h;
+}
+
+// (page_table, first, to, ends, refs, free_pages, free_count, page_size, Kc, Vc, norms_c, pos_c, workspace, stream, stream's handle)
+PyObject* pages_reserve_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 15) Py_RETURN_NONE;
+    Arguments a{args};
+    const PageTable table = page_table_of(a);
+    const int32_t *const from = a.ints(table.n_seq), *const to = a.ints(table.n_seq);
+    int32_t* const ends = a.ints(table.n_seq);
+    const Holders h = holders_of(a);
+    const int64_t size = a.integer();
+    const Cache c = cache_of(a);
+    size_t bytes;
+    void* const ws = a.workspace(&bytes);
+    a.require(all_int32({table.n_seq, table.max_pages, size, c.planes, c.D}) && c.slots == h.n_pages * size);
+    if (!a.good) Py_RETURN_NONE;
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return pages_reserve_entry(table.pages, (int32_t)table.n_seq, (int32_t)table.max_pages, (int32_t)size, from, to, ends, h.refs, h.free_pages,
+                                   h.free_count, (int32_t)h.n_pages, c.dt, (int32_t)c.planes, (int32_t)c.D, c.Kc, c.Vc, c.norms, c.pos, ws, bytes, s);
+    });
+}
+
+// (page_table, keep_lens, refs, free_pages, free_count, page_size, workspace, stream, stream's handle)
+PyObject* pages_release_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 9) Py_RETURN_NONE;
+    Arguments a{args};
+    const PageTable table = page_table_of(a);
+    const int32_t* const keep = a.ints(table.n_seq);
+    const Holders h = holders_of(a);
+    const int64_t size = a.integer();
+    size_t bytes;
+    void* const ws = a.workspace(&bytes);
+    a.require(all_int32({table.n_seq, table.max_pages, size}));
+    if (!a.good) Py_RETURN_NONE;
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return pages_release_entry(table.pages, (int32_t)table.n_seq, (int32_t)table.max_pages, (int32_t)size, keep, h.refs, h.free_pages, h.free_count,
+                                   (int32_t)h.n_pages, ws, bytes, s);
+    });
+}
+
+// (Kc, Vc, norms_c, pos_c, table_in, lens_in, keep, table_out, lens_out, page_size, total_rows, total_kept, max_len, workspace, stream,
+// stream's handle)
+PyObject* paged_compress_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != 16) Py_RETURN_NONE;
+    Arguments a{args};
+    const Cache c = cache_of(a);
+    const PageTable in = page_table_of(a);
+    const int32_t *const lens_in = a.ints(in.n_seq), *const keep = a.ints(in.n_seq);
+    const PageTable out = page_table_of(a);
+    int32_t* const lens_out = a.ints(in.n_seq);
+    int64_t n_pages;
+    const int64_t size = page_size_of(a, c.slots, &n_pages), rows = a.integer(), kept = a.integer(), max_len = a.integer();
+    size_t bytes;
+    void* const ws = a.workspace(&bytes);
+    a.require(out.n_seq == in.n_seq && all_int32({in.n_seq, in.max_pages, out.max_pages, n_pages, c.planes, c.D}));
+    if (!a.good) Py_RETURN_NONE;
+    void* s;
+    if (!a.stream(&s)) return nullptr;
+    return status_of([&] {
+        return paged_compress_entry(c.Kc, c.Vc, c.norms, c.pos, c.dt, (int32_t)c.planes, (int32_t)in.n_seq, (int32_t)c.D, (int32_t)size, (int32_t)n_pages,
+                                    in.pages, (int32_t)in.max_pages, lens_in, keep, out.pages, (int32_t)out.max_pages, lens_out, rows, kept, max_len, ws,
+                                    bytes, s);
+    });
+}
+
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_append_checked(a, n); }); }
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_attn_checked(a, n); }); }
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return pages_fork_checked(a, n); }); }
+PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return pages_reserve_checked(a, n); }); }
+PyObject* pages_release(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return pages_release_checked(a, n); }); }
+PyObject* paged_compress(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_compress_checked(a, n); }); }
 PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return prompt_attn_checked(a, n); }); }
 PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return tree_attn_checked(a, n); }); }
 PyObject* rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return rotary_append_checked(a, n); }); }
 PyObject* append_path(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return append_path_checked(a, n); }); }
 
 PyObject* bind(PyObject*, PyObject* args) {
-    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path;
-    if (!PyArg_ParseTuple(args, "KKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path)) return nullptr;
+    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path, append, paged, fork, reserve, release, compact;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path, &append, &paged, &fork, &reserve,
+                          &release, &compact))
+        return nullptr;
+    paged_append_entry = reinterpret_cast<decltype(paged_append_entry)>(append);
+    paged_attn_entry = reinterpret_cast<decltype(paged_attn_entry)>(paged);
+    pages_fork_entry = reinterpret_cast<decltype(pages_fork_entry)>(fork);
+    pages_reserve_entry = reinterpret_cast<decltype(pages_reserve_entry)>(reserve);
+    pages_release_entry = reinterpret_cast<decltype(pages_release_entry)>(release);
+    paged_compress_entry = reinterpret_cast<decltype(paged_compress_entry)>(compact);
     rotary_append_entry = reinterpret_cast<decltype(rotary_append_entry)>(rotary);
     prompt_attn_entry = reinterpret_cast<decltype(prompt_attn_entry)>(prompt);
     tree_attn_entry = reinterpret_cast<decltype(tree_attn_entry)>(tree);
@@ -434,6 +694,12 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"prompt_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prompt_attn)), METH_FASTCALL, nullptr},
                          {"tree_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_attn)), METH_FASTCALL, nullptr},
                          {"append_path", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_path)), METH_FASTCALL, nullptr},
+                         {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+                         {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attn)), METH_FASTCALL, nullptr},
+                         {"pages_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_fork)), METH_FASTCALL, nullptr},
+                         {"pages_reserve", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_reserve)), METH_FASTCALL, nullptr},
+                         {"pages_release", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_release)), METH_FASTCALL, nullptr},
+                         {"paged_compress", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_compress)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "l2kv_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -163,12 +163,44 @@ struct RotaryArgs {
     int64_t total_tokens, total_slots, q_stride, k_stride, v_stride;      // strides of tokens, in elements
     double amplitude;
     int32_t n_seq, Hq, Hkv, rot, tokens_per_block;
+    // weights of the norm of queries and of keys (NULL: none), and the pages that slots are found by (NULL: slot_off)
+    const float *q_weight, *k_weight;
+    const int32_t* page_table;
+    double eps;
+    int32_t max_pages, n_pages, page_shift;
 };
 l2kv_status rotary_dispatch(RotaryArgs args, l2kv_dtype dt, int32_t D, bool interleaved, hipStream_t stream);
 
 // Attention of many query rows (rows_attn.hip).
 RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree);
-l2kv_status rows_attn_dispatch(RowsArgs args, const RowsPlan& plan, int32_t D, l2kv_dtype dt, bool tree, hipStream_t stream);
+l2kv_status rows_attn_dispatch(RowsArgs args, const RowsPlan& plan, int32_t D, l2kv_dtype dt, RowsKind kind, hipStream_t stream);
+
+// Pages of a cache (pages.hip).
+struct PagesArgs {
+    int32_t* table;            // [n_seq][max_pages], -1: no page
+    int32_t *refs, *free_pages, *free_count;
+    int32_t n_seq, max_pages, n_pages, page_shift;
+};
+size_t pages_workspace_bytes(int64_t n_pages);
+l2kv_status pages_init_dispatch(const PagesArgs& args, hipStream_t stream);
+l2kv_status pages_fork_dispatch(const int32_t* table_in, const int32_t* lens_in, int32_t n_in, const int32_t* parents, const PagesArgs& out,
+                                int32_t* lens_out, hipStream_t stream);
+l2kv_status pages_reserve_dispatch(const PagesArgs& args, const int32_t* from, const int32_t* to, int32_t* ends, l2kv_dtype dt, int32_t n_planes,
+                                   int32_t D, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* workspace, hipStream_t stream);
+l2kv_status pages_release_dispatch(const PagesArgs& args, const int32_t* keep, void* workspace, hipStream_t stream);
+
+// Compaction of a cache in pages (paged_compress.hip).
+struct PagedCompressArgs {
+    char *Kc, *Vc;
+    float* norms_c;
+    int32_t* pos_c;
+    const int32_t *table_in, *lens_in, *keep, *table_out;
+    int32_t* lens_out;
+    int64_t total_rows, total_kept, max_len;
+    int32_t n_planes, n_seq, max_in, max_out, n_pages, page_shift;
+};
+size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept);
+l2kv_status paged_compress_dispatch(const PagedCompressArgs& args, l2kv_dtype dt, int32_t D, void* workspace, hipStream_t stream);
 
 // The accepted path of a drafted tree (append_path.hip).
 l2kv_status append_path_dispatch(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t, l2kv_dtype dt,

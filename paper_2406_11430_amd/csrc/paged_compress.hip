@@ -1,0 +1,216 @@
+// Compaction of a cache in pages: of every plane and sequence the rows with the lowest (norm bits, row), in the order of the rows, into the
+// pages of another table (arXiv 2406.11430, Sec. 1: keep the lowest-norm keys and their values).
+//
+// Norms are gathered from their pages into one line per plane (4 bytes a row beside the 2 * row bytes of each kept one), the selection of ragged
+// batches works on that line, and the kept rows are copied from page to page, 16 bytes a lane, with norms and token ids.  Source and
+// destination are other pages, so rows that several sequences share are only read, and nothing has to be read before it is written over.
+#include "l2kv_device.hpp"
+#include "l2kv_host.hpp"
+
+namespace l2kv {
+namespace {
+
+constexpr int kPcThreads = 256, kPcWaves = kPcThreads / kWaveSize, kPcScan = 1024;
+constexpr int kPcUnroll = 4;
+template <int kRowBytes> constexpr int kPcRowsPerBlock = kPcWaves * RowCopy<kRowBytes>::kRowsPerWave * kPcUnroll;
+
+struct CompressScratch {
+    int64_t *in_off, *out_off;             // [n_seq + 1]
+    float* norms;                          // [n_planes][total_rows]
+    int32_t* kept;                         // [n_planes][total_kept]
+    __host__ __device__ CompressScratch(void* workspace, int64_t n_planes, int64_t n_seq, int64_t total_rows) {
+        in_off = static_cast<int64_t*>(workspace);
+        out_off = in_off + n_seq + 1;
+        norms = reinterpret_cast<float*>(out_off + n_seq + 1);
+        kept = reinterpret_cast<int32_t*>(norms + n_planes * total_rows);
+    }
+};
+
+// Rows and kept rows of a sequence, as far as lengths, bounds and pages go.
+struct Rows { int64_t have, keep; };
+__device__ __forceinline__ Rows rows_of(const PagedCompressArgs& a, int64_t s) {
+    int64_t have = a.lens_in[s], keep = a.keep[s];
+    const int64_t room = (int64_t)a.max_in << a.page_shift, to = (int64_t)a.max_out << a.page_shift;
+    have = have < room ? have : room;
+    have = have < a.max_len ? have : a.max_len;
+    have = have < 0 ? 0 : have;
+    keep = keep < have ? keep : have;
+    keep = keep < to ? keep : to;
+    return Rows{have, keep < 0 ? 0 : keep};
+}
+
+// Where the rows of the sequences begin in a line, and the kept ones; what goes beyond the lines' ends is left out.  One workgroup.
+__global__ __launch_bounds__(kPcScan)
+void compress_offsets_kernel(const PagedCompressArgs a, CompressScratch w) {
+    __shared__ int64_t waves[2][kPcScan / kWaveSize];
+    const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
+    int64_t rows = 0, kept = 0;
+    for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPcScan) {
+        const int32_t s = s0 + (int32_t)threadIdx.x;
+        Rows r = {0, 0};
+        if (s < a.n_seq) r = rows_of(a, s);
+        int64_t have = r.have, keep = r.keep;
+#pragma unroll
+        for (int d = 1; d < kWaveSize; d *= 2) {
+            const int64_t h = __shfl_up(have, d), k = __shfl_up(keep, d);
+            have += lane >= d ? h : 0;
+            keep += lane >= d ? k : 0;
+        }
+        if (lane == kWaveSize - 1) waves[0][wave] = have, waves[1][wave] = keep;
+        __syncthreads();
+        int64_t before[2] = {rows, kept};
+        for (int i = 0; i < kPcScan / kWaveSize; ++i) {
+            if (i < wave) before[0] += waves[0][i], before[1] += waves[1][i];
+            rows += waves[0][i], kept += waves[1][i];
+        }
+        const int64_t first = before[0] + have - r.have, out = before[1] + keep - r.keep;
+        if (s < a.n_seq) {
+            const int64_t end = first + r.have < a.total_rows ? first + r.have : a.total_rows;
+            const int64_t held = end > first ? end - first : 0, room = a.total_kept - out;
+            int64_t k = r.keep < held ? r.keep : held;
+            k = k < room ? k : room;
+            k = k < 0 ? 0 : k;
+            // past the end of the line nothing is kept, of this sequence and of those behind it
+            w.in_off[s] = first < a.total_rows ? first : a.total_rows;
+            w.out_off[s] = out < a.total_kept ? out : a.total_kept;
+            a.lens_out[s] = (int32_t)k;
+            if (s == a.n_seq - 1) {
+                w.in_off[s + 1] = end > first ? end : (first < a.total_rows ? first : a.total_rows);
+                w.out_off[s + 1] = out + r.keep < a.total_kept ? out + r.keep : a.total_kept;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The last sequence that begins at or before j, 64 candidates a step; j the same in all lanes.
+__device__ __forceinline__ int32_t sequence_at(const int64_t* off, int32_t n_seq, int64_t j, int lane) {
+    int32_t lo = 0, count = n_seq;
+    while (count > 1) {
+        const int32_t step = (count + kWaveSize - 1) / kWaveSize;
+        const bool at_or_before = (int64_t)lane * step < count && off[lo + (int64_t)lane * step < n_seq ? lo + lane * step : n_seq - 1] <= j;
+        const uint64_t found = __ballot(at_or_before);
+        const int32_t last = found == 0 ? 0 : 63 - __builtin_clzll(found);
+        lo += last * step;
+        count = count - last * step < step ? count - last * step : step;
+    }
+    return lo;
+}
+// The same for j of this lane, from a sequence that begins at or before it.
+__device__ __forceinline__ int32_t sequence_from(const int64_t* off, int32_t n_seq, int32_t s, int64_t j) {
+    int32_t lo = s, hi = n_seq;                                    // off[lo] <= j, and off[hi] > j where hi < n_seq
+    while (hi - lo > 1) {
+        const int32_t mid = lo + (hi - lo) / 2;
+        if (off[mid] <= j) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ int64_t slot_of(const int32_t* table, int32_t max_pages, int32_t seq, int64_t row, int32_t shift, int32_t n_pages) {
+    int32_t p = table[(int64_t)seq * max_pages + (row >> shift)];
+    p = p < 0 ? 0 : (p < n_pages ? p : n_pages - 1);
+    return ((int64_t)p << shift) + (row & ((1 << shift) - 1));
+}
+
+// Grid (256 rows, planes): norms from their pages into the line.
+__global__ __launch_bounds__(kPcThreads)
+void compress_gather_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
+    const int lane = threadIdx.x % kWaveSize;
+    const int64_t plane = first_plane + blockIdx.y, base = (int64_t)blockIdx.x * kPcThreads + threadIdx.x - lane, j = base + lane;
+    const int64_t end = w.in_off[a.n_seq];
+    if (base >= end) return;
+    const int32_t s = sequence_from(w.in_off, a.n_seq, sequence_at(w.in_off, a.n_seq, base, lane), j < end ? j : end - 1);
+    if (j >= end) return;
+    const int64_t slots = (int64_t)a.n_pages << a.page_shift;
+    w.norms[plane * a.total_rows + j] = a.norms_c[plane * slots + slot_of(a.table_in, a.max_in, s, j - w.in_off[s], a.page_shift, a.n_pages)];
+}
+
+// Grid (chunks of kept rows, alternately of K and of V, x planes), as compact_ragged_kernel.
+template <int kRowBytes>
+__global__ __launch_bounds__(kPcThreads)
+void compress_copy_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
+    using P = RowCopy<kRowBytes>;
+    const bool is_v = blockIdx.x % 2 != 0;
+    const int64_t plane = first_plane + blockIdx.y, slots = (int64_t)a.n_pages << a.page_shift;
+    const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize, c = lane % P::kLanes, rg = lane / P::kLanes;
+    const int64_t end = w.out_off[a.n_seq];
+    const int64_t wave_first = (int64_t)(blockIdx.x / 2) * kPcRowsPerBlock<kRowBytes> + wave * (P::kRowsPerWave * kPcUnroll);
+    if (wave_first >= end) return;
+    const int32_t s0 = sequence_at(w.out_off, a.n_seq, wave_first, lane);
+    int64_t src[kPcUnroll], dst[kPcUnroll];
+    bool live[kPcUnroll];
+#pragma unroll
+    for (int u = 0; u < kPcUnroll; ++u) {
+        const int64_t at = wave_first + u * P::kRowsPerWave + rg, j = at < end ? at : end - 1;
+        const int32_t s = sequence_from(w.out_off, a.n_seq, s0, j);
+        const int64_t out = j - w.out_off[s];
+        live[u] = at < end && out < a.lens_out[s];
+        int64_t row = w.kept[plane * a.total_kept + j];
+        const int64_t have = w.in_off[s + 1] - w.in_off[s];
+        row = row < have ? row : have - 1;                         // inside the sequence whatever is there
+        row = row < 0 ? 0 : row;
+        src[u] = plane * slots + slot_of(a.table_in, a.max_in, s, row, a.page_shift, a.n_pages);
+        const int32_t page = a.table_out[(int64_t)s * a.max_out + (live[u] ? out >> a.page_shift : 0)];
+        live[u] = live[u] && page >= 0 && page < a.n_pages;        // nothing is written where there is no page
+        dst[u] = plane * slots + ((int64_t)(live[u] ? page : 0) << a.page_shift) + (out & ((1 << a.page_shift) - 1));
+    }
+    char* const rows = is_v ? a.Vc : a.Kc;
+    Words<P::kWords> x[kPcUnroll];
+#pragma unroll
+    for (int u = 0; u < kPcUnroll; ++u) x[u] = load_words_stream<P::kWords, P::kStride>(rows + src[u] * kRowBytes + c * 16);
+    float norm[kPcUnroll] = {};
+    int32_t pos[kPcUnroll] = {};
+    if (!is_v && c == 0) {
+#pragma unroll
+        for (int u = 0; u < kPcUnroll; ++u) norm[u] = a.norms_c[src[u]], pos[u] = a.pos_c[src[u]];
+    }
+#pragma unroll
+    for (int u = 0; u < kPcUnroll; ++u) {
+        if (!live[u]) continue;
+        store_words_stream<P::kWords, P::kStride>(rows + dst[u] * kRowBytes + c * 16, x[u]);
+        if (!is_v && c == 0) {
+            a.norms_c[dst[u]] = norm[u];
+            a.pos_c[dst[u]] = pos[u];
+        }
+    }
+}
+
+}  // namespace
+
+size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
+    return (size_t)(16 * (n_seq + 1) + 4 * n_planes * (total_rows + total_kept));
+}
+
+l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, int32_t D, void* workspace, hipStream_t stream) {
+    const CompressScratch w(workspace, a.n_planes, a.n_seq, a.total_rows);
+    hipLaunchKernelGGL(compress_offsets_kernel, dim3(1), dim3(kPcScan), 0, stream, a, w);
+    if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+    constexpr int64_t kMaxY = 65535;
+    const unsigned gather = (unsigned)((a.total_rows + kPcThreads - 1) / kPcThreads);
+    for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
+        const unsigned planes = (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY);
+        hipLaunchKernelGGL(compress_gather_kernel, dim3(gather, planes), dim3(kPcThreads), 0, stream, a, w, p0);
+        if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+    }
+    if (l2kv_status st = select_ragged_dispatch(w.norms, a.n_planes, a.n_seq, a.total_rows, w.in_off, w.out_off, a.total_kept, a.max_len,
+                                                L2KV_KEEP_LOWEST, w.kept, stream);
+        st != L2KV_OK)
+        return st;
+    const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
+    const int64_t per_block = row_bytes == 128 ? kPcRowsPerBlock<128> : kPcRowsPerBlock<256>;
+    static_assert(kPcRowsPerBlock<256> == kPcRowsPerBlock<512>, "one chunk size for rows of 16 lanes");
+    const unsigned chunks = (unsigned)((a.total_kept + per_block - 1) / per_block);
+    for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
+        const dim3 grid(2 * chunks, (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY));
+        switch (row_bytes) {
+            case 128: hipLaunchKernelGGL((compress_copy_kernel<128>), grid, dim3(kPcThreads), 0, stream, a, w, p0); break;
+            case 256: hipLaunchKernelGGL((compress_copy_kernel<256>), grid, dim3(kPcThreads), 0, stream, a, w, p0); break;
+            default: hipLaunchKernelGGL((compress_copy_kernel<512>), grid, dim3(kPcThreads), 0, stream, a, w, p0); break;
+        }
+        if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+    }
+    return L2KV_OK;
+}
+
+}  // namespace l2kv

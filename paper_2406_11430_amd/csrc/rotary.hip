@@ -31,8 +31,8 @@ constexpr int kRotRows = 96;
 constexpr int64_t kNoSlot = -1, kNoSequence = -2;
 
 // Slot of token t: its place among its sequence's tokens behind the occupied slots; kNoSlot where they are full, kNoSequence for a token
-// that no sequence has.  For a wave, t the same in all lanes.
-__device__ __forceinline__ int64_t token_slot(const RotaryArgs& a, int64_t t, int lane) {
+// that no sequence has.  For a wave, t the same in all lanes.  kMore: there may be pages.
+template <bool kMore> __device__ __forceinline__ int64_t token_slot(const RotaryArgs& a, int64_t t, int lane) {
     if (a.token_off == nullptr) return t;
     int32_t lo = 0, count = a.n_seq;
     while (count > 1) {                                            // the last sequence that starts at or before t, 64 candidates a step
@@ -45,11 +45,53 @@ __device__ __forceinline__ int64_t token_slot(const RotaryArgs& a, int64_t t, in
         lo += last * step;
         count = left < step ? left : step;
     }
-    const Range tokens = clamped_range(a.token_off, lo, a.total_tokens), slots = clamped_range(a.slot_off, lo, a.total_slots);
+    const Range tokens = clamped_range(a.token_off, lo, a.total_tokens);
     const int64_t at = t - tokens.first;
     if (at < 0 || at >= tokens.count) return kNoSequence;
     const int64_t have = a.lens_in[lo] < 0 ? 0 : a.lens_in[lo];
+    if constexpr (kMore) {
+        if (a.page_table != nullptr) {
+            const int64_t row = have + at, index = row >> a.page_shift;
+            if (index >= a.max_pages) return kNoSlot;
+            const int32_t page = a.page_table[(int64_t)lo * a.max_pages + index];
+            return page < 0 || page >= a.n_pages ? kNoSlot : ((int64_t)page << a.page_shift) + (row & ((1 << a.page_shift) - 1));
+        }
+    }
+    const Range slots = clamped_range(a.slot_off, lo, a.total_slots);
     return have + at < slots.count ? slots.first + have + at : kNoSlot;
+}
+
+// Slots behind which a sequence's rows end after the call: as many as there is room for, and in pages only as far as there are pages.
+template <bool kMore> __device__ __forceinline__ int64_t end_of_rows(const RotaryArgs& a, int64_t s) {
+    const int64_t n = clamped_range(a.token_off, s, a.total_tokens).count, have = a.lens_in[s] < 0 ? 0 : a.lens_in[s];
+    if constexpr (kMore) {
+        if (a.page_table != nullptr) {
+            int64_t index = have >> a.page_shift;
+            for (; index < a.max_pages && index << a.page_shift < have + n; ++index) {
+                const int32_t page = a.page_table[s * a.max_pages + index];
+                if (page < 0 || page >= a.n_pages) break;
+            }
+            const int64_t room = index << a.page_shift, end = have + n < room ? have + n : room;
+            return end > have ? end : have;
+        }
+    }
+    const int64_t room = clamped_range(a.slot_off, s, a.total_slots).count, end = have + n < room ? have + n : room;
+    return end > have ? end : have;
+}
+
+// Sum over the kLanes (4, 8 or 16) consecutive lanes that share a row, in every one of them the same.
+template <int CTRL> __device__ __forceinline__ double dpp_read(double v) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int kLanes> __device__ __forceinline__ double sum_of_row(double v) {
+    v += dpp_read<kDppXor1>(v);
+    v += dpp_read<kDppXor2>(v);
+    if constexpr (kLanes >= 8) v += dpp_read<kDppHalfMirror>(v);
+    if constexpr (kLanes >= 16) v += dpp_read<kDppMirror>(v);
+    return v;
 }
 
 // 8 elements: 16 bytes of bf16, 32 of fp32.
@@ -72,7 +114,7 @@ template <typename E> __device__ __forceinline__ Piece<E> make_piece(const float
     return p;
 }
 
-template <typename E, int D, bool kInterleaved>
+template <typename E, int D, bool kInterleaved, bool kMore>
 __global__ __launch_bounds__(kRotThreads)
 void rotary_kernel(const RotaryArgs a) {
     constexpr int kLanes = D / 16, kRows = kWaveSize / kLanes;     // lanes of a row, rows of a wave
@@ -80,6 +122,7 @@ void rotary_kernel(const RotaryArgs a) {
     constexpr int kTokens = rot_tokens(kRowBytes);
     __shared__ __attribute__((aligned(16))) double angle[kTokens][D / 2][2];
     __shared__ int64_t slot_of[kTokens];
+    __shared__ __attribute__((aligned(16))) float weights[kMore ? 2 : 1][kMore ? D : 4];     // of queries, of keys
     __shared__ __attribute__((aligned(16))) char key_rows[kRotWaves][kRows * kRowBytes];
 
     const int lane = threadIdx.x % kWaveSize;
@@ -89,10 +132,7 @@ void rotary_kernel(const RotaryArgs a) {
 
     if (a.lens_out != nullptr) {
         for (int64_t s = (int64_t)blockIdx.x * kRotThreads + threadIdx.x; s < a.n_seq; s += (int64_t)gridDim.x * kRotThreads) {
-            const int64_t n = clamped_range(a.token_off, s, a.total_tokens).count, room = clamped_range(a.slot_off, s, a.total_slots).count;
-            const int64_t have = a.lens_in[s] < 0 ? 0 : a.lens_in[s];
-            const int64_t end = have + n < room ? have + n : room;
-            a.lens_out[s] = (int32_t)(end > have ? end : have);
+            a.lens_out[s] = (int32_t)end_of_rows<kMore>(a, s);
         }
     }
     const int heads = a.Hq + 2 * a.Hkv, u = lane % kLanes;
@@ -121,7 +161,7 @@ void rotary_kernel(const RotaryArgs a) {
     Place place = place_of(wave * kRows);
     if (wave * kRows < rows) load_rows(place);
     for (int t = wave; t < tokens; t += kRotWaves) {
-        const int64_t slot = token_slot(a, t0 + t, lane);
+        const int64_t slot = token_slot<kMore>(a, t0 + t, lane);
         if (lane == 0) slot_of[t] = slot;
     }
     const int pairs = a.rot / 2;
@@ -136,6 +176,12 @@ void rotary_kernel(const RotaryArgs a) {
         angle[t][f][0] = c * a.amplitude;
         angle[t][f][1] = s * a.amplitude;
     }
+    if constexpr (kMore) {
+        for (int i = threadIdx.x; i < 2 * D; i += kRotThreads) {
+            const float* const w = i < D ? a.q_weight : a.k_weight;
+            if (w != nullptr) weights[i / D][i % D] = w[i % D];
+        }
+    }
     __syncthreads();
 
     for (int first = wave * kRows; first < rows; first += kRotWaves * kRows) {
@@ -146,6 +192,28 @@ void rotary_kernel(const RotaryArgs a) {
             place = place_of(first + kRotWaves * kRows);
             load_rows(place);
         }
+        [[maybe_unused]] double root = 1.0;            // one over the root of the mean square of a row that is normed
+        const bool normed = kMore && (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr);
+        if constexpr (kMore) {
+            if (__ballot(normed) != 0) {
+                double sum = 0.0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double p = piece_element<E>(x, i), q = piece_element<E>(y, i);
+                    sum = __builtin_fma(p, p, __builtin_fma(q, q, sum));
+                }
+                sum = sum_of_row<kLanes>(sum);
+                if (normed) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + a.eps);
+            }
+        }
+        // Element i of the lane's first or second piece, as it is turned or stored.
+        [[maybe_unused]] const float* const w0 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p0 : 0);
+        [[maybe_unused]] const float* const w1 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p1 : 0);
+        auto element = [&](bool second, int i) -> double {
+            const double v = piece_element<E>(second ? y : x, i);
+            if constexpr (kMore) return normed ? v * root * (double)(second ? w1 : w0)[i] : v;
+            return v;
+        };
         if (turn) {
             float r0[8], r1[8];
 #pragma unroll
@@ -154,11 +222,11 @@ void rotary_kernel(const RotaryArgs a) {
                 const double c = angle[t][pair][0], s = angle[t][pair][1];
                 double x1, x2;
                 if constexpr (kInterleaved) {
-                    x1 = piece_element<E>(i < 4 ? x : y, 2 * i % 8);
-                    x2 = piece_element<E>(i < 4 ? x : y, 2 * i % 8 + 1);
+                    x1 = element(i >= 4, 2 * i % 8);
+                    x2 = element(i >= 4, 2 * i % 8 + 1);
                 } else {
-                    x1 = piece_element<E>(x, i);
-                    x2 = piece_element<E>(y, i);
+                    x1 = element(false, i);
+                    x2 = element(true, i);
                 }
                 const float a1 = (float)(x1 * c - x2 * s), a2 = (float)(x2 * c + x1 * s);
                 if constexpr (kInterleaved) {
@@ -168,6 +236,15 @@ void rotary_kernel(const RotaryArgs a) {
                     r0[i] = a1;
                     r1[i] = a2;
                 }
+            }
+            x = make_piece<E>(r0);
+            y = make_piece<E>(r1);
+        } else if (normed) {
+            float r0[8], r1[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                r0[i] = (float)element(false, i);
+                r1[i] = (float)element(true, i);
             }
             x = make_piece<E>(r0);
             y = make_piece<E>(r1);
@@ -226,10 +303,12 @@ l2kv_status rotary_dispatch(RotaryArgs a, l2kv_dtype dt, int32_t D, bool interle
     const int64_t blocks = (a.total_tokens + a.tokens_per_block - 1) / a.tokens_per_block;
     if (blocks > (1 << 24) - 1) return L2KV_ERR_SHAPE;             // a launch has fewer than 2^32 lanes
     const dim3 grid((unsigned)blocks);
-#define L2KV_ROT(E, D_)                                                                                     \
-    do {                                                                                                    \
-        if (interleaved) hipLaunchKernelGGL((rotary_kernel<E, D_, true>), grid, dim3(kRotThreads), 0, stream, a); \
-        else hipLaunchKernelGGL((rotary_kernel<E, D_, false>), grid, dim3(kRotThreads), 0, stream, a);       \
+    const bool more = a.q_weight != nullptr || a.k_weight != nullptr || a.page_table != nullptr;
+#define L2KV_ROT(E, D_)                                                                                                       \
+    do {                                                                                                                      \
+        auto kernel = more ? (interleaved ? rotary_kernel<E, D_, true, true> : rotary_kernel<E, D_, false, true>)             \
+                           : (interleaved ? rotary_kernel<E, D_, true, false> : rotary_kernel<E, D_, false, false>);          \
+        hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), 0, stream, a);                                                    \
     } while (0)
     if (dt == L2KV_F32) {
         if (D == 64) L2KV_ROT(F32, 64);

@@ -1,18 +1,23 @@
-// Plan and dispatch of l2kv_prompt_attn and l2kv_tree_attn (kernels in rows_attn_kernels.hpp, one translation unit per row type).
+// Plan and dispatch of l2kv_prompt_attn, l2kv_tree_attn and l2kv_paged_attn (kernels in rows_attn_kernels.hpp, one translation unit per row type).
 #include "rows_attn_kernels.hpp"
 
 namespace l2kv {
 
-extern template l2kv_status rows_attn_launch<BF16, 64, false>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 64, true>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 128, false>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 128, true>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 256, false>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<BF16, 256, true>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 64, false>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 64, true>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 128, false>(const RowsArgs&, int, hipStream_t);
-extern template l2kv_status rows_attn_launch<F32, 128, true>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 64, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 64, kRowsTree>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 64, kRowsPaged>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 128, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 128, kRowsTree>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 128, kRowsPaged>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 256, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 256, kRowsTree>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<BF16, 256, kRowsPaged>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 64, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 64, kRowsTree>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 64, kRowsPaged>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 128, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 128, kRowsTree>(const RowsArgs&, int, hipStream_t);
+extern template l2kv_status rows_attn_launch<F32, 128, kRowsPaged>(const RowsArgs&, int, hipStream_t);
 
 constexpr int kNarrowest = 2;              // of the shapes; 0 is the widest
 struct ShapeSizes { int32_t rows, keys; };
@@ -87,14 +92,17 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     return p;
 }
 
-l2kv_status rows_attn_dispatch(RowsArgs a, const RowsPlan& p, int32_t D, l2kv_dtype dt, bool tree, hipStream_t stream) {
+l2kv_status rows_attn_dispatch(RowsArgs a, const RowsPlan& p, int32_t D, l2kv_dtype dt, RowsKind kind, hipStream_t stream) {
     a.tokens_per_block = p.tokens_per_block;
     a.n_blocks = p.n_blocks;
     a.workgroups = p.workgroups < 2 ? 0 : p.workgroups;
     a.least_tiles = p.least_tiles;
     a.once = p.once;
     a.joins = reinterpret_cast<RowsJoin*>(reinterpret_cast<char*>(a.partial) + p.partial_bytes);
-#define L2KV_ROWS(E, D_) return tree ? rows_attn_launch<E, D_, true>(a, p.shape, stream) : rows_attn_launch<E, D_, false>(a, p.shape, stream)
+#define L2KV_ROWS(E, D_)                                                                 \
+    return kind == kRowsTree    ? rows_attn_launch<E, D_, kRowsTree>(a, p.shape, stream)  \
+           : kind == kRowsPaged ? rows_attn_launch<E, D_, kRowsPaged>(a, p.shape, stream) \
+                                : rows_attn_launch<E, D_, kRowsPrompt>(a, p.shape, stream)
     if (dt == L2KV_F32) {
         if (D == 64) L2KV_ROWS(F32, 64);
         L2KV_ROWS(F32, 128);

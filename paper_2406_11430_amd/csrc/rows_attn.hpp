@@ -12,6 +12,9 @@ struct RowsJoin {
     int32_t parts, rows, slot, unused;
 };
 
+// What the keys of a launch are: rows of a sequence one behind the other, the same and the nodes of a tree, or rows in pages.
+enum RowsKind : int { kRowsPrompt = 0, kRowsTree = 1, kRowsPaged = 2 };
+
 struct RowsArgs {
     const char *Q, *K, *V, *Kt, *Vt;
     char* O;
@@ -21,7 +24,9 @@ struct RowsArgs {
     const int32_t* kv_lens;
     const uint32_t* mask;
     int64_t total_q, total_rows, kv_head_stride, q_stride;      // strides in elements
-    int64_t most_rows;                                          // of a sequence: where the next head begins
+    int64_t most_rows;                                          // of a sequence: where the next head begins, or what its pages hold
+    const int32_t* page_table;                                  // [n_seq][max_pages]
+    int32_t max_pages, n_pages, page_shift;                     // a page has 1 << page_shift rows
     int32_t n_seq, Hkv, G, mask_words;
     int32_t tokens_per_block, n_blocks, workgroups, least_tiles;
     float scale;                                                // softmax scale times log2(e)

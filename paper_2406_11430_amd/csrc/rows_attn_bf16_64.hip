@@ -2,6 +2,6 @@
 #include "rows_attn_kernels.hpp"
 
 namespace l2kv {
-template l2kv_status rows_attn_launch<BF16, 64, false>(const RowsArgs&, int, hipStream_t);
-template l2kv_status rows_attn_launch<BF16, 64, true>(const RowsArgs&, int, hipStream_t);
+template l2kv_status rows_attn_launch<BF16, 64, kRowsPrompt>(const RowsArgs&, int, hipStream_t);
+template l2kv_status rows_attn_launch<BF16, 64, kRowsTree>(const RowsArgs&, int, hipStream_t);
 }  // namespace l2kv

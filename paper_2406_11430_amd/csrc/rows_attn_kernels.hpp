@@ -24,8 +24,8 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
     return (int64_t)((uint64_t)n / (uint64_t)d);
 }
 
-__device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int32_t s) {
-    const Range q = clamped_range(a.q_off, s, a.total_q), kv = clamped_range(a.kv_off, s, a.total_rows);
+template <int kKind> __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int32_t s) {
+    const Range q = clamped_range(a.q_off, s, a.total_q), kv = kKind == kRowsPaged ? Range{0, a.most_rows} : clamped_range(a.kv_off, s, a.total_rows);
     int64_t rows = kv.count < a.most_rows ? kv.count : a.most_rows;
     if (a.kv_lens != nullptr) {
         const int64_t len = a.kv_lens[s];
@@ -43,10 +43,10 @@ __device__ __forceinline__ RowsSeq uniform(const RowsSeq& q) {
 
 // Lengths of items, in keys.  A block of a prompt sees the rows up to its last token's limit; a block of a tree all cached rows and all
 // nodes, in whole tiles each.  An item counts for some tiles more than it has: what its beginning and its end take, and so that none is empty.
-template <bool kTree, int kTileKeys> struct RowsLength {
-    static constexpr int kExtra = rows_item_tiles(kTree) * kTileKeys;
+template <int kKind, int kTileKeys> struct RowsLength {
+    static constexpr int kExtra = rows_item_tiles(kKind == kRowsTree) * kTileKeys;
     static __device__ __forceinline__ int64_t keys(const RowsArgs& a, const RowsSeq& q, int64_t block) {
-        if constexpr (kTree) {
+        if constexpr (kKind == kRowsTree) {
             return (((int64_t)q.n_rows + kTileKeys - 1) / kTileKeys + ((int64_t)q.n_q + kTileKeys - 1) / kTileKeys) * kTileKeys;
         } else {
             const int64_t end = (block + 1) * a.tokens_per_block, limit = (end < q.n_q ? end : q.n_q) + q.n_rows - q.n_q;
@@ -55,7 +55,7 @@ template <bool kTree, int kTileKeys> struct RowsLength {
     }
     // of the blocks before `block`, together
     static __device__ __forceinline__ int64_t before(const RowsArgs& a, const RowsSeq& q, int64_t block) {
-        if constexpr (kTree) {
+        if constexpr (kKind == kRowsTree) {
             return block * (kExtra + keys(a, q, 0));
         } else {
             const int64_t step = a.tokens_per_block, more = (int64_t)q.n_rows - q.n_q;
@@ -97,15 +97,15 @@ template <int kTileKeys> __device__ __forceinline__ int64_t rows_stretch(const R
 
 // The stretch of this workgroup, [begin, end), and the item that it begins in; false if there is none.  A lane for each sequence, 64 at
 // a time.
-template <bool kTree, int kTileKeys>
+template <int kKind, int kTileKeys>
 __device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& it, int64_t& stretch, int64_t& end, int lane) {
-    using L = RowsLength<kTree, kTileKeys>;
+    using L = RowsLength<kKind, kTileKeys>;
     RowsSeq q = {};
     int64_t mine = 0, upto = 0, total = 0;                     // of the lane's sequence, of those up to it, of all
     int32_t s0 = 0;
     auto look = [&] {
         q = RowsSeq{};
-        if (s0 + lane < a.n_seq) q = rows_seq(a, s0 + lane);
+        if (s0 + lane < a.n_seq) q = rows_seq<kKind>(a, s0 + lane);
         mine = a.Hkv * L::before(a, q, q.blocks);
         upto = wave_prefix(mine);
     };
@@ -154,7 +154,7 @@ __device__ __forceinline__ bool rows_stretch_item(const RowsArgs& a, RowsItem& i
 // without a block behind those that have one do no harm; between them they did, as the hardware deals workgroups out in turn: a batch
 // whose every other number was empty ran on half of the device.)
 constexpr int32_t kSummedSequences = kWaveSize * kWaveSize;
-template <bool kTree, int kTileKeys>
+template <int kKind, int kTileKeys>
 __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, int lane) {
     it.head = (int32_t)(blockIdx.x % (uint32_t)a.Hkv);
     it.start = it.at = 0;
@@ -178,7 +178,7 @@ __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, i
             count = count - last * step < step ? count - last * step : step;
         }
         it.seq = __builtin_amdgcn_readfirstlane(lo);
-        it.q = uniform(rows_seq(a, it.seq));
+        it.q = uniform(rows_seq<kKind>(a, it.seq));
         block = id - (int32_t)((uint32_t)it.q.q_first / (uint32_t)a.tokens_per_block) - it.seq;
         it.block = block;
         return block >= 0 && block < it.q.blocks;
@@ -188,7 +188,7 @@ __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, i
         RowsSeq q = {};
         uint32_t mine = 0;
         if (step <= 1) {
-            if (lane < count) q = rows_seq(a, lo + lane);
+            if (lane < count) q = rows_seq<kKind>(a, lo + lane);
             mine = (uint32_t)q.blocks;
         } else {
             for (int32_t n = 0; n < step; ++n) {
@@ -224,6 +224,42 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
     }
 }
 
+// Rows of a tile that lie in pages, on their way to LDS: what stage_rows does for rows one behind the other.  Of the 1024 bytes that a
+// wave copies at a time all rows are in one page (8 rows at most, a page has 16 or more), so a page's place is the same in all lanes; the table is
+// read through the scalar cache, a tile ahead of its use.  A number that is no page's is forced into them.
+template <typename E, int D, int kRows, int kWaves> struct TilePages {
+    using R = AttnRow<E, D>;
+    static constexpr int kRowsPerChunk = 1024 / R::kBytes, kChunks = kRows / kRowsPerChunk / kWaves;
+    typedef const __attribute__((address_space(4))) int32_t table_t;      // not written while the kernel runs
+    int32_t page[kChunks];
+
+    // First row of a wave's n-th chunk; of one behind the end the last.
+    static __device__ __forceinline__ int32_t first_row(int64_t k0, int32_t rows, int n, int wave) {
+        const int64_t r = k0 + (n * kWaves + wave) * kRowsPerChunk;
+        return r < rows ? (int32_t)r : rows - 1;
+    }
+    __device__ __forceinline__ void ask(const RowsArgs& a, int32_t seq, int64_t k0, int32_t rows, int wave) {
+        if (rows <= 0) return;
+        table_t* const table = (table_t*)(uintptr_t)(a.page_table + (int64_t)seq * a.max_pages);
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) page[n] = table[first_row(k0, rows, n, wave) >> a.page_shift];
+    }
+    template <bool kIsV, bool kOnce>
+    __device__ __forceinline__ void stage(const RowsArgs& a, const char* base, int64_t k0, int32_t rows, uint32_t lds, int wave, int lane) {
+        constexpr int kLanesPerRow = R::kPieces;
+        if constexpr (R::kBytes == 512) asm volatile("" : "+v"(lane));     // as in stage_rows
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            const int32_t first = first_row(k0, rows, n, wave), left = rows - 1 - first;
+            const int32_t p = page[n] < 0 ? 0 : (page[n] < a.n_pages ? page[n] : a.n_pages - 1);
+            const int64_t slot = ((int64_t)p << a.page_shift) + (first & ((1 << a.page_shift) - 1));
+            const int chunk = n * kWaves + wave, own = lane / kLanesPerRow, r = chunk * kRowsPerChunk + own;
+            const int piece = (lane % kLanesPerRow) ^ (kIsV ? R::v_swizzle(r) : R::k_swizzle(r));
+            load_to_lds<kOnce>(base + slot * R::kBytes, (uint32_t)((own < left ? own : left) * R::kBytes + piece * 16), lds + chunk * 1024);
+        }
+    }
+};
+
 // kWR x kWK waves: kWR groups of 32 rows each, the keys of a tile shared among kWK waves of a group.  A tile has kWK * kNK * 32 keys;
 // kStages of them have room in LDS, all but one on their way while that one is worked on.  kOnce: cached rows are not read again soon.
 //
@@ -231,14 +267,15 @@ template <typename E> __device__ __forceinline__ void store_four(char* at, const
 // busy for 55 % of the cycles, exponentials, maxima and roundings for 46, and the clock falls as they are busier.  A prompt of 32768 tokens (32 query heads, 8 KV heads) takes 7.7 to 8.4 ms
 // from card to card, 1.05 to 1.14 PFLOP/s of the 1.37 that a large matrix product reaches.  Batches of trees are bound by memory:
 // 64 of 1 to 32 nodes over 500 to 4000 rows 119 to 121 us, 5.1 TB/s (a large copy: 4.80).
-template <typename E, int D, int kWR, int kWK, int kNK, int kStages, bool kTree, bool kOnce>
+template <typename E, int D, int kWR, int kWK, int kNK, int kStages, int kKind, bool kOnce>
 __global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {
     using R = AttnRow<E, D>;
+    constexpr bool kTree = kKind == kRowsTree, kPaged = kKind == kRowsPaged;
     constexpr int kWaves = kWR * kWK, kTileKeys = kWK * kNK * kTile, kBlockRows = kWR * kTile;
     constexpr int kHalf = kTileKeys * R::kBytes;               // bytes of a tile of K, and of one of V
     constexpr int kLoads = 2 * kHalf / 1024 / kWaves;          // of a wave, for a tile
-    using L = RowsLength<kTree, kTileKeys>;
+    using L = RowsLength<kKind, kTileKeys>;
     // Sized at the launch: the compiler takes a workgroup that fills the LDS for one wave per SIMD whatever else it is told, and spreads its
     // registers over both files, with copies between them in every tile.
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -252,11 +289,11 @@ void rows_attn_kernel(const RowsArgs a) {
     RowsItem it;
     int64_t end, stretch = 0;                                  // of this workgroup's stretch
     if (a.workgroups == 0) {
-        if (!rows_own_item<kTree, kTileKeys>(a, it, lane)) return;
+        if (!rows_own_item<kKind, kTileKeys>(a, it, lane)) return;
         end = L::kExtra + L::keys(a, it.q, it.block);
     } else {
         if (threadIdx.x == 0) a.joins[blockIdx.x].parts = 0;   // until an item begins here that ends elsewhere
-        if (!rows_stretch_item<kTree, kTileKeys>(a, it, stretch, end, lane)) return;
+        if (!rows_stretch_item<kKind, kTileKeys>(a, it, stretch, end, lane)) return;
     }
     for (int slot = 0;; slot = 1) {                            // one item after the other
         int row = wr * kTile + lane % kTile, half = lane / kTile;
@@ -285,7 +322,17 @@ void rows_attn_kernel(const RowsArgs a) {
         const char* const V = a.V + ((int64_t)it.head * a.kv_head_stride + it.q.row_first * D) * E::kBytes;
         const int64_t node_base = kTree ? ((int64_t)it.head * a.total_q + it.q.q_first) * R::kBytes : 0;
 
+        // Pages of the rows that this wave copies of a tile, asked for a tile ahead.
+        [[maybe_unused]] TilePages<E, D, kTileKeys, kWaves> pages;
+        if constexpr (kPaged) pages.ask(a, it.seq, (int64_t)first_tile * kTileKeys, it.q.n_rows, wave);
         auto stage = [&](int32_t tile, int where) {
+            if constexpr (kPaged) {
+                const int64_t k0 = (int64_t)tile * kTileKeys;
+                pages.template stage<false, kOnce>(a, K, k0, it.q.n_rows, lds_at + where, wave, lane);
+                pages.template stage<true, kOnce>(a, V, k0, it.q.n_rows, lds_at + where + kHalf, wave, lane);
+                pages.ask(a, it.seq, k0 + kTileKeys, it.q.n_rows, wave);
+                return;
+            }
             const bool nodes = kTree && tile >= row_tiles;
             const int64_t k0 = (int64_t)(nodes ? tile - row_tiles : tile) * kTileKeys;
             const int64_t rows = nodes ? it.q.n_q : it.q.n_rows;
@@ -472,7 +519,7 @@ void rows_attn_kernel(const RowsArgs a) {
             it.block = 0;
             if (++it.head == a.Hkv) {
                 it.head = 0;
-                do it.q = uniform(rows_seq(a, ++it.seq));      // one with tokens follows: the stretch does not end here
+                do it.q = uniform(rows_seq<kKind>(a, ++it.seq));      // one with tokens follows: the stretch does not end here
                 while (it.q.blocks == 0 && it.seq + 1 < a.n_seq);
             }
         }
@@ -543,7 +590,7 @@ template <> struct RowsShape<512, 0> { static constexpr int kWR = 8, kWK = 1, kN
 template <> struct RowsShape<512, 1> { static constexpr int kWR = 4, kWK = 1, kNK = 1, kStages = 2; };
 template <> struct RowsShape<512, 2> { static constexpr int kWR = 2, kWK = 2, kNK = 1, kStages = 2; };
 
-template <typename E, int D, int kShape, bool kTree>
+template <typename E, int D, int kShape, int kKind>
 l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     using S = RowsShape<AttnRow<E, D>::kBytes, kShape>;
     constexpr int kRows = S::kWR * kTile;
@@ -552,10 +599,10 @@ l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     static_assert((S::kWK - 1) * S::kWR * (D / 2 + 2) * kWaveSize * sizeof(float) <= kLds, "room for what the waves of a group join");
     const dim3 grid((unsigned)(a.workgroups == 0 ? a.n_blocks * a.Hkv : a.workgroups));
     const dim3 block(S::kWR * S::kWK * kWaveSize);
-    if (kTree && a.once)
-        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree, kTree>), grid, block, kLds, stream, a);
+    if (kKind == kRowsTree && a.once)
+        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kKind, kKind == kRowsTree>), grid, block, kLds, stream, a);
     else
-        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kTree, false>), grid, block, kLds, stream, a);
+        hipLaunchKernelGGL((rows_attn_kernel<E, D, S::kWR, S::kWK, S::kNK, S::kStages, kKind, false>), grid, block, kLds, stream, a);
     if (a.workgroups > 1) {
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
         // (of a few tokens not all rows of a block: 7 nodes take 2.8 us, the 64 rows of a block 5.8)
@@ -566,12 +613,12 @@ l2kv_status rows_attn_launch_shape(const RowsArgs& a, hipStream_t stream) {
     return launch_status();
 }
 
-template <typename E, int D, bool kTree>
+template <typename E, int D, int kKind>
 l2kv_status rows_attn_launch(const RowsArgs& a, int shape, hipStream_t stream) {
     switch (shape) {
-        case 0: return rows_attn_launch_shape<E, D, 0, kTree>(a, stream);
-        case 1: return rows_attn_launch_shape<E, D, 1, kTree>(a, stream);
-        default: return rows_attn_launch_shape<E, D, 2, kTree>(a, stream);
+        case 0: return rows_attn_launch_shape<E, D, 0, kKind>(a, stream);
+        case 1: return rows_attn_launch_shape<E, D, 1, kKind>(a, stream);
+        default: return rows_attn_launch_shape<E, D, 2, kKind>(a, stream);
     }
 }
 

@@ -1,0 +1,6 @@
+// Attention over bf16 rows of 64 elements in pages.
+#include "rows_attn_kernels.hpp"
+
+namespace l2kv {
+template l2kv_status rows_attn_launch<BF16, 64, kRowsPaged>(const RowsArgs&, int, hipStream_t);
+}  // namespace l2kv

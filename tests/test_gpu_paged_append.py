@@ -1,0 +1,202 @@
+"""Norms and rotary positions on the way into slots and into pages, against their definition in 64 bits."""
+import pytest
+import torch
+
+import paper_2406_11430_amd as l2kv
+from paged import DEV, PAGES, ints, table_of
+from test_gpu_prompt_attn import ROWS, offsets, randn, starts
+from test_gpu_rotary import cache, close, inputs, turned
+
+pytestmark = pytest.mark.gpu
+
+
+def normed(x, weight, eps):
+    y = x.double()
+    return y if weight is None else y / torch.sqrt(y.square().mean(-1, keepdim=True) + eps) * weight.double()
+
+
+def weights(seed, D):
+    w = 1 + 0.3 * randn(torch.Generator(device=DEV).manual_seed(seed), 2, D)
+    return w[0].contiguous(), w[1].contiguous()
+
+
+def test_append_is_the_same_without_weights():
+    Q, K, V = inputs(1, 133, 6, 2, 128, torch.bfloat16)
+    positions, freqs = torch.arange(133, dtype=torch.int32, device=DEV), l2kv.l2kv_rotary_freqs(64).to(DEV)
+    results = []
+    for call in (lambda *x: l2kv.l2kv_rotary_append(Q, K, V, *x), lambda *x: l2kv.l2kv_norm_rotary_append(Q, K, V, None, None, 1e-6, *x)):
+        Qr, c = torch.empty_like(Q, memory_format=torch.contiguous_format), cache(2, 133, 128, torch.bfloat16)
+        call(positions, freqs, Qr, *c)
+        results.append((Qr, *c))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,D,rot", [(*row, rot) for row in ROWS for rot in (16, 48, 64, 128, 256) if rot <= row[1]])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("kinds", ["qk", "q", "k"])
+def test_prompts(dtype, D, layout, rot, kinds):
+    """Packed, straight from a projection, part of the head and all of it, of one kind of heads and both, rows of very different sizes."""
+    total, Hq, Hkv, eps = 133, 5, 2, 1e-5
+    Q, K, V = inputs(rot, total, Hq, Hkv, D, dtype)
+    size = torch.exp2((torch.arange(total, device=DEV) % 37 - 18).float())[:, None, None]
+    Q.mul_(size.to(dtype)), K.mul_(size.to(dtype))
+    K[3] = 0                                                       # a head of zeros stays one
+    qw, kw = weights(rot, D)
+    qw, kw = qw if "q" in kinds else None, kw if "k" in kinds else None
+    positions = torch.cat([torch.arange(100), torch.arange(33) * 31251 - 1000]).to(torch.int32).to(DEV)
+    freqs = l2kv.l2kv_rotary_freqs(rot, 10000.0).to(DEV)
+    Qr = torch.empty((total, Hq, D), dtype=dtype, device=DEV)
+    Kc, Vc, norms, pos = cache(Hkv, total, D, dtype)
+    l2kv.l2kv_norm_rotary_append(Q, K, V, qw, kw, eps, positions, freqs, Qr, Kc, Vc, norms, pos, layout=layout, amplitude=1.25)
+    # heads that are not normed are up to 2^18 in size: what the angle's error in 64 bits makes of them
+    far = 2.0 ** 18 * 2.0 ** -40
+    close(Qr, turned(normed(Q, qw, eps), positions, freqs, layout, 1.25), far)
+    close(Kc.transpose(0, 1), turned(normed(K, kw, eps), positions, freqs, layout, 1.25), far)
+    assert torch.equal(Vc, V.transpose(0, 1)) and torch.equal(pos, positions.expand(Hkv, total))
+    again = torch.empty_like(norms)
+    l2kv.l2kv_norms(Kc, again)
+    assert torch.equal(norms, again)                              # bit for bit the norms of the rows as stored
+
+
+def test_numbers_at_the_ends_of_fp32():
+    """Squares that fp32 cannot hold, at both ends."""
+    D = 128
+    K = torch.ones((4, 1, D), device=DEV) * torch.tensor([1e30, 3e38, 1e-30, 1e-44], device=DEV)[:, None, None]
+    w = torch.full((D,), 2.0, device=DEV)
+    Kc, Vc, norms, pos = cache(1, 4, D, torch.float32)
+    zero = torch.zeros(4, dtype=torch.int32, device=DEV)
+    l2kv.l2kv_norm_rotary_append(None, K, K, None, w, 0.0, zero, l2kv.l2kv_rotary_freqs(D).to(DEV), None, Kc, Vc, norms, pos)
+    assert torch.allclose(Kc, torch.full_like(Kc, 2.0), rtol=2.0 ** -23, atol=0)
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("new,have,room", [([1, 1, 1], [0, 7, 20], [4, 4, 4]), ([3, 0, 70, 2, 1], [2, 5, 0, 9, 4], [2, 2, 3, 1, 0])])
+def test_slots(dtype, D, new, have, room):
+    """Behind the occupied slots, as l2kv_rotary_append."""
+    total, Hq, Hkv, eps = sum(new), 2, 2, 1e-6
+    slots = [h + r for h, r in zip(have, room)]
+    Q, K, V = inputs(len(new), total, Hq, Hkv, D, dtype)
+    qw, kw = weights(1, D)
+    positions = (torch.arange(total, dtype=torch.int32) * 3).to(DEV)
+    freqs = l2kv.l2kv_rotary_freqs(D, 500000.0).to(DEV)
+    Qr = torch.empty((total, Hq, D), dtype=dtype, device=DEV)
+    Kc, Vc, norms, pos = cache(Hkv, sum(slots), D, dtype)
+    lens_in = ints(have)
+    lens_out = torch.full_like(lens_in, -1)
+    l2kv.l2kv_norm_rotary_append(Q, K, V, qw, kw, eps, positions, freqs, Qr, Kc, Vc, norms, pos, offsets(new), offsets(slots), lens_in, lens_out)
+    assert lens_out.tolist() == [h + min(n, r) for n, h, r in zip(new, have, room)]
+    close(Qr, turned(normed(Q, qw, eps), positions, freqs, 0, 1.0))
+    want = turned(normed(K, kw, eps), positions, freqs, 0, 1.0)
+    written = torch.zeros(sum(slots), dtype=torch.bool)
+    for s, (n, h, r) in enumerate(zip(new, have, room)):
+        for j in range(min(n, r)):
+            at = starts(slots)[s] + h + j
+            written[at] = True
+            close(Kc[:, at], want[starts(new)[s] + j])
+    for x in (Kc, Vc, norms, pos):
+        assert (x[:, ~written.to(DEV)] == 9).all()
+
+
+@pytest.mark.parametrize("page", PAGES)
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("new,have", [([1, 1, 1], [0, 7, 300]), ([3, 0, 270, 2, 40], [13, 5, 0, 255, 256]), ([1] * 200, [7 * i % 300 for i in range(200)]),
+                                      ([1500], [0])])
+@pytest.mark.parametrize("with_norm", [False, True])
+def test_pages(page, dtype, D, new, have, with_norm):
+    """Rows from the middle of a page on and across pages; everything else stays as it was."""
+    total, Hq, Hkv, eps = sum(new), 3, 2, 1e-6
+    rows = [h + n for h, n in zip(have, new)]
+    table, n_pages, slots = table_of(rows, page, len(new))
+    Q, K, V = inputs(len(new), total + 2, Hq, Hkv, D, dtype)       # two tokens that no sequence has
+    qw, kw = weights(2, D) if with_norm else (None, None)
+    positions = (torch.arange(total + 2, dtype=torch.int32) * 3).to(DEV)
+    freqs = l2kv.l2kv_rotary_freqs(32, 500000.0).to(DEV)
+    Qr = torch.full((total + 2, Hq, D), 9.0, dtype=dtype, device=DEV)
+    Kc, Vc, norms, pos = cache(Hkv, n_pages * page, D, dtype)
+    lens_in = ints(have)
+    lens_out = torch.full_like(lens_in, -1)
+    l2kv.l2kv_paged_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms, pos, offsets(new), ints(table), page, lens_in, lens_out, qw, kw, eps, layout=1)
+    assert lens_out.tolist() == rows
+    close(Qr[:total], turned(normed(Q, qw, eps), positions, freqs, 1, 1.0)[:total])
+    assert (Qr[total:] == 9).all()
+    to = torch.cat([x[h:] for x, h in zip(slots, have)]).to(DEV)
+    close(Kc[:, to].transpose(0, 1), turned(normed(K, kw, eps), positions, freqs, 1, 1.0)[:total])
+    assert torch.equal(Vc[:, to], V[:total].transpose(0, 1)) and torch.equal(pos[:, to], positions[:total].expand(Hkv, total))
+    rest = torch.ones(n_pages * page, dtype=torch.bool, device=DEV)
+    rest[to] = False
+    for x in (Kc, Vc, norms, pos):
+        assert (x[:, rest] == 9).all()
+    again = torch.empty_like(norms)
+    l2kv.l2kv_norms(Kc, again)
+    assert torch.equal(norms[:, to], again[:, to])
+
+
+def test_missing_pages():
+    """Tokens whose row has no page are not stored, the length ends before the first of them; queries are turned all the same."""
+    page, D, Hkv = 16, 64, 1
+    table = [[2, 3, -1, 4], [-1, 0, 1, 5], [6, 99, 7, -2], [8, 9, 10, 11]]
+    new, have = [40, 3, 30, 9], [10, 15, 0, 60]
+    Q, K, V = inputs(3, sum(new), 1, Hkv, D, torch.float32)
+    positions, freqs = torch.zeros(sum(new), dtype=torch.int32, device=DEV), l2kv.l2kv_rotary_freqs(D).to(DEV)
+    Qr = torch.empty((sum(new), 1, D), device=DEV)
+    Kc, Vc, norms, pos = cache(Hkv, 12 * page, D, torch.float32)
+    lens_out = ints([0] * 4)
+    l2kv.l2kv_paged_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms, pos, offsets(new), ints(table), page, ints(have), lens_out)
+    assert lens_out.tolist() == [32, 15, 16, 64]
+    assert torch.equal(Qr, Q)
+    b, stored = starts(new), set()
+    for s in range(4):
+        for j in range(new[s]):
+            r = have[s] + j
+            if r < 64 and 0 <= table[s][r // page] < 12:
+                at = table[s][r // page] * page + r % page
+                stored.add(at)
+                assert torch.equal(Vc[0, at], V[b[s] + j, 0])
+    rest = torch.tensor([i not in stored for i in range(12 * page)], device=DEV)
+    assert (Kc[:, rest] == 9).all() and (norms[:, rest] == 9).all() and (pos[:, rest] == 9).all()
+
+
+def test_inconsistent_arrays_stay_inside():
+    Hkv, D, page = 2, 128, 16
+    Q, K, V = inputs(2, 20, 2, Hkv, D, torch.bfloat16)
+    positions, freqs = torch.arange(20, dtype=torch.int32, device=DEV), l2kv.l2kv_rotary_freqs(D).to(DEV)
+    w = torch.ones(D, device=DEV)
+    for tokens in ([0, 30, 10], [-4, 5, 1 << 40], [9, 3, 0]):
+        for table in ([[0, 1], [2, 5]], [[-9, 1 << 30], [3, -1]]):
+            for lens in ([0, 0], [-5, 1 << 30], [31, 2147483647]):
+                Qr = torch.full((22, 2, D), 3.0, dtype=torch.bfloat16, device=DEV)
+                Kc, Vc = (torch.full((Hkv * 48 + 2, D), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+                _, _, norms, pos = cache(Hkv, 48, D, torch.bfloat16)
+                l2kv.l2kv_paged_append(Q, K, V, positions, freqs, Qr[1:21], Kc[1:-1].view(Hkv, 48, D), Vc[1:-1].view(Hkv, 48, D), norms, pos,
+                                       torch.tensor(tokens, device=DEV), ints(table), page, ints(lens), ints([0, 0]), w, w)
+                assert all((x[0] == 3).all() and (x[-1] == 3).all() for x in (Qr, Kc, Vc))
+
+
+def test_a_graph_and_another_stream():
+    total, Hq, Hkv, D, page = 301, 4, 2, 64, 16
+    Q, K, V = (x.contiguous() for x in inputs(3, total, Hq, Hkv, D, torch.float32))
+    positions, freqs = torch.arange(total, dtype=torch.int32, device=DEV), l2kv.l2kv_rotary_freqs(32).to(DEV)
+    (qw, kw), (table, n_pages, slots) = weights(5, D), table_of([200, 101], page)
+    Qr, c, off, t, lens_in, lens_out = torch.empty_like(Q), cache(Hkv, n_pages * page, D, torch.float32), offsets([200, 101]), ints(table), ints([0, 0]), ints([0, 0])
+    at = torch.cat(slots).to(DEV)
+
+    def call():
+        l2kv.l2kv_paged_append(Q, K, V, positions, freqs, Qr, *c, off, t, page, lens_in, lens_out, qw, kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    close(Qr, turned(normed(Q, qw, 1e-6), positions, freqs, 0, 1.0))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(3):
+        for x in (Q, K, V):
+            x.copy_(randn(torch.Generator(device=DEV).manual_seed(seed), *x.shape))
+        Qr.zero_(), c[0].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        close(Qr, turned(normed(Q, qw, 1e-6), positions, freqs, 0, 1.0))
+        close(c[0][:, at].transpose(0, 1), turned(normed(K, kw, 1e-6), positions, freqs, 0, 1.0))
