@@ -22,6 +22,7 @@ SOURCES = ["decode_attn_bf16_128.hip", "decode_attn_bf16_256.hip", "decode_attn_
            "stream.hip", "alr.hip", "rows_attn_bf16_128.hip", "rows_attn_bf16_256.hip", "rows_attn_bf16_64.hip",
            "rows_attn_f32_128.hip", "rows_attn_f32_64.hip", "rows_attn_paged_bf16_128.hip",
            "rows_attn_paged_bf16_256.hip", "rows_attn_paged_bf16_64.hip", "rows_attn_paged_f32_128.hip", "rows_attn_paged_f32_64.hip",
+           "token_attn_bf16_128.hip", "token_attn_bf16_256.hip", "token_attn_bf16_64.hip", "token_attn_f32_128.hip", "token_attn_f32_64.hip",
            "rows_attn.hip", "rotary.hip", "append_path.hip", "pages.hip", "paged_compress.hip"]
 ARCH = "gfx950"
 

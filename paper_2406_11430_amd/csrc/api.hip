@@ -579,24 +579,24 @@ static bool rows_sizes_ok(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_
     return (total_q / 4 + n_seq) <= ((int64_t{1} << 24) - 1) / Hkv;
 }
 
-static size_t rows_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree) {
+static size_t rows_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, RowsKind kind) {
     if (!rows_sizes_ok(n_seq, Hq, Hkv, total_q, max_kv, D, dt)) return 0;
-    return rows_plan(n_seq, Hkv, Hq / Hkv, total_q, max_kv, D, dt, tree).bytes;
+    return rows_plan(n_seq, Hkv, Hq / Hkv, total_q, max_kv, D, dt, kind).bytes;
 }
 
 size_t l2kv_prompt_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
                                         l2kv_dtype dt) {
-    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt, false);
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt, kRowsPrompt);
 }
 
 size_t l2kv_tree_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_nodes, int64_t max_len, int32_t D,
                                       l2kv_dtype dt) {
-    return rows_workspace_bytes(n_seq, Hq, Hkv, total_nodes, max_len, D, dt, true);
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_nodes, max_len, D, dt, kRowsTree);
 }
 
 size_t l2kv_paged_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D,
                                        l2kv_dtype dt) {
-    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt, false);
+    return rows_workspace_bytes(n_seq, Hq, Hkv, total_q, max_kv, D, dt, kRowsPaged);
 }
 
 // The rest of the three calls, from the checks that they share to the launch.
@@ -612,7 +612,7 @@ static l2kv_status rows_attn(RowsArgs a, l2kv_dtype dt, int32_t Hq, int32_t D, i
     l2kv_status st = check_token_stride(a.q_stride, a.total_q, Hq, D, dt);
     if (st == L2KV_ERR_SHAPE) return st;
     a.G = Hq / a.Hkv;
-    const RowsPlan plan = rows_plan(a.n_seq, a.Hkv, a.G, a.total_q, max_kv, D, dt, tree);
+    const RowsPlan plan = rows_plan(a.n_seq, a.Hkv, a.G, a.total_q, max_kv, D, dt, kind);
     if (workspace_bytes < plan.bytes || (workspace == nullptr && plan.bytes > 0)) return L2KV_ERR_WORKSPACE;
     if (st != L2KV_OK || (a.kv_head_stride * elem_bytes(dt)) % 16 != 0) return L2KV_ERR_ALIGN;
     if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Kt, 16) || !aligned(a.Vt, 16) || !aligned(a.O, 16) ||

@@ -172,7 +172,7 @@ struct RotaryArgs {
 l2kv_status rotary_dispatch(RotaryArgs args, l2kv_dtype dt, int32_t D, bool interleaved, hipStream_t stream);
 
 // Attention of many query rows (rows_attn.hip).
-RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree);
+RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, RowsKind kind);
 l2kv_status rows_attn_dispatch(RowsArgs args, const RowsPlan& plan, int32_t D, l2kv_dtype dt, RowsKind kind, hipStream_t stream);
 
 // Pages of a cache (pages.hip).

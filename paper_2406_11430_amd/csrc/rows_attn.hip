@@ -1,5 +1,5 @@
 // Plan and dispatch of l2kv_prompt_attn, l2kv_tree_attn and l2kv_paged_attn (kernels in rows_attn_kernels.hpp, one translation unit per row type).
-#include "rows_attn_kernels.hpp"
+#include "token_attn_kernels.hpp"
 
 namespace l2kv {
 
@@ -19,6 +19,12 @@ extern template l2kv_status rows_attn_launch<F32, 128, kRowsPrompt>(const RowsAr
 extern template l2kv_status rows_attn_launch<F32, 128, kRowsTree>(const RowsArgs&, int, hipStream_t);
 extern template l2kv_status rows_attn_launch<F32, 128, kRowsPaged>(const RowsArgs&, int, hipStream_t);
 
+extern template l2kv_status token_attn_launch<BF16, 64>(const RowsArgs&, hipStream_t);
+extern template l2kv_status token_attn_launch<BF16, 128>(const RowsArgs&, hipStream_t);
+extern template l2kv_status token_attn_launch<BF16, 256>(const RowsArgs&, hipStream_t);
+extern template l2kv_status token_attn_launch<F32, 64>(const RowsArgs&, hipStream_t);
+extern template l2kv_status token_attn_launch<F32, 128>(const RowsArgs&, hipStream_t);
+
 constexpr int kNarrowest = 2;              // of the shapes; 0 is the widest
 struct ShapeSizes { int32_t rows, keys; };
 template <int kRowBytes, int kShape> static constexpr ShapeSizes sizes_of() {
@@ -28,6 +34,25 @@ template <int kRowBytes, int kShape> static constexpr ShapeSizes sizes_of() {
 template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
     constexpr ShapeSizes all[3] = {sizes_of<kRowBytes, 0>(), sizes_of<kRowBytes, 1>(), sizes_of<kRowBytes, 2>()};
     return all[shape];
+}
+
+// One new token a sequence, as a rule.
+constexpr int kTokens = 3;                 // the shape of such launches
+static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, int row_bytes) {
+    const int64_t units = device_compute_units(), items = total_q * Hkv;
+    const int32_t keys = row_bytes == 128 ? TokenGeometry<BF16, 64>::kBlock : TokenGeometry<BF16, 128>::kBlock;
+    RowsPlan p = {};
+    p.shape = kTokens;
+    p.tokens_per_block = 1;
+    p.n_blocks = (int32_t)(total_q + n_seq);
+    p.least_tiles = rows_item_tiles(false) + 2;
+    if (n_seq <= 1024) {
+        const int64_t most = items * (max_kv / keys + 2) / 2, wanted = 2 * units;
+        p.workgroups = (int32_t)(most < wanted ? most : wanted);
+    }
+    p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * kTokenRows * rows_partial_floats(D) * sizeof(float);
+    p.bytes = p.workgroups < 2 ? 0 : p.partial_bytes + (size_t)p.workgroups * sizeof(RowsJoin);
+    return p;
 }
 
 // Which block of rows a launch takes and whether a workgroup has an item for itself or an equal stretch of all of them.  Wide blocks read
@@ -42,7 +67,8 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
 // Over 90 sizes of all row types what this chooses took 3 % longer than the best of the six (the best single one, stretches of 128 rows: 33 %).
 // It knows the longest sequence and not the sum: a batch with one that is much longer than the others may get workgroups of their own where
 // stretches are far better (64 trees of 8 nodes, one over 131072 rows and the others over 2000: 2006 us, stretches 197).
-RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, bool tree) {
+RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, l2kv_dtype dt, RowsKind kind) {
+    const bool tree = kind == kRowsTree;
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t units = device_compute_units(), mean = (total_q + n_seq - 1) / n_seq;
     auto sizes = [&](int shape) { return row_bytes == 128 ? shape_sizes<128>(shape) : (row_bytes == 256 ? shape_sizes<256>(shape) : shape_sizes<512>(shape)); };
@@ -52,6 +78,7 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     };
     // the smallest block that takes the rows of a sequence, somewhat more than the average where there are several
     const int64_t rows = mean * G, room = n_seq == 1 ? rows : rows + rows / 4;
+    if (kind == kRowsPaged && total_q <= n_seq) return token_plan(n_seq, Hkv, total_q, max_kv, D, row_bytes);
     RowsPlan p;
     p.shape = kNarrowest;
     while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
@@ -99,6 +126,10 @@ l2kv_status rows_attn_dispatch(RowsArgs a, const RowsPlan& p, int32_t D, l2kv_dt
     a.least_tiles = p.least_tiles;
     a.once = p.once;
     a.joins = reinterpret_cast<RowsJoin*>(reinterpret_cast<char*>(a.partial) + p.partial_bytes);
+    if (p.shape == kTokens) {
+        if (dt == L2KV_F32) return D == 64 ? token_attn_launch<F32, 64>(a, stream) : token_attn_launch<F32, 128>(a, stream);
+        return D == 64 ? token_attn_launch<BF16, 64>(a, stream) : (D == 128 ? token_attn_launch<BF16, 128>(a, stream) : token_attn_launch<BF16, 256>(a, stream));
+    }
 #define L2KV_ROWS(E, D_)                                                                 \
     return kind == kRowsTree    ? rows_attn_launch<E, D_, kRowsTree>(a, p.shape, stream)  \
            : kind == kRowsPaged ? rows_attn_launch<E, D_, kRowsPaged>(a, p.shape, stream) \

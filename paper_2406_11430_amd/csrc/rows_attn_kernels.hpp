@@ -213,6 +213,20 @@ __device__ __forceinline__ bool rows_own_item(const RowsArgs& a, RowsItem& it, i
     }
 }
 
+// The item behind one that ends at item_end, from its beginning; there is one.
+template <int kKind> __device__ __forceinline__ void rows_next_item(const RowsArgs& a, RowsItem& it, int64_t item_end) {
+    it.start = item_end;
+    it.at = 0;
+    if (++it.block >= it.q.blocks) {
+        it.block = 0;
+        if (++it.head == a.Hkv) {
+            it.head = 0;
+            do it.q = uniform(rows_seq<kKind>(a, ++it.seq));       // one with tokens follows: the stretch does not end here
+            while (it.q.blocks == 0 && it.seq + 1 < a.n_seq);
+        }
+    }
+}
+
 template <typename E> __device__ __forceinline__ void store_four(char* at, const float (&v)[4]) {
     if constexpr (E::kBytes == 4) {
         *reinterpret_cast<f32x4_t*>(at) = f32x4_t{v[0], v[1], v[2], v[3]};
@@ -512,17 +526,7 @@ void rows_attn_kernel(const RowsArgs a) {
                                                tokens * a.G, slot, 0};
             return;
         }
-        // the next item, from its beginning
-        it.start = item_end;
-        it.at = 0;
-        if (++it.block >= it.q.blocks) {
-            it.block = 0;
-            if (++it.head == a.Hkv) {
-                it.head = 0;
-                do it.q = uniform(rows_seq<kKind>(a, ++it.seq));      // one with tokens follows: the stretch does not end here
-                while (it.q.blocks == 0 && it.seq + 1 < a.n_seq);
-            }
-        }
+        rows_next_item<kKind>(a, it, item_end);
         __syncthreads();                                       // before the first tile goes where this item's were
     }
 }
