@@ -36,8 +36,14 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
     return all[shape];
 }
 
-// One new token a sequence, as a rule.
+// One new token a sequence, as a rule: a workgroup for each compute unit and equal stretches, or, where the join of stretches costs more than
+// it brings, a workgroup for each (token, KV head).  us, one for each item / 128 / 256 / 512 stretches (bf16, D 128, groups of 4):
+//   1 sequence of 300 rows, 8 KV heads   8.7 /  9.9 / 10.0 / 10.0      4 of 16384                215 /  61 / 49 / 52
+//   8 of 500                            11.6 / 13.8 / 12.3 / 13.1      1 of 131072              1690 / 116 / 89 / 97
+//   64 of 700 (D 64, groups of 3)       18.2 / 32.8 / 22.9 / 20.6      64 of 500 to 4000         105 / 143 / 102 / 102
+//   1 of 8192                            109 / 17.8 / 17.0 / 19.6      256 of 500 to 700         120 / 193 / 122 / 122
 constexpr int kTokens = 3;                 // the shape of such launches
+constexpr int64_t kTokenOwnRows = 512, kTokenOwnRowsMany = 1024;
 static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, int row_bytes) {
     const int64_t units = device_compute_units(), items = total_q * Hkv;
     const int32_t keys = row_bytes == 128 ? TokenGeometry<BF16, 64>::kBlock : TokenGeometry<BF16, 128>::kBlock;
@@ -45,10 +51,11 @@ static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int64_t total_q, int64_t 
     p.shape = kTokens;
     p.tokens_per_block = 1;
     p.n_blocks = (int32_t)(total_q + n_seq);
-    p.least_tiles = rows_item_tiles(false) + 2;
-    if (n_seq <= 1024) {
-        const int64_t most = items * (max_kv / keys + 2) / 2, wanted = 2 * units;
-        p.workgroups = (int32_t)(most < wanted ? most : wanted);
+    p.least_tiles = rows_item_tiles(false) + 1;
+    // the search for a stretch's beginning goes over all sequences
+    if (n_seq <= 1024 && max_kv > (items >= 2 * units ? kTokenOwnRowsMany : kTokenOwnRows)) {
+        const int64_t most = items * (max_kv / keys + 2) / 2;
+        p.workgroups = (int32_t)(most < units ? most : units);
     }
     p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * kTokenRows * rows_partial_floats(D) * sizeof(float);
     p.bytes = p.workgroups < 2 ? 0 : p.partial_bytes + (size_t)p.workgroups * sizeof(RowsJoin);
@@ -78,7 +85,8 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     };
     // the smallest block that takes the rows of a sequence, somewhat more than the average where there are several
     const int64_t rows = mean * G, room = n_seq == 1 ? rows : rows + rows / 4;
-    if (kind == kRowsPaged && total_q <= n_seq) return token_plan(n_seq, Hkv, total_q, max_kv, D, row_bytes);
+    // (a launch has fewer than 2^32 lanes)
+    if (kind == kRowsPaged && total_q <= n_seq && (total_q + n_seq) * Hkv < (1 << 24)) return token_plan(n_seq, Hkv, total_q, max_kv, D, row_bytes);
     RowsPlan p;
     p.shape = kNarrowest;
     while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
