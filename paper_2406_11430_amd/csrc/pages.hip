@@ -6,7 +6,8 @@
 // matter, and of the entries that name one page the last is found with an atomic maximum.
 //
 // The tables are small (64 sequences of 500 pages: 128 KB) and every decision needs all those before it, so one workgroup works through them,
-// 1024 sequences and then 1024 entries at a time; the copies are a launch of their own behind it.
+// 1024 sequences and 8192 entries at a time; where that is all, as a rule, entries stay in registers.  It is bound by the
+// memory round trips that follow one another.  The copies are a launch of their own behind it.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 
@@ -32,69 +33,96 @@ struct PagesScratch {
 
 struct PagesShared {
     int32_t first[kPageThreads];           // of a sequence: index of its first entry
-    int64_t upto[kPageThreads];            // entries of the sequences up to it
-    int64_t waves[kPageWaves];
-    int64_t news[kPageThreads];            // reserving: new pages wanted up to the end of a sequence
+    int32_t upto[kPageThreads];            // entries of the sequences up to it
+    int32_t waves[kPageWaves];
+    int32_t news[kPageThreads];            // reserving: new pages wanted up to the end of a sequence
     int32_t need[kPageThreads];            // of them by itself
     bool others[kPageThreads];             // it would write a page that others hold as well
     int32_t handed;                        // new pages handed out
 };
 
-// Inclusive prefix sum over the workgroup, of numbers whose sum is below 2^31 within a wave.
-__device__ __forceinline__ int64_t block_prefix(uint32_t v, int64_t (&waves)[kPageWaves], int64_t& total) {
+// Inclusive prefix sum over the workgroup, and the sum of all; below 2^31.
+__device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t (&waves)[kPageWaves], int32_t& total) {
     const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
-    const uint32_t mine = wave_inclusive_sum(v);
+    const int32_t mine = (int32_t)wave_inclusive_sum((uint32_t)v);
     __syncthreads();                       // what was in `waves` is not read any more
     if (lane == kWaveSize - 1) waves[wave] = mine;
     __syncthreads();
-    int64_t before = 0;
-    total = 0;
-    for (int w = 0; w < kPageWaves; ++w) {
-        before += w < wave ? waves[w] : 0;
-        total += waves[w];
-    }
-    return before + mine;
+    const int32_t all = (int32_t)wave_inclusive_sum((uint32_t)waves[lane % kPageWaves]);      // of each 16 lanes' copies; the first are enough
+    total = __builtin_amdgcn_readlane(all, kPageWaves - 1);
+    return mine + (wave == 0 ? 0 : __shfl(all, wave - 1));
 }
 
-// The entries of up to 1024 sequences laid end to end.  `range` gives the first entry of a sequence and how many there are.
-template <typename F> __device__ __forceinline__ int64_t lay_out(PagesShared& sh, int32_t s0, int32_t n_seq, F&& range) {
+// Counts and numbers of pages are this workgroup's alone while it runs: atomics and loads of its own scope, which the die's L2 answers.
+__device__ __forceinline__ int32_t own_load(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void own_store(int32_t* p, int32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void own_add(int32_t* p, int32_t v) { (void)__hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void own_max(int32_t* p, int32_t v) { (void)__hip_atomic_fetch_max(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
+// The same of what this workgroup has loaded before: not from the L1, which additions by way of the L2 may have left behind.
+__device__ __forceinline__ int32_t own_load_again(int32_t* p) { return __hip_atomic_fetch_or(p, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__device__ __forceinline__ bool is_page(int32_t p, int32_t n_pages) { return p >= 0 && p < n_pages; }
+
+// kPer consecutive entries of a lane: place in the table (-1: none), sequence among the 1024 at hand, page (-1: none), whether it is its
+// sequence's last.
+constexpr int kPer = 8, kEntries = kPageThreads * kPer;
+struct Entries {
+    int32_t at[kPer], seq[kPer], page[kPer];
+    bool last[kPer];
+    __device__ __forceinline__ void load(const PagesShared& sh, const PagesArgs& a, int32_t s0, int32_t e0, int32_t total) {
+        const int32_t first = e0 + (int32_t)threadIdx.x * kPer;
+        int32_t lo = 0;                                        // the first sequence whose entries reach beyond it
+#pragma unroll
+        for (int step = kPageThreads / 2; step > 0; step /= 2) lo = sh.upto[lo + step - 1] <= first ? lo + step : lo;
+        int32_t begin = lo == 0 ? 0 : sh.upto[lo - 1], end = sh.upto[lo], index = sh.first[lo];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int32_t e = first + k;
+            at[k] = -1, page[k] = -1, seq[k] = lo, last[k] = false;
+            if (e >= total) continue;
+            while (end <= e) ++lo, begin = end, end = sh.upto[lo], index = sh.first[lo];
+            seq[k] = lo;
+            at[k] = (s0 + lo) * a.max_pages + index + (e - begin);
+            last[k] = e + 1 == end;
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (at[k] >= 0) page[k] = a.table[at[k]];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) page[k] = is_page(page[k], a.n_pages) ? page[k] : -1;
+    }
+};
+
+// The entries of up to 1024 sequences from s0 on, laid end to end; `range` gives the first entry of a sequence and how many there are.
+template <typename R> __device__ __forceinline__ int32_t lay_out(PagesShared& sh, int32_t s0, int32_t n_seq, R&& range) {
     int32_t first = 0, count = 0;
-    const int64_t s = (int64_t)s0 + threadIdx.x;
-    if (s < n_seq) range((int32_t)s, first, count);
-    int64_t total;
-    const int64_t upto = block_prefix((uint32_t)count, sh.waves, total);
+    if (const int32_t s = s0 + (int32_t)threadIdx.x; s < n_seq) range(s, first, count);
+    int32_t total;
+    const int32_t upto = block_prefix(count, sh.waves, total);
     sh.first[threadIdx.x] = first;
     sh.upto[threadIdx.x] = upto;
     __syncthreads();
     return total;
 }
-struct Entry { int32_t seq; int64_t at; bool last_of_seq; };                  // sequence among the 1024, place in the table
-__device__ __forceinline__ Entry entry_of(const PagesShared& sh, int32_t s0, int32_t max_pages, int64_t e) {
-    int32_t lo = 0;                                                       // the first whose entries reach beyond e
-#pragma unroll
-    for (int step = kPageThreads / 2; step > 0; step /= 2) lo = sh.upto[lo + step - 1] <= e ? lo + step : lo;
-    const int64_t before = lo == 0 ? 0 : sh.upto[lo - 1];
-    return Entry{lo, (int64_t)(s0 + lo) * max_pages + sh.first[lo] + (e - before), e + 1 == sh.upto[lo]};
-}
-__device__ __forceinline__ bool is_page(int32_t p, int32_t n_pages) { return p >= 0 && p < n_pages; }
 
-template <typename T> __device__ __forceinline__ T device_load(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void device_store(int32_t* p, int32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ int32_t device_add(int32_t* p, int32_t v) { return __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
-// Runs `visit` for every entry that `range` gives, all lanes together (an entry that is not there: e = -1).
+// Runs `visit` over all entries that `range` gives, all lanes together, kEntries at a time.  Where all of them are kept in registers from
+// one visit to the next (`kept`), nothing is read again.
 template <typename R, typename F>
-__device__ __forceinline__ void for_entries(PagesShared& sh, const PagesArgs& a, R&& range, F&& visit) {
-    for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
-        const int64_t total = lay_out(sh, s0, a.n_seq, range);
-        for (int64_t e0 = 0; e0 < total; e0 += kPageThreads) {
-            const int64_t e = e0 + threadIdx.x;
-            Entry x = {0, -1, false};
-            if (e < total) x = entry_of(sh, s0, a.max_pages, e);
-            visit(s0, x);
+__device__ __forceinline__ void for_entries(PagesShared& sh, const PagesArgs& a, bool kept, Entries& x, R&& range, F&& visit) {
+    if (kept) {
+        visit(x);
+    } else {
+        for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
+            const int32_t total = lay_out(sh, s0, a.n_seq, range);
+            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
+                x.load(sh, a, s0, e0, total);
+                visit(x);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
+    __syncthreads();
 }
 
 __global__ __launch_bounds__(kForkThreads)
@@ -125,7 +153,7 @@ void pages_fork_kernel(const int32_t* __restrict__ table_in, const int32_t* __re
             if (!is_page(page, a.n_pages)) page = -1;
         }
         a.table[e] = page;
-        if (page >= 0) device_add(a.refs + page, 1);
+        if (page >= 0) (void)__hip_atomic_fetch_add(a.refs + page, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (i == 0) lens_out[s] = len;
     }
 }
@@ -137,88 +165,148 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
                           void* workspace) {
     __shared__ PagesShared sh;
     const PagesScratch w(workspace, a.n_pages);
+    int32_t have = *a.free_count;
     auto range = [&](int32_t s, int32_t& first, int32_t& count) {
         const int64_t b = from[s], e = to[s];
         if (b < 0 || e <= b || e > (int64_t)a.max_pages << a.page_shift) return;
         first = (int32_t)(b >> a.page_shift);
         count = (int32_t)((e - 1) >> a.page_shift) - first + 1;
     };
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-        if (!is_page(p, a.n_pages)) return;
-        device_store(w.left + p, device_load(a.refs + p));           // the same whoever does it
-        device_store(w.last + p, -1);
+    Entries x;
+    int32_t total = lay_out(sh, 0, a.n_seq, range);
+    const bool kept = a.n_seq <= kPageThreads && total <= kEntries;
+    if (kept) x.load(sh, a, 0, 0, total);
+    // Pages that have one holder are that entry's own: nothing has to be counted for them (the same entry twice in a table has two).
+    bool shared = false;
+    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+        int32_t refs[kPer];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) refs[k] = x.page[k] < 0 ? 1 : own_load(a.refs + x.page[k]);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            if (x.page[k] < 0) continue;
+            shared |= refs[k] != 1;
+            own_store(w.left + x.page[k], refs[k] - 1);             // the same whoever does it: without the one who asks
+            own_store(w.last + x.page[k], -1);
+        }
     });
-    __threadfence();
-    __syncthreads();
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-        if (!is_page(p, a.n_pages)) return;
-        device_add(w.left + p, -1);
-        __hip_atomic_fetch_max(w.last + p, (int32_t)x.at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    });
-    __threadfence();
-    __syncthreads();
-    int64_t have = *a.free_count;
+    shared = __syncthreads_or(shared) != 0;
+    if (shared) {
+        for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                if (x.page[k] < 0) continue;
+                own_add(w.left + x.page[k], -1);
+                own_max(w.last + x.page[k], x.at[k]);
+            }
+        });
+    }
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
-    int64_t base = 0;                                          // new pages wanted by the sequences before these
-    if (threadIdx.x == 0) sh.handed = 0;
-    auto wants = [&](int64_t at, int32_t p) {
-        return at >= 0 && (!is_page(p, a.n_pages) || device_load(w.left + p) > 0 || device_load(w.last + p) != (int32_t)at);
+    // Which entries want a new page: those without one, and of a page's holders all but the last if all of them ask, else all.
+    auto wanted = [&](const Entries& x, bool (&want)[kPer]) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            want[k] = x.at[k] >= 0 && x.page[k] < 0;
+            if (shared && x.page[k] >= 0) want[k] = own_load(w.left + x.page[k]) >= 0 || own_load(w.last + x.page[k]) != x.at[k];
+        }
     };
+    int32_t base = 0;                                          // new pages wanted by the sequences before these
+    if (threadIdx.x == 0) sh.handed = 0;
     for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
-        const int64_t total = lay_out(sh, s0, a.n_seq, range);
+        if (!kept) total = lay_out(sh, s0, a.n_seq, range);
         sh.news[threadIdx.x] = 0;
         sh.need[threadIdx.x] = 0;
         sh.others[threadIdx.x] = false;
         __syncthreads();
         // how many are wanted up to the end of each sequence, then who gets one
-        int64_t sum = 0;
-        for (int pass = 0; pass < 2; ++pass) {
-            sum = base;
-            for (int64_t e0 = 0; e0 < total; e0 += kPageThreads) {
-                const int64_t e = e0 + threadIdx.x;
-                Entry x = {0, -1, false};
-                if (e < total) x = entry_of(sh, s0, a.max_pages, e);
-                const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-                const bool want = wants(x.at, p);
-                int64_t these;
-                const int64_t upto = sum + block_prefix(want ? 1u : 0u, sh.waves, these);
-                sum += these;
-                if (pass == 0) {
-                    if (want) __hip_atomic_fetch_add(&sh.need[x.seq], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    if (x.last_of_seq) sh.news[x.seq] = upto;
-                } else if (want && sh.news[x.seq] <= have) {
-                    const int32_t raw = a.free_pages[have - upto];
-                    const int32_t page = is_page(raw, a.n_pages) ? raw : 0;
-                    w.copies[upto - 1] = make_int2(is_page(p, a.n_pages) ? p : -1, page);
-                    if (is_page(p, a.n_pages)) device_add(a.refs + p, -1);
-                    device_store(a.refs + page, 1);
-                    a.table[x.at] = page;
-                    __hip_atomic_fetch_max(&sh.handed, (int32_t)upto, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                }
+        int32_t sum = base;
+        auto count = [&](const Entries& x, bool (&want)[kPer]) {
+            int32_t mine = 0, these;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) mine += want[k] ? 1 : 0;
+            const int32_t upto = sum + block_prefix(mine, sh.waves, these);
+            sum += these;
+            int32_t so_far = upto - mine;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                so_far += want[k] ? 1 : 0;
+                if (want[k]) (void)__hip_atomic_fetch_add(&sh.need[x.seq[k]], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                if (x.last[k]) sh.news[x.seq[k]] = so_far;
             }
-            __threadfence();
+            return upto - mine;
+        };
+        auto hand_out = [&](Entries& x, const bool (&want)[kPer], int32_t so_far) {
+            int32_t page[kPer], number[kPer], most = 0;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                so_far += want[k] ? 1 : 0;
+                number[k] = want[k] && sh.news[x.seq[k]] <= have ? so_far : 0;
+                if (number[k] > 0) page[k] = a.free_pages[have - number[k]];
+            }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                if (number[k] == 0) continue;
+                const int32_t fresh = is_page(page[k], a.n_pages) ? page[k] : 0;
+                w.copies[number[k] - 1] = make_int2(x.page[k], fresh);
+                if (x.page[k] >= 0) own_add(a.refs + x.page[k], -1);
+                own_store(a.refs + fresh, 1);
+                a.table[x.at[k]] = fresh;
+                x.page[k] = -1;                                    // not asked about below
+                most = number[k];
+            }
+            if (most > 0) (void)__hip_atomic_fetch_max(&sh.handed, most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        };
+        // The last holder of a page keeps it only if the others got their copies.
+        auto check = [&](const Entries& x) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (x.page[k] >= 0 && sh.news[x.seq[k]] > have && own_load_again(a.refs + x.page[k]) != 1) sh.others[x.seq[k]] = true;
+        };
+        bool want[kPer];
+        if (kept) {
+            wanted(x, want);
+            const int32_t before = count(x, want);
             __syncthreads();
+            hand_out(x, want, before);
+            __syncthreads();
+            if (sum > have) check(x);
+        } else {
+            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
+                x.load(sh, a, s0, e0, total);
+                wanted(x, want);
+                (void)count(x, want);
+            }
+            __syncthreads();
+            const int32_t all = sum;
+            sum = base;
+            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
+                x.load(sh, a, s0, e0, total);
+                wanted(x, want);
+                int32_t mine = 0, these;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) mine += want[k] ? 1 : 0;
+                const int32_t upto = sum + block_prefix(mine, sh.waves, these);
+                sum += these;
+                hand_out(x, want, upto - mine);
+            }
+            __syncthreads();
+            for (int32_t e0 = 0; e0 < total && all > have; e0 += kEntries) {
+                x.load(sh, a, s0, e0, total);
+                check(x);
+            }
         }
         base = sum;
-        // The last holder of a page keeps it only if the others got their copies.
-        for (int64_t e = threadIdx.x; e < total; e += kPageThreads) {
-            const Entry x = entry_of(sh, s0, a.max_pages, e);
-            const int32_t p = a.table[x.at];
-            if (sh.news[x.seq] > have && is_page(p, a.n_pages) && device_load(a.refs + p) != 1) sh.others[x.seq] = true;
-        }
         __syncthreads();
         if (const int32_t s = s0 + (int32_t)threadIdx.x; s < a.n_seq) {
-            int32_t first, count = 0;
-            range(s, first, count);
-            const bool fits = count > 0 && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
+            int32_t first, count_of = 0;
+            range(s, first, count_of);
+            const bool fits = count_of > 0 && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
             ends[s] = fits ? to[s] : from[s];
         }
         __syncthreads();
     }
     if (threadIdx.x == 0) {
-        *a.free_count = (int32_t)(have - sh.handed);
+        *a.free_count = have - sh.handed;
         *w.n_copies = sh.handed;
     }
 }
@@ -256,48 +344,73 @@ __global__ __launch_bounds__(kPageThreads)
 void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, void* workspace) {
     __shared__ PagesShared sh;
     const PagesScratch w(workspace, a.n_pages);
+    int32_t have = *a.free_count;
     auto range = [&](int32_t s, int32_t& first, int32_t& count) {
         const int64_t rows = keep[s] < 0 ? 0 : keep[s], from = (rows + (1 << a.page_shift) - 1) >> a.page_shift;
         if (from >= a.max_pages) return;
         first = (int32_t)from;
         count = a.max_pages - first;
     };
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-        if (is_page(p, a.n_pages)) device_store(w.last + p, -1);
+    Entries x;
+    const int32_t total = lay_out(sh, 0, a.n_seq, range);
+    const bool kept = a.n_seq <= kPageThreads && total <= kEntries;
+    if (kept) x.load(sh, a, 0, 0, total);
+    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (x.page[k] >= 0) own_store(w.last + x.page[k], -1);
     });
-    __threadfence();
-    __syncthreads();
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-        if (!is_page(p, a.n_pages)) return;
-        device_add(a.refs + p, -1);
-        __hip_atomic_fetch_max(w.last + p, (int32_t)x.at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            if (x.page[k] < 0) continue;
+            own_add(a.refs + x.page[k], -1);
+            own_max(w.last + x.page[k], x.at[k]);
+        }
     });
-    __threadfence();
-    __syncthreads();
-    auto freed = [&](const Entry& x, int32_t p) {
-        return x.at >= 0 && is_page(p, a.n_pages) && device_load(a.refs + p) <= 0 && device_load(w.last + p) == (int32_t)x.at;
+    // Of the entries that name a page without holders the last gives it back; the first of these on top.
+    auto freed = [&](const Entries& x, bool (&mine)[kPer]) {
+        int32_t refs[kPer], last[kPer], n = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            refs[k] = x.page[k] < 0 ? 1 : own_load(a.refs + x.page[k]);
+            last[k] = x.page[k] < 0 ? 0 : own_load(w.last + x.page[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            mine[k] = x.page[k] >= 0 && refs[k] <= 0 && last[k] == x.at[k];
+            n += mine[k] ? 1 : 0;
+        }
+        return n;
     };
-    int64_t all = 0, sum = 0;
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        int64_t these;
-        (void)block_prefix(freed(x, x.at < 0 ? -1 : a.table[x.at]) ? 1u : 0u, sh.waves, these);
-        all += these;
-    });
-    int64_t have = *a.free_count;
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
-    __syncthreads();
-    for_entries(sh, a, range, [&](int32_t, const Entry& x) {
-        const int32_t p = x.at < 0 ? -1 : a.table[x.at];
-        const bool mine = freed(x, p);
-        int64_t these;
-        const int64_t upto = sum + block_prefix(mine ? 1u : 0u, sh.waves, these);
-        sum += these;
-        if (mine && have + all - upto < a.n_pages) a.free_pages[have + all - upto] = p;       // the first on top
-        if (x.at >= 0) a.table[x.at] = -1;
-    });
-    if (threadIdx.x == 0) *a.free_count = (int32_t)(have + all < a.n_pages ? have + all : a.n_pages);
+    bool mine[kPer];
+    int32_t all = 0, sum = 0, these;
+    auto give_back = [&](const Entries& x, int32_t upto) {
+#pragma unroll
+        for (int k = kPer - 1; k >= 0; --k) {
+            if (mine[k]) {
+                if (have + all - upto < a.n_pages) a.free_pages[have + all - upto] = x.page[k];
+                --upto;
+            }
+            if (x.at[k] >= 0) a.table[x.at[k]] = -1;
+        }
+    };
+    if (kept) {
+        const int32_t upto = block_prefix(freed(x, mine), sh.waves, all);
+        give_back(x, upto);
+    } else {
+        for_entries(sh, a, false, x, range, [&](const Entries& x) {
+            (void)block_prefix(freed(x, mine), sh.waves, these);
+            all += these;
+        });
+        for_entries(sh, a, false, x, range, [&](const Entries& x) {
+            const int32_t upto = sum + block_prefix(freed(x, mine), sh.waves, these);
+            sum += these;
+            give_back(x, upto);
+        });
+    }
+    if (threadIdx.x == 0) *a.free_count = have + all < a.n_pages ? have + all : a.n_pages;
 }
 
 }  // namespace

@@ -284,3 +284,16 @@ def test_a_step_in_pages(dtype, D):
     assert int(pool.count) == 80 - sum(pages_of(k, page) for k in keep)
     pool.reserve_rows(c, keep, [k + 1 for k in keep])
     append_and_attend(3, c, keep, [1, 1, 1], positions)
+
+
+def test_few_pages_and_many_holders():
+    """Pages run out at every place of a list of branches that share their last pages, with and without others behind them."""
+    for spare in range(9):
+        p = Pool(9 + spare, 16, 1)
+        t = p.init(2, 8)
+        p.reserve(t, [0, 0], [70, 50])
+        b, lens = p.fork(t, [70, 50], [0, 0, 1, 0, 1, 1])
+        if spare % 2 == 0:
+            p.release(t, [0, 0])
+        p.reserve(b, lens, [n + 1 for n in lens])
+        p.reserve(b, lens, [n + 20 for n in lens])
