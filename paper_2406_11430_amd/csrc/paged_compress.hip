@@ -120,7 +120,8 @@ void compress_gather_kernel(const PagedCompressArgs a, CompressScratch w, int64_
     const int64_t plane = first_plane + blockIdx.y, base = (int64_t)blockIdx.x * kPcThreads + threadIdx.x - lane, j = base + lane;
     const int64_t end = w.in_off[a.n_seq];
     if (base >= end) return;
-    const int32_t s = sequence_from(w.in_off, a.n_seq, sequence_at(w.in_off, a.n_seq, base, lane), j < end ? j : end - 1);
+    int32_t s = sequence_at(w.in_off, a.n_seq, base, lane);
+    if (s + 1 < a.n_seq && w.in_off[s + 1] < base + kWaveSize) s = sequence_from(w.in_off, a.n_seq, s, j < end ? j : end - 1);
     if (j >= end) return;
     const int64_t slots = (int64_t)a.n_pages << a.page_shift;
     w.norms[plane * a.total_rows + j] = a.norms_c[plane * slots + slot_of(a.table_in, a.max_in, s, j - w.in_off[s], a.page_shift, a.n_pages)];
@@ -137,23 +138,39 @@ void compress_copy_kernel(const PagedCompressArgs a, CompressScratch w, int64_t 
     const int64_t end = w.out_off[a.n_seq];
     const int64_t wave_first = (int64_t)(blockIdx.x / 2) * kPcRowsPerBlock<kRowBytes> + wave * (P::kRowsPerWave * kPcUnroll);
     if (wave_first >= end) return;
-    const int32_t s0 = sequence_at(w.out_off, a.n_seq, wave_first, lane);
-    int64_t src[kPcUnroll], dst[kPcUnroll];
-    bool live[kPcUnroll];
+    // which rows, before it is known whose they are
+    int64_t at[kPcUnroll], row[kPcUnroll];
 #pragma unroll
     for (int u = 0; u < kPcUnroll; ++u) {
-        const int64_t at = wave_first + u * P::kRowsPerWave + rg, j = at < end ? at : end - 1;
-        const int32_t s = sequence_from(w.out_off, a.n_seq, s0, j);
-        const int64_t out = j - w.out_off[s];
-        live[u] = at < end && out < a.lens_out[s];
-        int64_t row = w.kept[plane * a.total_kept + j];
-        const int64_t have = w.in_off[s + 1] - w.in_off[s];
-        row = row < have ? row : have - 1;                         // inside the sequence whatever is there
-        row = row < 0 ? 0 : row;
-        src[u] = plane * slots + slot_of(a.table_in, a.max_in, s, row, a.page_shift, a.n_pages);
+        at[u] = wave_first + u * P::kRowsPerWave + rg;
+        row[u] = w.kept[plane * a.total_kept + (at[u] < end ? at[u] : end - 1)];
+    }
+    const int32_t s0 = sequence_at(w.out_off, a.n_seq, wave_first, lane);
+    // all rows of a wave are one sequence's as a rule
+    const bool alone = s0 + 1 >= a.n_seq || w.out_off[s0 + 1] >= wave_first + P::kRowsPerWave * kPcUnroll;
+    int64_t src[kPcUnroll], dst[kPcUnroll];
+    bool live[kPcUnroll];
+    auto place = [&](int u, int32_t s, int64_t out_first, int64_t kept, int64_t have) {
+        const int64_t out = at[u] - out_first;
+        live[u] = at[u] < end && out < kept;
+        int64_t r = row[u] < have ? row[u] : have - 1;             // inside the sequence whatever is there
+        r = r < 0 ? 0 : r;
         const int32_t page = a.table_out[(int64_t)s * a.max_out + (live[u] ? out >> a.page_shift : 0)];
+        src[u] = plane * slots + slot_of(a.table_in, a.max_in, s, r, a.page_shift, a.n_pages);
         live[u] = live[u] && page >= 0 && page < a.n_pages;        // nothing is written where there is no page
         dst[u] = plane * slots + ((int64_t)(live[u] ? page : 0) << a.page_shift) + (out & ((1 << a.page_shift) - 1));
+    };
+    if (alone) {
+        const int32_t s = __builtin_amdgcn_readfirstlane(s0);
+        const int64_t out_first = w.out_off[s], kept = a.lens_out[s], have = w.in_off[s + 1] - w.in_off[s];
+#pragma unroll
+        for (int u = 0; u < kPcUnroll; ++u) place(u, s, out_first, kept, have);
+    } else {
+#pragma unroll
+        for (int u = 0; u < kPcUnroll; ++u) {
+            const int32_t s = sequence_from(w.out_off, a.n_seq, s0, at[u] < end ? at[u] : end - 1);
+            place(u, s, w.out_off[s], a.lens_out[s], w.in_off[s + 1] - w.in_off[s]);
+        }
     }
     char* const rows = is_v ? a.Vc : a.Kc;
     Words<P::kWords> x[kPcUnroll];
