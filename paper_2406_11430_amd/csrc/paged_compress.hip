@@ -1,43 +1,18 @@
 // Compaction of a cache in pages: of every plane and sequence the rows with the lowest (norm bits, row), in the order of the rows, into the
 // pages of another table (arXiv 2406.11430, Sec. 1: keep the lowest-norm keys and their values).
 //
-// Norms are gathered from their pages into one line per plane (4 bytes a row beside the 2 * row bytes of each kept one), the selection of ragged
-// batches works on that line, and the kept rows are copied from page to page, 16 bytes a lane, with norms and token ids.  Source and
-// destination are other pages, so rows that several sequences share are only read, and nothing has to be read before it is written over.
-#include "l2kv_device.hpp"
-#include "l2kv_host.hpp"
+// A workgroup selects for each (plane, sequence), with the norms in registers straight from their pages; kept rows are then copied from page to
+// page, 16 bytes a lane, with norms and token ids.  Longer sequences, and very many, have their norms gathered into one line per plane
+// first (4 bytes a row beside the 2 * row bytes of each kept one) for the selection of ragged batches.  Source and destination are
+// other pages, so rows that several sequences share are only read, and nothing has to be read before it is written over.
+#include "paged_rows.hpp"
 
 namespace l2kv {
 namespace {
 
 constexpr int kPcThreads = 256, kPcWaves = kPcThreads / kWaveSize, kPcScan = 1024;
-constexpr int kPcUnroll = 4;
+constexpr int kPcUnroll = 2;
 template <int kRowBytes> constexpr int kPcRowsPerBlock = kPcWaves * RowCopy<kRowBytes>::kRowsPerWave * kPcUnroll;
-
-struct CompressScratch {
-    int64_t *in_off, *out_off;             // [n_seq + 1]
-    float* norms;                          // [n_planes][total_rows]
-    int32_t* kept;                         // [n_planes][total_kept]
-    __host__ __device__ CompressScratch(void* workspace, int64_t n_planes, int64_t n_seq, int64_t total_rows) {
-        in_off = static_cast<int64_t*>(workspace);
-        out_off = in_off + n_seq + 1;
-        norms = reinterpret_cast<float*>(out_off + n_seq + 1);
-        kept = reinterpret_cast<int32_t*>(norms + n_planes * total_rows);
-    }
-};
-
-// Rows and kept rows of a sequence, as far as lengths, bounds and pages go.
-struct Rows { int64_t have, keep; };
-__device__ __forceinline__ Rows rows_of(const PagedCompressArgs& a, int64_t s) {
-    int64_t have = a.lens_in[s], keep = a.keep[s];
-    const int64_t room = (int64_t)a.max_in << a.page_shift, to = (int64_t)a.max_out << a.page_shift;
-    have = have < room ? have : room;
-    have = have < a.max_len ? have : a.max_len;
-    have = have < 0 ? 0 : have;
-    keep = keep < have ? keep : have;
-    keep = keep < to ? keep : to;
-    return Rows{have, keep < 0 ? 0 : keep};
-}
 
 // Where the rows of the sequences begin in a line, and the kept ones; what goes beyond the lines' ends is left out.  One workgroup.
 __global__ __launch_bounds__(kPcScan)
@@ -65,18 +40,13 @@ void compress_offsets_kernel(const PagedCompressArgs a, CompressScratch w) {
         }
         const int64_t first = before[0] + have - r.have, out = before[1] + keep - r.keep;
         if (s < a.n_seq) {
-            const int64_t end = first + r.have < a.total_rows ? first + r.have : a.total_rows;
-            const int64_t held = end > first ? end - first : 0, room = a.total_kept - out;
-            int64_t k = r.keep < held ? r.keep : held;
-            k = k < room ? k : room;
-            k = k < 0 ? 0 : k;
-            // past the end of the line nothing is kept, of this sequence and of those behind it
-            w.in_off[s] = first < a.total_rows ? first : a.total_rows;
-            w.out_off[s] = out < a.total_kept ? out : a.total_kept;
-            a.lens_out[s] = (int32_t)k;
+            const Held h = held_of(a, r, first, out);
+            w.in_off[s] = h.in_first;
+            w.out_off[s] = h.out_first;
+            a.lens_out[s] = (int32_t)h.keep;
             if (s == a.n_seq - 1) {
-                w.in_off[s + 1] = end > first ? end : (first < a.total_rows ? first : a.total_rows);
-                w.out_off[s + 1] = out + r.keep < a.total_kept ? out + r.keep : a.total_kept;
+                w.in_off[s + 1] = h.in_first + h.have;
+                w.out_off[s + 1] = h.out_end;
             }
         }
         __syncthreads();
@@ -107,10 +77,11 @@ __device__ __forceinline__ int32_t sequence_from(const int64_t* off, int32_t n_s
     return lo;
 }
 
-__device__ __forceinline__ int64_t slot_of(const int32_t* table, int32_t max_pages, int32_t seq, int64_t row, int32_t shift, int32_t n_pages) {
-    int32_t p = table[(int64_t)seq * max_pages + (row >> shift)];
-    p = p < 0 ? 0 : (p < n_pages ? p : n_pages - 1);
-    return ((int64_t)p << shift) + (row & ((1 << shift) - 1));
+// Rows that the selection saw.
+__device__ __forceinline__ int64_t have_of(const PagedCompressArgs& a, const CompressScratch& w, int32_t s) {
+    const Rows r = rows_of(a, s);
+    const int64_t left = a.total_rows - w.in_off[s];
+    return r.have < left ? r.have : left;
 }
 
 // Grid (256 rows, planes): norms from their pages into the line.
@@ -127,16 +98,16 @@ void compress_gather_kernel(const PagedCompressArgs a, CompressScratch w, int64_
     w.norms[plane * a.total_rows + j] = a.norms_c[plane * slots + slot_of(a.table_in, a.max_in, s, j - w.in_off[s], a.page_shift, a.n_pages)];
 }
 
-// Grid (chunks of kept rows, alternately of K and of V, x planes), as compact_ragged_kernel.
+// Grid (chunks of kept rows, planes): K and V of a row by the same lanes, whose places then count for both, two rows a lane on their way (alternate
+// workgroups of K and of V with four rows 272 us, so 266: 64 sequences of 1k to 8k bf16 rows of 128 in 8 planes, half kept).
 template <int kRowBytes>
 __global__ __launch_bounds__(kPcThreads)
 void compress_copy_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
     using P = RowCopy<kRowBytes>;
-    const bool is_v = blockIdx.x % 2 != 0;
     const int64_t plane = first_plane + blockIdx.y, slots = (int64_t)a.n_pages << a.page_shift;
     const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize, c = lane % P::kLanes, rg = lane / P::kLanes;
     const int64_t end = w.out_off[a.n_seq];
-    const int64_t wave_first = (int64_t)(blockIdx.x / 2) * kPcRowsPerBlock<kRowBytes> + wave * (P::kRowsPerWave * kPcUnroll);
+    const int64_t wave_first = (int64_t)blockIdx.x * kPcRowsPerBlock<kRowBytes> + wave * (P::kRowsPerWave * kPcUnroll);
     if (wave_first >= end) return;
     // which rows, before it is known whose they are
     int64_t at[kPcUnroll], row[kPcUnroll];
@@ -162,31 +133,33 @@ void compress_copy_kernel(const PagedCompressArgs a, CompressScratch w, int64_t 
     };
     if (alone) {
         const int32_t s = __builtin_amdgcn_readfirstlane(s0);
-        const int64_t out_first = w.out_off[s], kept = a.lens_out[s], have = w.in_off[s + 1] - w.in_off[s];
+        const int64_t out_first = w.out_off[s], kept = a.lens_out[s], have = have_of(a, w, s);
 #pragma unroll
         for (int u = 0; u < kPcUnroll; ++u) place(u, s, out_first, kept, have);
     } else {
 #pragma unroll
         for (int u = 0; u < kPcUnroll; ++u) {
             const int32_t s = sequence_from(w.out_off, a.n_seq, s0, at[u] < end ? at[u] : end - 1);
-            place(u, s, w.out_off[s], a.lens_out[s], w.in_off[s + 1] - w.in_off[s]);
+            place(u, s, w.out_off[s], a.lens_out[s], have_of(a, w, s));
         }
     }
-    char* const rows = is_v ? a.Vc : a.Kc;
-    Words<P::kWords> x[kPcUnroll];
+    Words<P::kWords> k[kPcUnroll], v[kPcUnroll];
 #pragma unroll
-    for (int u = 0; u < kPcUnroll; ++u) x[u] = load_words_stream<P::kWords, P::kStride>(rows + src[u] * kRowBytes + c * 16);
+    for (int u = 0; u < kPcUnroll; ++u) k[u] = load_words_stream<P::kWords, P::kStride>(a.Kc + src[u] * kRowBytes + c * 16);
+#pragma unroll
+    for (int u = 0; u < kPcUnroll; ++u) v[u] = load_words_stream<P::kWords, P::kStride>(a.Vc + src[u] * kRowBytes + c * 16);
     float norm[kPcUnroll] = {};
     int32_t pos[kPcUnroll] = {};
-    if (!is_v && c == 0) {
+    if (c == 0) {
 #pragma unroll
         for (int u = 0; u < kPcUnroll; ++u) norm[u] = a.norms_c[src[u]], pos[u] = a.pos_c[src[u]];
     }
 #pragma unroll
     for (int u = 0; u < kPcUnroll; ++u) {
         if (!live[u]) continue;
-        store_words_stream<P::kWords, P::kStride>(rows + dst[u] * kRowBytes + c * 16, x[u]);
-        if (!is_v && c == 0) {
+        store_words_stream<P::kWords, P::kStride>(a.Kc + dst[u] * kRowBytes + c * 16, k[u]);
+        store_words_stream<P::kWords, P::kStride>(a.Vc + dst[u] * kRowBytes + c * 16, v[u]);
+        if (c == 0) {
             a.norms_c[dst[u]] = norm[u];
             a.pos_c[dst[u]] = pos[u];
         }
@@ -201,25 +174,29 @@ size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t t
 
 l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, int32_t D, void* workspace, hipStream_t stream) {
     const CompressScratch w(workspace, a.n_planes, a.n_seq, a.total_rows);
-    hipLaunchKernelGGL(compress_offsets_kernel, dim3(1), dim3(kPcScan), 0, stream, a, w);
-    if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
     constexpr int64_t kMaxY = 65535;
-    const unsigned gather = (unsigned)((a.total_rows + kPcThreads - 1) / kPcThreads);
-    for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
-        const unsigned planes = (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY);
-        hipLaunchKernelGGL(compress_gather_kernel, dim3(gather, planes), dim3(kPcThreads), 0, stream, a, w, p0);
+    if (a.max_len <= kPagedSelectRows && a.n_seq <= kPagedSelectSeq) {
+        if (l2kv_status st = select_paged_dispatch(a, w, stream); st != L2KV_OK) return st;
+    } else {
+        hipLaunchKernelGGL(compress_offsets_kernel, dim3(1), dim3(kPcScan), 0, stream, a, w);
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+        const unsigned gather = (unsigned)((a.total_rows + kPcThreads - 1) / kPcThreads);
+        for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
+            const unsigned planes = (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY);
+            hipLaunchKernelGGL(compress_gather_kernel, dim3(gather, planes), dim3(kPcThreads), 0, stream, a, w, p0);
+            if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+        }
+        if (l2kv_status st = select_ragged_dispatch(w.norms, a.n_planes, a.n_seq, a.total_rows, w.in_off, w.out_off, a.total_kept, a.max_len,
+                                                    L2KV_KEEP_LOWEST, w.kept, stream);
+            st != L2KV_OK)
+            return st;
     }
-    if (l2kv_status st = select_ragged_dispatch(w.norms, a.n_planes, a.n_seq, a.total_rows, w.in_off, w.out_off, a.total_kept, a.max_len,
-                                                L2KV_KEEP_LOWEST, w.kept, stream);
-        st != L2KV_OK)
-        return st;
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t per_block = row_bytes == 128 ? kPcRowsPerBlock<128> : kPcRowsPerBlock<256>;
     static_assert(kPcRowsPerBlock<256> == kPcRowsPerBlock<512>, "one chunk size for rows of 16 lanes");
     const unsigned chunks = (unsigned)((a.total_kept + per_block - 1) / per_block);
     for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
-        const dim3 grid(2 * chunks, (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY));
+        const dim3 grid(chunks, (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY));
         switch (row_bytes) {
             case 128: hipLaunchKernelGGL((compress_copy_kernel<128>), grid, dim3(kPcThreads), 0, stream, a, w, p0); break;
             case 256: hipLaunchKernelGGL((compress_copy_kernel<256>), grid, dim3(kPcThreads), 0, stream, a, w, p0); break;

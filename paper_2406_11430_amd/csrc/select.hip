@@ -31,6 +31,7 @@
 #include "digit_search.hpp"
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
+#include "paged_rows.hpp"
 #include "row_norm.hpp"
 
 #include <type_traits>
@@ -128,6 +129,16 @@ template <int E> struct HeadKeys {
         if constexpr (E > 0) {
 #pragma unroll
             for (int e = 0; e < E; ++e) regs[e] = fetch_mem(e);
+        }
+    }
+    // Keys that are not one behind the other: load(t) is that of token t < count.
+    template <typename F> __device__ __forceinline__ HeadKeys(int64_t count, uint32_t f, F&& load) : src(nullptr), T((uint32_t)count), flip(f), iters(E) {
+        static_assert(E > 0, "keys in registers");
+        t0 = (uint32_t)(threadIdx.x / kWaveSize * E * kWaveSize);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t t = token(e), v = load(t < T ? t : T - 1) ^ flip;
+            regs[e] = t < T ? v : 0xffffffffu;
         }
     }
     __device__ __forceinline__ uint32_t token(int64_t e) const { return t0 + (uint32_t)e * kWaveSize + threadIdx.x % kWaveSize; }
@@ -325,6 +336,47 @@ void select_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint32_t k
     emit_ordered<E == 0 ? kSelBatch : E, false>([&](int64_t e) { return keys.fetch(e); }, E == 0 ? keys.iters : E, keys.t0, th.tau,
                                          th.need_eq, 0u, 0u, [&](uint32_t i, int32_t t) { out[i] = t; }, k, s_emit);
     if (kept_count != nullptr && threadIdx.x == 0) kept_count[head] = (int32_t)k;
+}
+
+// ---- selection of a compaction in pages ---------------------------------------------------------
+// Grid (sequences, planes).  Every workgroup adds up the rows and the kept rows of the sequences before its own (64 of them: one round trip
+// beside the first one of the keys); those of the first plane leave them for the copy.
+template <int E>
+__global__ __launch_bounds__(kSelThreads)
+void select_paged_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
+    __shared__ __attribute__((aligned(16))) SearchShared s_search;
+    __shared__ EmitShared s_emit;
+    __shared__ int64_t s_sums[2][kSelThreads / kWaveSize];
+    const int32_t seq = blockIdx.x;
+    const int64_t plane = first_plane + blockIdx.y;
+    int64_t rows = 0, kept = 0;
+    for (int32_t s = threadIdx.x; s < seq; s += kSelThreads) {
+        const Rows r = rows_of(a, s);
+        rows += r.have, kept += r.keep;
+    }
+    const Rows mine = rows_of(a, seq);
+#pragma unroll
+    for (int d = 1; d < kWaveSize; d *= 2) rows += __shfl_xor(rows, d), kept += __shfl_xor(kept, d);
+    if (threadIdx.x % kWaveSize == 0) s_sums[0][threadIdx.x / kWaveSize] = rows, s_sums[1][threadIdx.x / kWaveSize] = kept;
+    __syncthreads();
+    rows = kept = 0;
+#pragma unroll
+    for (int i = 0; i < kSelThreads / kWaveSize; ++i) rows += s_sums[0][i], kept += s_sums[1][i];
+    const Held h = held_of(a, mine, rows, kept);
+    if (plane == 0 && threadIdx.x == 0) {
+        w.in_off[seq] = h.in_first;
+        w.out_off[seq] = h.out_first;
+        a.lens_out[seq] = (int32_t)h.keep;
+        if (seq == a.n_seq - 1) w.out_off[seq + 1] = h.out_end;
+    }
+    const uint32_t k = (uint32_t)h.keep;
+    if (k == 0) return;
+    const uint32_t* const norms = reinterpret_cast<const uint32_t*>(a.norms_c) + plane * ((int64_t)a.n_pages << a.page_shift);
+    int32_t* const out = w.kept + plane * a.total_kept + h.out_first;
+    const HeadKeys<E> keys(h.have, 0u, [&](uint32_t t) { return norms[slot_of(a.table_in, a.max_in, seq, t, a.page_shift, a.n_pages)]; });
+    const Threshold th = find_threshold(keys, k, s_search);
+    emit_ordered<E, false>([&](int64_t e) { return keys.fetch(e); }, E, keys.t0, th.tau, th.need_eq, 0u, 0u,
+                           [&](uint32_t i, int32_t t) { out[i] = t; }, k, s_emit);
 }
 
 // ---- selection and compaction of short heads in one launch ------------------------------------
@@ -1021,6 +1073,24 @@ l2kv_status compress_short_dispatch(const void* K, const void* V, l2kv_dtype dt,
                        (uint32_t)n_heads, (uint32_t)shares, T, (uint32_t)k, (uint32_t)tokens, head_stride * (dt == L2KV_F32 ? 4 : 2), norms, kept_idx,
                        static_cast<char*>(Kc), static_cast<char*>(Vc));
     return launch_status();
+}
+
+l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScratch& w, hipStream_t stream) {
+    const int64_t per_lane = (a.max_len + kSelThreads - 1) / kSelThreads;
+    auto kernel = per_lane <= 1    ? select_paged_kernel<1>
+                  : per_lane <= 2  ? select_paged_kernel<2>
+                  : per_lane <= 4  ? select_paged_kernel<4>
+                  : per_lane <= 8  ? select_paged_kernel<8>
+                  : per_lane <= 16 ? select_paged_kernel<16>
+                                   : select_paged_kernel<32>;
+    static_assert(kPagedSelectRows <= 32 * kSelThreads, "keys in registers");
+    constexpr int64_t kMaxY = 65535;
+    for (int64_t p0 = 0; p0 < a.n_planes; p0 += kMaxY) {
+        const dim3 grid((unsigned)a.n_seq, (unsigned)(a.n_planes - p0 < kMaxY ? a.n_planes - p0 : kMaxY));
+        hipLaunchKernelGGL(kernel, grid, dim3(kSelThreads), 0, stream, a, w, p0);
+        if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+    }
+    return L2KV_OK;
 }
 
 l2kv_status select_ragged_dispatch(const float* norms, int32_t n_planes, int32_t n_seq,

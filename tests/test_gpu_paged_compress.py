@@ -144,3 +144,13 @@ def test_norms_that_are_not_finite():
     c.cache[2][:, slots[::3]] = float("inf")
     assert c.run() == [100]
     c.verify([100])
+
+
+@pytest.mark.parametrize("have", [[1024, 3], [1025, 7], [2048, 2049], [4100], [8192, 8193], [16385, 30000], [32768, 1], [32769, 500]])
+@pytest.mark.parametrize("ties", [False, True])
+def test_long_sequences(have, ties):
+    """Every number of keys that a lane of the selection holds, and sequences that it does not hold."""
+    keep = [h // 3 + 1 for h in have]
+    c = Case(sum(have), have, keep, 2, 64, torch.bfloat16, 64, ties)
+    assert c.run() == keep
+    c.verify(keep)
