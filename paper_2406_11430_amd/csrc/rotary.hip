@@ -122,7 +122,7 @@ void rotary_kernel(const RotaryArgs a) {
     constexpr int kTokens = rot_tokens(kRowBytes);
     __shared__ __attribute__((aligned(16))) double angle[kTokens][D / 2][2];
     __shared__ int64_t slot_of[kTokens];
-    __shared__ __attribute__((aligned(16))) float weights[kMore ? 2 : 1][kMore ? D : 4];     // of queries, of keys
+    __shared__ __attribute__((aligned(16))) double weights[kMore ? 2 : 1][kMore ? D : 2];    // of queries, of keys; ones where there are none
     __shared__ __attribute__((aligned(16))) char key_rows[kRotWaves][kRows * kRowBytes];
 
     const int lane = threadIdx.x % kWaveSize;
@@ -131,7 +131,8 @@ void rotary_kernel(const RotaryArgs a) {
     const int tokens = (int)(a.total_tokens - t0 < a.tokens_per_block ? a.total_tokens - t0 : a.tokens_per_block);
 
     if (a.lens_out != nullptr) {
-        for (int64_t s = (int64_t)blockIdx.x * kRotThreads + threadIdx.x; s < a.n_seq; s += (int64_t)gridDim.x * kRotThreads) {
+        // by the last waves: the first ones look for slots
+        for (int64_t s = (int64_t)blockIdx.x * kRotThreads + (kRotThreads - 1 - threadIdx.x); s < a.n_seq; s += (int64_t)gridDim.x * kRotThreads) {
             a.lens_out[s] = (int32_t)end_of_rows<kMore>(a, s);
         }
     }
@@ -165,7 +166,7 @@ void rotary_kernel(const RotaryArgs a) {
         if (lane == 0) slot_of[t] = slot;
     }
     const int pairs = a.rot / 2;
-    for (int i = threadIdx.x; i < tokens * pairs; i += kRotThreads) {
+    for (int i = (threadIdx.x + kRotThreads - kWaveSize) % kRotThreads; i < tokens * pairs; i += kRotThreads) {      // from the second wave on
         const int t = i / pairs, f = i - t * pairs;
         const double theta = (double)a.positions[t0 + t] * a.freqs[f];
         // less whole turns: 2 pi in two parts, so that the difference is as exact as the angle
@@ -179,7 +180,7 @@ void rotary_kernel(const RotaryArgs a) {
     if constexpr (kMore) {
         for (int i = threadIdx.x; i < 2 * D; i += kRotThreads) {
             const float* const w = i < D ? a.q_weight : a.k_weight;
-            if (w != nullptr) weights[i / D][i % D] = w[i % D];
+            weights[i / D][i % D] = w != nullptr ? (double)w[i % D] : 1.0;
         }
     }
     __syncthreads();
@@ -192,7 +193,9 @@ void rotary_kernel(const RotaryArgs a) {
             place = place_of(first + kRotWaves * kRows);
             load_rows(place);
         }
-        [[maybe_unused]] double root = 1.0;            // one over the root of the mean square of a row that is normed
+        // kMore: elements times their weight over the root of the mean square (heads that are not normed: times one), without a branch
+        // for each of them.
+        [[maybe_unused]] double root = 1.0;
         const bool normed = kMore && (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr);
         if constexpr (kMore) {
             if (__ballot(normed) != 0) {
@@ -202,16 +205,19 @@ void rotary_kernel(const RotaryArgs a) {
                     const double p = piece_element<E>(x, i), q = piece_element<E>(y, i);
                     sum = __builtin_fma(p, p, __builtin_fma(q, q, sum));
                 }
-                sum = sum_of_row<kLanes>(sum);
-                if (normed) root = 1.0 / __builtin_sqrt(sum * (1.0 / D) + a.eps);
+                const double mean = sum_of_row<kLanes>(sum) * (1.0 / D) + a.eps;
+                // The instruction is good to 2^-14 at least; each step more than doubles the bits.
+                double r = __builtin_amdgcn_rsq(mean);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) r = __builtin_fma(r * 0.5, __builtin_fma(-mean * r, r, 1.0), r);
+                root = !normed ? 1.0 : mean == __builtin_inf() ? 0.0 : r;
             }
         }
-        // Element i of the lane's first or second piece, as it is turned or stored.
-        [[maybe_unused]] const float* const w0 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p0 : 0);
-        [[maybe_unused]] const float* const w1 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p1 : 0);
+        [[maybe_unused]] const double* const w0 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p0 : 0);
+        [[maybe_unused]] const double* const w1 = weights[kMore && !is_q ? 1 : 0] + (kMore ? 8 * p1 : 0);
         auto element = [&](bool second, int i) -> double {
             const double v = piece_element<E>(second ? y : x, i);
-            if constexpr (kMore) return normed ? v * root * (double)(second ? w1 : w0)[i] : v;
+            if constexpr (kMore) return v * (second ? w1 : w0)[i] * root;
             return v;
         };
         if (turn) {

@@ -200,3 +200,21 @@ def test_a_graph_and_another_stream():
         torch.cuda.synchronize()
         close(Qr, turned(normed(Q, qw, 1e-6), positions, freqs, 0, 1.0))
         close(c[0][:, at].transpose(0, 1), turned(normed(K, kw, 1e-6), positions, freqs, 0, 1.0))
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+def test_heads_that_are_not_finite(dtype, D):
+    """An infinity makes the other elements of its head zeros and itself NaN, a NaN all of them; other heads do not see them."""
+    Q, K, V = inputs(4, 3, 1, 2, D, dtype)
+    K[0, 0, 5], K[1, 1, 7] = float("inf"), float("nan")
+    V[2, 0, 3] = float("nan")
+    w = torch.full((D,), 2.0, device=DEV)
+    Kc, Vc, norms, pos = cache(2, 3, D, dtype)
+    zero = torch.zeros(3, dtype=torch.int32, device=DEV)
+    l2kv.l2kv_norm_rotary_append(None, K, V, None, w, 1e-6, zero, l2kv.l2kv_rotary_freqs(16).to(DEV), None, Kc, Vc, norms, pos)
+    want = normed(K, w, 1e-6)
+    rest = torch.ones((3, 2), dtype=torch.bool, device=DEV)
+    rest[0, 0] = rest[1, 1] = False
+    close(Kc.transpose(0, 1)[rest], want[rest])
+    assert Kc[1, 1].isnan().all() and Kc[0, 0, 16:].eq(0).all() and Kc[0, 0, 5].isnan()
+    assert torch.equal(Vc.transpose(0, 1).view(torch.int16), V.contiguous().view(torch.int16))
