@@ -93,9 +93,19 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     const int64_t longest = max_kv + (tree ? mean : 0);            // keys of an item
     const double bytes = 2.0 * (double)max_kv * n_seq * Hkv * row_bytes;     // of K and V, at most
     bool stretches = false;
-    if (p.shape == 0 && longest >= 2048 && items(0) >= 2 * units) {
+    int64_t per_unit = 1;
+    // Chunks over rows in pages, whose lengths differ more than those of prompts.  Wide blocks where there is one for each compute unit (8 chunks of
+    // 1 to 512 tokens over 1k to 8k rows, 265 us, 246 so), and stretches of them where each has eight tiles and more: the narrowest
+    // would read K and V four times as often (2 chunks of 273 to 1062 tokens over 733 to 22124 rows, groups of 8, 749 and 463; 4 of D 256 over 14000
+    // 1585 and 704).  fp32 products take so long that two of half the width share a unit (10 of 30 to 200 over 2000 311 and 254).
+    const double tiles = (double)items(0) * ((double)longest - 0.5 * (double)(mean < longest ? mean : longest)) / sizes(0).keys / (double)units;
+    const bool chunks = kind == kRowsPaged && p.shape == 0;
+    if (p.shape == 0 && longest >= 2048 && items(0) >= (chunks && dt != L2KV_F32 ? units : 2 * units)) {
     } else if (p.shape < kNarrowest && items(1) >= 2 * units) {
         p.shape = 1;
+    } else if (chunks && tiles >= 8.0 && n_seq <= 1024) {
+        stretches = true;
+        if (dt == L2KV_F32) p.shape = 1, per_unit = 2;
     } else {
         // Of the narrowest block: the keys of the longest item, with something for two in a compute unit, against those of a stretch, with
         // 8 tiles' time for its beginning and the join.  Stretches of the widest block take 0.6 of the time for the same keys.
@@ -119,8 +129,9 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     p.least_tiles = rows_item_tiles(tree) + 2;
     p.workgroups = 0;
     if (stretches) {
-        const int64_t most = blocks * Hkv * (max_kv / s.keys + 2) / 2;
-        p.workgroups = (int32_t)(most < units ? most : units);
+        // (less four: their parts and joins then fit where those of wide ones do)
+        const int64_t most = blocks * Hkv * (max_kv / s.keys + 2) / 2, wanted = per_unit == 1 ? units : per_unit * units - 4;
+        p.workgroups = (int32_t)(most < wanted ? most : wanted);
     }
     p.partial_bytes = p.workgroups < 2 ? 0 : (size_t)p.workgroups * 2 * s.rows * rows_partial_floats(D) * sizeof(float);
     p.bytes = p.workgroups < 2 ? 0 : p.partial_bytes + (size_t)p.workgroups * sizeof(RowsJoin);

@@ -208,3 +208,14 @@ def test_streams_and_graphs():
             graph.replay()
             torch.cuda.synchronize()
             fresh.verify(O)
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("new,rows", [([300, 120], [7000, 1500]), ([700], [9000]), ([40, 1, 350, 0, 90], [6000, 5000, 350, 9, 4444])])
+@pytest.mark.parametrize("G,Hkv", [(4, 4), (2, 1)])
+def test_chunks_in_stretches(dtype, D, new, rows, G, Hkv):
+    """Few chunks over many rows: equal stretches of wide blocks, which begin and end inside of items."""
+    c = Case(17, new, rows, G * Hkv, Hkv, D, dtype, 32)
+    first = c.run()
+    c.verify(first)
+    assert torch.equal(first, c.run())
