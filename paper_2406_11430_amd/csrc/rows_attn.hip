@@ -125,8 +125,9 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     p.tokens_per_block = s.rows / G;
     const int64_t blocks = total_q / p.tokens_per_block + n_seq;
     p.n_blocks = (int32_t)blocks;
-    // Two tiles of keys and what an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 15.0 us, 17.0 with four tiles.
-    p.least_tiles = rows_item_tiles(tree) + 2;
+    // Two tiles of keys and what an item counts for by itself: 7 nodes over 2048 rows of 32 heads take 15.0 us, 17.0 with four tiles.  Chunks
+    // over pages two in all: three fp32 ones of 1 to 77 tokens over 511 to 1533 rows 22.2 us, 18.6 so.
+    p.least_tiles = kind == kRowsPaged ? 2 : rows_item_tiles(tree) + 2;
     p.workgroups = 0;
     if (stretches) {
         // (less four: their parts and joins then fit where those of wide ones do)
