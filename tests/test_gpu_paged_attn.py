@@ -97,17 +97,19 @@ def test_many_sequences(n_seq, most):
 
 @pytest.mark.parametrize("dtype,D", ROWS)
 def test_like_prompt_attention(dtype, D):
-    """Pages in the order of a plane are that plane: the same bits as l2kv_prompt_attn where the work is cut alike, queries from a projection."""
-    new, rows, page, Hkv, Hq = [30, 100], [320, 640], 32, 2, 4
+    """Pages in the order of a plane are that plane: the same bits as l2kv_prompt_attn where every item has a workgroup for itself (shares of items
+    are cut elsewhere), queries from a projection."""
+    n, page, Hkv, Hq = 300, 32, 2, 4
+    new, rows = [12 - s % 3 for s in range(n)], [64] * n
     gen = torch.Generator(device=DEV).manual_seed(1)
     K, V = (randn(gen, Hkv, sum(rows), D).to(dtype) for _ in range(2))
     Q = randn(gen, sum(new), 3 * Hq, D).to(dtype)[:, Hq:2 * Hq]
     a, b = (torch.empty((sum(new), Hq, D), dtype=dtype, device=DEV) for _ in range(2))
-    ws = torch.empty(max(1, l2kv.l2kv_prompt_attn_workspace_bytes(2, Hq, Hkv, sum(new), 640, D, dtype),
-                         l2kv.l2kv_paged_attn_workspace_bytes(2, Hq, Hkv, sum(new), 640, D, dtype)), dtype=torch.uint8, device=DEV)
-    l2kv.l2kv_prompt_attn(Q, K, V, offsets(new), offsets(rows), None, 640, a, ws, 0.3)
-    table = [list(range(10)) + [-1] * 10, list(range(10, 30))]
-    l2kv.l2kv_paged_attn(Q, K, V, offsets(new), ints(table), page, ints(rows), 640, b, ws, 0.3)
+    sizes = (n, Hq, Hkv, sum(new), 64, D, dtype)
+    assert l2kv.l2kv_prompt_attn_workspace_bytes(*sizes) == l2kv.l2kv_paged_attn_workspace_bytes(*sizes) == 0
+    l2kv.l2kv_prompt_attn(Q, K, V, offsets(new), offsets(rows), None, 64, a, None, 0.3)
+    table = [[2 * s, 2 * s + 1] for s in range(n)]
+    l2kv.l2kv_paged_attn(Q, K, V, offsets(new), ints(table), page, ints(rows), 64, b, None, 0.3)
     assert torch.equal(a, b)
 
 
