@@ -6,19 +6,20 @@
 // matter, and of the entries that name one page the last is found with an atomic maximum.
 //
 // The tables are small (64 sequences of 500 pages: 128 KB) and every decision needs all those before it, so one workgroup works through them,
-// 1024 sequences and 8192 entries at a time; where that is all, as a rule, entries stay in registers.  It is bound by the
-// memory round trips that follow one another.  The copies are a launch of their own behind it.
+// 1024 sequences and 2048 entries at a time; up to 8192 entries stay in LDS from phase to phase.  It is bound by the
+// memory round trips that follow one another and by the fetch of its own instructions.  The copies are a launch of their own behind it.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 
 namespace l2kv {
 namespace {
 
-constexpr int kPageThreads = 1024, kPageWaves = kPageThreads / kWaveSize;
+constexpr int kPageThreads = 1024, kKeptEntries = 8192, kPageWaves = kPageThreads / kWaveSize;
 constexpr int kForkThreads = 256, kCopyThreads = 256;
 
 // In the workspace: of every page how many of its holders are left when the entries at hand are taken off, and the last of those entries;
-// pages to copy, {from, to} (from -1: none), and their number.
+// pages to copy, {from, to}, and their number.  (A release of large tables has the free pages before it, and those freed by each
+// workgroup, in the same places.)
 struct PagesScratch {
     int32_t *left, *last;
     int2* copies;
@@ -38,7 +39,10 @@ struct PagesShared {
     int32_t news[kPageThreads];            // reserving: new pages wanted up to the end of a sequence
     int32_t need[kPageThreads];            // of them by itself
     bool others[kPageThreads];             // it would write a page that others hold as well
-    int32_t handed;                        // new pages handed out
+    int32_t handed, copied;                // new pages handed out, those of them that are copies
+    // entries that are looked at in every phase (place in the table, page, sequence), where they are few enough
+    int32_t at[kKeptEntries], page[kKeptEntries];
+    uint16_t seq[kKeptEntries];
 };
 
 // Inclusive prefix sum over the workgroup, and the sum of all; below 2^31.
@@ -65,8 +69,9 @@ __device__ __forceinline__ int32_t own_load_again(int32_t* p) { return __hip_ato
 __device__ __forceinline__ bool is_page(int32_t p, int32_t n_pages) { return p >= 0 && p < n_pages; }
 
 // kPer consecutive entries of a lane: place in the table (-1: none), sequence among the 1024 at hand, page (-1: none), whether it is its
-// sequence's last.
-constexpr int kPer = 8, kEntries = kPageThreads * kPer;
+// sequence's last.  (Two: a kernel that works through eight is 33 KB of instructions that every call fetches anew, 41 us a step of 32 branches,
+// 31 so; with one tables of 64 sequences of 250 pages take 114 us, 100 with two.)
+constexpr int kPer = 2, kEntries = kPageThreads * kPer;
 struct Entries {
     int32_t at[kPer], seq[kPer], page[kPer];
     bool last[kPer];
@@ -92,6 +97,28 @@ struct Entries {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) page[k] = is_page(page[k], a.n_pages) ? page[k] : -1;
     }
+    __device__ __forceinline__ void keep(PagesShared& sh, int32_t e0) const {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int32_t e = e0 + (int32_t)threadIdx.x * kPer + k;
+            if (e >= kKeptEntries) continue;
+            sh.at[e] = at[k];
+            sh.page[e] = page[k];
+            sh.seq[e] = (uint16_t)seq[k];
+        }
+    }
+    __device__ __forceinline__ void kept(const PagesShared& sh, int32_t e0, int32_t total) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int32_t e = e0 + (int32_t)threadIdx.x * kPer + k;
+            at[k] = -1, page[k] = -1, seq[k] = 0, last[k] = false;
+            if (e >= total) continue;
+            at[k] = sh.at[e];
+            page[k] = sh.page[e];
+            seq[k] = sh.seq[e];
+            last[k] = e + 1 == sh.upto[seq[k]];
+        }
+    }
 };
 
 // The entries of up to 1024 sequences from s0 on, laid end to end; `range` gives the first entry of a sequence and how many there are.
@@ -106,24 +133,42 @@ template <typename R> __device__ __forceinline__ int32_t lay_out(PagesShared& sh
     return total;
 }
 
-// Runs `visit` over all entries that `range` gives, all lanes together, kEntries at a time.  Where all of them are kept in registers from
-// one visit to the next (`kept`), nothing is read again.
-template <typename R, typename F>
-__device__ __forceinline__ void for_entries(PagesShared& sh, const PagesArgs& a, bool kept, Entries& x, R&& range, F&& visit) {
-    if (kept) {
-        visit(x);
-    } else {
+// All entries that `range` gives, 1024 sequences and kEntries entries at a time.  Where they fit they are kept, and nothing of the
+// tables and ranges is read again.
+template <typename R> struct AllEntries {
+    PagesShared& sh;
+    const PagesArgs& a;
+    R range;
+    int32_t total;
+    bool kept;
+    __device__ __forceinline__ AllEntries(PagesShared& sh_, const PagesArgs& a_, R range_) : sh(sh_), a(a_), range(range_) {
+        total = lay_out(sh, 0, a.n_seq, range);
+        kept = a.n_seq <= kPageThreads && total <= kKeptEntries;
+        if (!kept) return;
+        for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
+            Entries x;
+            x.load(sh, a, 0, e0, total);
+            x.keep(sh, e0);
+        }
+        __syncthreads();
+    }
+    // of the sequences from s0 on, which are laid out
+    template <typename F> __device__ __forceinline__ void each_of(int32_t s0, F&& visit) {
+        for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
+            Entries x;
+            if (kept) x.kept(sh, e0, total);
+            else x.load(sh, a, s0, e0, total);
+            visit(x, e0);
+        }
+        __syncthreads();
+    }
+    template <typename F> __device__ __forceinline__ void each(F&& visit) {
         for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
-            const int32_t total = lay_out(sh, s0, a.n_seq, range);
-            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
-                x.load(sh, a, s0, e0, total);
-                visit(x);
-            }
-            __syncthreads();
+            if (!kept) total = lay_out(sh, s0, a.n_seq, range);
+            each_of(s0, visit);
         }
     }
-    __syncthreads();
-}
+};
 
 __global__ __launch_bounds__(kForkThreads)
 void pages_init_kernel(const PagesArgs a) {
@@ -172,13 +217,10 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         first = (int32_t)(b >> a.page_shift);
         count = (int32_t)((e - 1) >> a.page_shift) - first + 1;
     };
-    Entries x;
-    int32_t total = lay_out(sh, 0, a.n_seq, range);
-    const bool kept = a.n_seq <= kPageThreads && total <= kEntries;
-    if (kept) x.load(sh, a, 0, 0, total);
+    AllEntries all(sh, a, range);
     // Pages that have one holder are that entry's own: nothing has to be counted for them (the same entry twice in a table has two).
     bool shared = false;
-    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+    all.each([&](const Entries& x, int32_t) {
         int32_t refs[kPer];
 #pragma unroll
         for (int k = 0; k < kPer; ++k) refs[k] = x.page[k] < 0 ? 1 : own_load(a.refs + x.page[k]);
@@ -192,7 +234,7 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
     });
     shared = __syncthreads_or(shared) != 0;
     if (shared) {
-        for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+        all.each([&](const Entries& x, int32_t) {
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 if (x.page[k] < 0) continue;
@@ -202,40 +244,48 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         });
     }
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
-    // Which entries want a new page: those without one, and of a page's holders all but the last if all of them ask, else all.
+    // Which entries want a new page: those without one, and of a page's holders all but the last if all of them ask, else all.  The sum of
+    // the lane's.
     auto wanted = [&](const Entries& x, bool (&want)[kPer]) {
+        int32_t n = 0;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             want[k] = x.at[k] >= 0 && x.page[k] < 0;
             if (shared && x.page[k] >= 0) want[k] = own_load(w.left + x.page[k]) >= 0 || own_load(w.last + x.page[k]) != x.at[k];
+            n += want[k] ? 1 : 0;
         }
+        return n;
     };
     int32_t base = 0;                                          // new pages wanted by the sequences before these
-    if (threadIdx.x == 0) sh.handed = 0;
+    if (threadIdx.x == 0) sh.handed = sh.copied = 0;
     for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
-        if (!kept) total = lay_out(sh, s0, a.n_seq, range);
+        if (!all.kept) all.total = lay_out(sh, s0, a.n_seq, range);
         sh.news[threadIdx.x] = 0;
         sh.need[threadIdx.x] = 0;
         sh.others[threadIdx.x] = false;
         __syncthreads();
-        // how many are wanted up to the end of each sequence, then who gets one
+        // how many are wanted up to the end of each sequence
         int32_t sum = base;
-        auto count = [&](const Entries& x, bool (&want)[kPer]) {
-            int32_t mine = 0, these;
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) mine += want[k] ? 1 : 0;
-            const int32_t upto = sum + block_prefix(mine, sh.waves, these);
+        all.each_of(s0, [&](const Entries& x, int32_t) {
+            bool want[kPer];
+            const int32_t mine = wanted(x, want);
+            int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
             sum += these;
-            int32_t so_far = upto - mine;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 so_far += want[k] ? 1 : 0;
                 if (want[k]) (void)__hip_atomic_fetch_add(&sh.need[x.seq[k]], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 if (x.last[k]) sh.news[x.seq[k]] = so_far;
             }
-            return upto - mine;
-        };
-        auto hand_out = [&](Entries& x, const bool (&want)[kPer], int32_t so_far) {
+        });
+        const int32_t end = sum;
+        // who gets one
+        sum = base;
+        all.each_of(s0, [&](const Entries& x, int32_t e0) {
+            bool want[kPer];
+            const int32_t mine = wanted(x, want);
+            int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
+            sum += these;
             int32_t page[kPer], number[kPer], most = 0;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
@@ -247,67 +297,38 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
             for (int k = 0; k < kPer; ++k) {
                 if (number[k] == 0) continue;
                 const int32_t fresh = is_page(page[k], a.n_pages) ? page[k] : 0;
-                w.copies[number[k] - 1] = make_int2(x.page[k], fresh);
-                if (x.page[k] >= 0) own_add(a.refs + x.page[k], -1);
+                if (x.page[k] >= 0) {
+                    own_add(a.refs + x.page[k], -1);
+                    // in no order: copies do not meet
+                    w.copies[__hip_atomic_fetch_add(&sh.copied, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)] = make_int2(x.page[k], fresh);
+                }
                 own_store(a.refs + fresh, 1);
                 a.table[x.at[k]] = fresh;
-                x.page[k] = -1;                                    // not asked about below
+                if (all.kept) sh.page[e0 + (int32_t)threadIdx.x * kPer + k] = -1;      // not asked about below
                 most = number[k];
             }
             if (most > 0) (void)__hip_atomic_fetch_max(&sh.handed, most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        };
+        });
         // The last holder of a page keeps it only if the others got their copies.
-        auto check = [&](const Entries& x) {
+        if (end > have) {
+            all.each_of(s0, [&](const Entries& x, int32_t) {
 #pragma unroll
-            for (int k = 0; k < kPer; ++k)
-                if (x.page[k] >= 0 && sh.news[x.seq[k]] > have && own_load_again(a.refs + x.page[k]) != 1) sh.others[x.seq[k]] = true;
-        };
-        bool want[kPer];
-        if (kept) {
-            wanted(x, want);
-            const int32_t before = count(x, want);
-            __syncthreads();
-            hand_out(x, want, before);
-            __syncthreads();
-            if (sum > have) check(x);
-        } else {
-            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
-                x.load(sh, a, s0, e0, total);
-                wanted(x, want);
-                (void)count(x, want);
-            }
-            __syncthreads();
-            const int32_t all = sum;
-            sum = base;
-            for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
-                x.load(sh, a, s0, e0, total);
-                wanted(x, want);
-                int32_t mine = 0, these;
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) mine += want[k] ? 1 : 0;
-                const int32_t upto = sum + block_prefix(mine, sh.waves, these);
-                sum += these;
-                hand_out(x, want, upto - mine);
-            }
-            __syncthreads();
-            for (int32_t e0 = 0; e0 < total && all > have; e0 += kEntries) {
-                x.load(sh, a, s0, e0, total);
-                check(x);
-            }
+                for (int k = 0; k < kPer; ++k)
+                    if (x.page[k] >= 0 && sh.news[x.seq[k]] > have && own_load_again(a.refs + x.page[k]) != 1) sh.others[x.seq[k]] = true;
+            });
         }
-        base = sum;
-        __syncthreads();
+        base = end;
         if (const int32_t s = s0 + (int32_t)threadIdx.x; s < a.n_seq) {
-            int32_t first, count_of = 0;
-            range(s, first, count_of);
-            const bool fits = count_of > 0 && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
+            int32_t first, count = 0;
+            range(s, first, count);
+            const bool fits = count > 0 && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
             ends[s] = fits ? to[s] : from[s];
         }
         __syncthreads();
     }
     if (threadIdx.x == 0) {
         *a.free_count = have - sh.handed;
-        *w.n_copies = sh.handed;
+        *w.n_copies = sh.copied;
     }
 }
 
@@ -326,7 +347,7 @@ void pages_copy_kernel(char* __restrict__ Kc, char* __restrict__ Vc, float* __re
         const int64_t pair = i / (per_page * n_planes), rest = i - pair * per_page * n_planes, plane = rest / per_page;
         const int64_t row = (rest - plane * per_page) * kRows + r;
         const int2 p = w.copies[pair];
-        if (p.x < 0 || row >= (int64_t)1 << page_shift) continue;
+        if (row >= (int64_t)1 << page_shift) continue;
         const int64_t src = plane * total_slots + ((int64_t)p.x << page_shift) + row, dst = plane * total_slots + ((int64_t)p.y << page_shift) + row;
         const Words<P::kWords> k = load_words_stream<P::kWords, P::kStride>(Kc + src * kRowBytes + c * 16);
         const Words<P::kWords> v = load_words_stream<P::kWords, P::kStride>(Vc + src * kRowBytes + c * 16);
@@ -351,16 +372,13 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
         first = (int32_t)from;
         count = a.max_pages - first;
     };
-    Entries x;
-    const int32_t total = lay_out(sh, 0, a.n_seq, range);
-    const bool kept = a.n_seq <= kPageThreads && total <= kEntries;
-    if (kept) x.load(sh, a, 0, 0, total);
-    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+    AllEntries every(sh, a, range);
+    every.each([&](const Entries& x, int32_t) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
             if (x.page[k] >= 0) own_store(w.last + x.page[k], -1);
     });
-    for_entries(sh, a, kept, x, range, [&](const Entries& x) {
+    every.each([&](const Entries& x, int32_t) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             if (x.page[k] < 0) continue;
@@ -384,9 +402,18 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
         return n;
     };
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
-    bool mine[kPer];
-    int32_t all = 0, sum = 0, these;
-    auto give_back = [&](const Entries& x, int32_t upto) {
+    int32_t all = 0, sum = 0;
+    every.each([&](const Entries& x, int32_t) {
+        bool mine[kPer];
+        int32_t these;
+        (void)block_prefix(freed(x, mine), sh.waves, these);
+        all += these;
+    });
+    every.each([&](const Entries& x, int32_t) {
+        bool mine[kPer];
+        int32_t these;
+        int32_t upto = sum + block_prefix(freed(x, mine), sh.waves, these);
+        sum += these;
 #pragma unroll
         for (int k = kPer - 1; k >= 0; --k) {
             if (mine[k]) {
@@ -395,23 +422,88 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
             }
             if (x.at[k] >= 0) a.table[x.at[k]] = -1;
         }
-    };
-    if (kept) {
-        const int32_t upto = block_prefix(freed(x, mine), sh.waves, all);
-        give_back(x, upto);
-    } else {
-        for_entries(sh, a, false, x, range, [&](const Entries& x) {
-            (void)block_prefix(freed(x, mine), sh.waves, these);
-            all += these;
-        });
-        for_entries(sh, a, false, x, range, [&](const Entries& x) {
-            const int32_t upto = sum + block_prefix(freed(x, mine), sh.waves, these);
-            sum += these;
-            give_back(x, upto);
-        });
-    }
+    });
     if (threadIdx.x == 0) *a.free_count = have + all < a.n_pages ? have + all : a.n_pages;
 }
+
+// The same for large tables, by many workgroups with a stretch of the table each and a launch for every phase (64 sequences of 8192 pages,
+// with their reservation: 1400 us by one workgroup).
+struct LargeRelease {
+    int32_t *have, *counts;                // free pages before, pages freed by each workgroup
+    __device__ __forceinline__ explicit LargeRelease(const PagesScratch& w) : have(w.n_copies + 1), counts(reinterpret_cast<int32_t*>(w.copies)) {}
+};
+template <typename F>
+__device__ __forceinline__ void for_stretch(const PagesArgs& a, const int32_t* keep, F&& visit) {
+    const int64_t all = (int64_t)a.n_seq * a.max_pages, each = (all + gridDim.x - 1) / gridDim.x;
+    const int64_t first = blockIdx.x * each, end = first + each < all ? first + each : all;
+    for (int64_t e0 = first; e0 < end; e0 += kPageThreads) {
+        const int64_t e = e0 + threadIdx.x;
+        int32_t at = -1, page = -1;
+        if (e < end) {
+            const uint32_t s = (uint32_t)e / (uint32_t)a.max_pages, i = (uint32_t)e - s * (uint32_t)a.max_pages;
+            const int64_t rows = keep[s] < 0 ? 0 : keep[s];
+            if (i >= (rows + (1 << a.page_shift) - 1) >> a.page_shift) {
+                at = (int32_t)e;
+                page = a.table[e];
+                page = is_page(page, a.n_pages) ? page : -1;
+            }
+        }
+        visit(at, page);
+    }
+}
+
+__global__ __launch_bounds__(kPageThreads)
+void pages_release_begin_kernel(const PagesArgs a, const int32_t* __restrict__ keep, void* workspace) {
+    const PagesScratch w(workspace, a.n_pages);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const int32_t have = *a.free_count;
+        *LargeRelease(w).have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
+    }
+    for_stretch(a, keep, [&](int32_t, int32_t page) {
+        if (page >= 0) w.last[page] = -1;
+    });
+}
+__global__ __launch_bounds__(kPageThreads)
+void pages_release_holders_kernel(const PagesArgs a, const int32_t* __restrict__ keep, void* workspace) {
+    const PagesScratch w(workspace, a.n_pages);
+    for_stretch(a, keep, [&](int32_t at, int32_t page) {
+        if (page < 0) return;
+        (void)__hip_atomic_fetch_add(a.refs + page, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        (void)__hip_atomic_fetch_max(w.last + page, at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+}
+__global__ __launch_bounds__(kPageThreads)
+void pages_release_count_kernel(const PagesArgs a, const int32_t* __restrict__ keep, void* workspace) {
+    const PagesScratch w(workspace, a.n_pages);
+    int32_t n = 0;
+    for_stretch(a, keep, [&](int32_t at, int32_t page) { n += page >= 0 && a.refs[page] <= 0 && w.last[page] == at; });
+    __shared__ int32_t waves[kPageWaves];
+    int32_t all;
+    (void)block_prefix(n, waves, all);
+    if (threadIdx.x == 0) LargeRelease(w).counts[blockIdx.x] = all;
+}
+__global__ __launch_bounds__(kPageThreads)
+void pages_release_end_kernel(const PagesArgs a, const int32_t* __restrict__ keep, void* workspace) {
+    const PagesScratch w(workspace, a.n_pages);
+    const LargeRelease r(w);
+    __shared__ int32_t waves[kPageWaves];
+    const int32_t have = *r.have, mine = threadIdx.x < gridDim.x ? r.counts[threadIdx.x] : 0;      // kLargeWorkgroups at most
+    int32_t all, sum;
+    (void)block_prefix(mine, waves, all);
+    (void)block_prefix(threadIdx.x < blockIdx.x ? mine : 0, waves, sum);
+    for_stretch(a, keep, [&](int32_t at, int32_t page) {
+        const bool freed = page >= 0 && a.refs[page] <= 0 && w.last[page] == at;
+        int32_t these;
+        const int32_t upto = sum + block_prefix(freed ? 1 : 0, waves, these);
+        sum += these;
+        if (freed && have + all - upto < a.n_pages) a.free_pages[have + all - upto] = page;
+        if (at >= 0) a.table[at] = -1;
+    });
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.free_count = have + all < a.n_pages ? have + all : a.n_pages;
+}
+
+// Entries that one workgroup looks at in the time of the three launches more, and those that a workgroup of many has.
+constexpr int64_t kLargeEntries = 4096, kLargeEach = 2048, kLargeWorkgroups = kPageThreads;
 
 }  // namespace
 
@@ -436,8 +528,9 @@ l2kv_status pages_reserve_dispatch(const PagesArgs& a, const int32_t* from, cons
                                    int32_t D, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* workspace, hipStream_t stream) {
     hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kPageThreads), 0, stream, a, from, to, ends, workspace);
     if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+    // as if every sequence had a page copied, and a workgroup for each compute unit at least
     const int64_t rows = (int64_t)a.n_seq * n_planes << a.page_shift, blocks = (rows + 15) / 16;
-    const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048));
+    const dim3 grid((unsigned)(blocks < 256 ? 256 : (blocks < 2048 ? blocks : 2048)));
     const int64_t slots = (int64_t)a.n_pages << a.page_shift;
 #define L2KV_COPY(RB)                                                                                                             \
     hipLaunchKernelGGL((pages_copy_kernel<RB>), grid, dim3(kCopyThreads), 0, stream, static_cast<char*>(Kc), static_cast<char*>(Vc), norms_c, \
@@ -452,6 +545,17 @@ l2kv_status pages_reserve_dispatch(const PagesArgs& a, const int32_t* from, cons
 }
 
 l2kv_status pages_release_dispatch(const PagesArgs& a, const int32_t* keep, void* workspace, hipStream_t stream) {
+    const int64_t entries = (int64_t)a.n_seq * a.max_pages;
+    if (entries > kLargeEntries) {
+        int64_t n = (entries + kLargeEach - 1) / kLargeEach;
+        n = n < kLargeWorkgroups ? n : kLargeWorkgroups;
+        n = n < 2 * (int64_t)a.n_pages ? n : 2 * (int64_t)a.n_pages;       // that their counts have room for
+        for (auto kernel : {pages_release_begin_kernel, pages_release_holders_kernel, pages_release_count_kernel, pages_release_end_kernel}) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(kPageThreads), 0, stream, a, keep, workspace);
+            if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
+        }
+        return L2KV_OK;
+    }
     hipLaunchKernelGGL(pages_release_kernel, dim3(1), dim3(kPageThreads), 0, stream, a, keep, workspace);
     return launch_status();
 }
