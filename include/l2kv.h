@@ -648,8 +648,8 @@ l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_
  *   Q      in : [total_q] x Hq heads, q_offsets DEVICE int64 [n_seq+1]
  *   Kc, Vc in : one layer's planes [Hkv][n_pages*page_size][D]
  *   kv_lens in: DEVICE int32 [n_seq], rows of every sequence (0 allowed)
- *   max_kv    : an upper bound of all of them, at least 1 (sizes the workspace and the decomposition; rows beyond it
- *               are still attended to)
+ *   max_kv    : an upper bound of all of them, 1 .. max_pages*page_size (sizes the workspace and the decomposition;
+ *               rows beyond it are still attended to)
  *   O     out : [total_q][Hq][D], dense, of type dt
  *   workspace : l2kv_paged_attn_workspace_bytes(...), as for l2kv_prompt_attn, with the same bound for all sizes
  * Arithmetic and errors: as l2kv_prompt_attn; SHAPE for page_size, max_pages, n_pages and where n_seq * max_pages exceeds 2^31-1.
@@ -728,8 +728,8 @@ size_t l2kv_pages_workspace_bytes(int64_t n_pages);
  *   table_in [n_seq][max_in], lens_in, keep [n_seq]; table_out [n_seq][max_out], lens_out [n_seq] = rows kept (capped at the
  *             pages' room; rows whose entry is no page are not written).  lens_out must not be an input.
  *   total_rows, total_kept: upper bounds of the sums of lens_in and of the rows kept (size the workspace and the launches;
- *             what goes beyond them is left out); total_kept < 2^29
- *   max_len : an upper bound of lens_in (chooses the kernel variant; rows beyond it are left out)
+ *             what goes beyond them is left out); total_kept < 2^28
+ *   max_len : an upper bound of lens_in, at most total_rows (chooses the kernel variant; rows beyond it are left out)
  *   workspace: l2kv_paged_compress_workspace_bytes(...) bytes, 16-aligned; contents irrelevant before and after, one per call
  *             that may run at the same time
  * Errors: NULL, DTYPE, SHAPE, WORKSPACE, ALIGN, LAUNCH.

@@ -160,7 +160,7 @@ _calls = None
 class _PythonCalls:
     """In place of the native calls: leaves every call to the checks and the marshalling in this file."""
     decode_attn = decode_attn_out = compress = rotary_append = prompt_attn = tree_attn = append_path = staticmethod(lambda *args: None)
-    paged_append = paged_attn = pages_fork = pages_reserve = pages_release = paged_compress = staticmethod(lambda *args: None)
+    norm_rotary_append = paged_append = paged_attn = pages_fork = pages_reserve = pages_release = paged_compress = staticmethod(lambda *args: None)
 
 
 def _load_calls():
@@ -186,7 +186,7 @@ def calls():
                 handle.l2kv_decode_attn, handle.l2kv_decode_attn_out, handle.l2kv_compress, handle.l2kv_keep_count,
                 handle.l2kv_rotary_append, handle.l2kv_prompt_attn, handle.l2kv_tree_attn, handle.l2kv_stream_append_path,
                 handle.l2kv_paged_append, handle.l2kv_paged_attn, handle.l2kv_pages_fork, handle.l2kv_pages_reserve,
-                handle.l2kv_pages_release, handle.l2kv_paged_compress)))
+                handle.l2kv_pages_release, handle.l2kv_paged_compress, handle.l2kv_norm_rotary_append)))
         except ImportError as e:
             warnings.warn("%s; calls go through ctypes (build with `python -m paper_2406_11430_amd.build`)" % e, RuntimeWarning)
             module = _PythonCalls
@@ -717,6 +717,10 @@ def l2kv_norm_rotary_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch
                             lens_in: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
                             layout: int = L2KV_ROTARY_HALF, amplitude: float = 1.0, stream=None) -> None:
     """l2kv_rotary_append with norms of the query and key heads before the rotation; weights are float32 ``[D]`` or None."""
+    st = (_calls or calls()).norm_rotary_append(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, slot_offsets, lens_in,
+                                              lens_out, q_weight, k_weight, eps, layout, amplitude, stream, _stream)
+    if st is not None:
+        return _check("l2kv_norm_rotary_append", st)
     total, Hkv, D, Hq, strides, total_slots = _append_shapes(Q, K, V, q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)
     _dev(token_offsets, slot_offsets, lens_in, lens_out)
     n_seq = 0

@@ -762,7 +762,7 @@ l2kv_status l2kv_pages_release(int32_t* page_table, int32_t n_seq, int32_t max_p
 
 static bool paged_compress_ok(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
     return n_planes > 0 && n_seq > 0 && n_seq <= kMaxPagedSeq && n_planes <= kMaxHeads / n_seq && total_rows > 0 && total_rows <= kMaxTokens &&
-           total_kept > 0 && total_kept < (int64_t{1} << 29);
+           total_kept > 0 && total_kept < (int64_t{1} << 28);
 }
 
 size_t l2kv_paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {

@@ -23,6 +23,7 @@ decltype(&l2kv_rotary_append) rotary_append_entry = nullptr;
 decltype(&l2kv_prompt_attn) prompt_attn_entry = nullptr;
 decltype(&l2kv_tree_attn) tree_attn_entry = nullptr;
 decltype(&l2kv_stream_append_path) append_path_entry = nullptr;
+decltype(&l2kv_norm_rotary_append) norm_rotary_append_entry = nullptr;
 decltype(&l2kv_paged_append) paged_append_entry = nullptr;
 decltype(&l2kv_paged_attn) paged_attn_entry = nullptr;
 decltype(&l2kv_pages_fork) pages_fork_entry = nullptr;
@@ -313,9 +314,9 @@ PyObject* tree_attn_checked(PyObject* const* args, Py_ssize_t n_args) {
 }
 
 // (Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, slot_offsets, lens_in, lens_out, layout, amplitude, stream,
-// stream's handle)
-PyObject* rotary_append_checked(PyObject* const* args, Py_ssize_t n_args) {
-    if (n_args != 18) Py_RETURN_NONE;
+// stream's handle); kNorm: q_weight, k_weight and eps in front of the layout
+template <bool kNorm> PyObject* rotary_append_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != (kNorm ? 21 : 18)) Py_RETURN_NONE;
     Arguments a{args};
     int64_t q_stride = 0, k_stride = 0, v_stride = 0, Hq = 0;
     l2kv_dtype dt;
@@ -358,6 +359,13 @@ PyObject* rotary_append_checked(PyObject* const* args, Py_ssize_t n_args) {
     } else {
         for (int i = 0; i < 3; ++i) a.require(a.none());
     }
+    const float *q_weight = nullptr, *k_weight = nullptr;
+    double eps = 0.0;
+    if constexpr (kNorm) {
+        if (!a.none()) q_weight = a.data<float>(at::kFloat, D);
+        if (!a.none()) k_weight = a.data<float>(at::kFloat, D);
+        eps = a.number();
+    }
     const int64_t layout = a.integer();
     const double amplitude = a.number();
     a.require(all_int32({n_seq, Hq, Hkv, D, 2 * freqs->numel()}) && (layout == L2KV_ROTARY_HALF || layout == L2KV_ROTARY_INTERLEAVED));
@@ -368,6 +376,10 @@ PyObject* rotary_append_checked(PyObject* const* args, Py_ssize_t n_args) {
     void *const kc = Kc->data_ptr(), *s;
     if (!a.stream(&s)) return nullptr;
     return status_of([&] {
+        if constexpr (kNorm)
+            return norm_rotary_append_entry(q, k, v, dt, total, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, q_stride, k_stride, v_stride, q_weight, k_weight,
+                                            eps, positions, f, rot_dim, (l2kv_rotary_layout)layout, amplitude, (int32_t)n_seq, token_off, slot_off,
+                                            lens_in, lens_out, slots, Qr, kc, Vc, norms, pos, s);
         return rotary_append_entry(q, k, v, dt, total, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, q_stride, k_stride, v_stride, positions, f, rot_dim,
                                    (l2kv_rotary_layout)layout, amplitude, (int32_t)n_seq, token_off, slot_off, lens_in, lens_out, slots, Qr, kc,
                                    Vc, norms, pos, s);
@@ -661,14 +673,16 @@ PyObject* pages_release(PyObject*, PyObject* const* a, Py_ssize_t n) { return gu
 PyObject* paged_compress(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_compress_checked(a, n); }); }
 PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return prompt_attn_checked(a, n); }); }
 PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return tree_attn_checked(a, n); }); }
-PyObject* rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return rotary_append_checked(a, n); }); }
+PyObject* rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return rotary_append_checked<false>(a, n); }); }
+PyObject* norm_rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return rotary_append_checked<true>(a, n); }); }
 PyObject* append_path(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return append_path_checked(a, n); }); }
 
 PyObject* bind(PyObject*, PyObject* args) {
-    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path, append, paged, fork, reserve, release, compact;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path, &append, &paged, &fork, &reserve,
-                          &release, &compact))
+    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path, append, paged, fork, reserve, release, compact, norm;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path, &append, &paged, &fork, &reserve,
+                          &release, &compact, &norm))
         return nullptr;
+    norm_rotary_append_entry = reinterpret_cast<decltype(norm_rotary_append_entry)>(norm);
     paged_append_entry = reinterpret_cast<decltype(paged_append_entry)>(append);
     paged_attn_entry = reinterpret_cast<decltype(paged_attn_entry)>(paged);
     pages_fork_entry = reinterpret_cast<decltype(pages_fork_entry)>(fork);
@@ -694,6 +708,7 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"prompt_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prompt_attn)), METH_FASTCALL, nullptr},
                          {"tree_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_attn)), METH_FASTCALL, nullptr},
                          {"append_path", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_path)), METH_FASTCALL, nullptr},
+                         {"norm_rotary_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_rotary_append)), METH_FASTCALL, nullptr},
                          {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
                          {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attn)), METH_FASTCALL, nullptr},
                          {"pages_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_fork)), METH_FASTCALL, nullptr},

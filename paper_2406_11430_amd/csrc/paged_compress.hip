@@ -186,10 +186,14 @@ l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, i
             hipLaunchKernelGGL(compress_gather_kernel, dim3(gather, planes), dim3(kPcThreads), 0, stream, a, w, p0);
             if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
         }
-        if (l2kv_status st = select_ragged_dispatch(w.norms, a.n_planes, a.n_seq, a.total_rows, w.in_off, w.out_off, a.total_kept, a.max_len,
-                                                    L2KV_KEEP_LOWEST, w.kept, stream);
-            st != L2KV_OK)
-            return st;
+        const int64_t step = (int64_t{1} << 21) / a.n_seq;         // planes of a launch: it has fewer than 2^32 lanes
+        for (int64_t p0 = 0; p0 < a.n_planes; p0 += step) {
+            const int32_t planes = (int32_t)(a.n_planes - p0 < step ? a.n_planes - p0 : step);
+            if (l2kv_status st = select_ragged_dispatch(w.norms + p0 * a.total_rows, planes, a.n_seq, a.total_rows, w.in_off, w.out_off, a.total_kept,
+                                                        a.max_len, L2KV_KEEP_LOWEST, w.kept + p0 * a.total_kept, stream);
+                st != L2KV_OK)
+                return st;
+        }
     }
     const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t per_block = row_bytes == 128 ? kPcRowsPerBlock<128> : kPcRowsPerBlock<256>;

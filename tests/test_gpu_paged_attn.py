@@ -221,3 +221,19 @@ def test_chunks_in_stretches(dtype, D, new, rows, G, Hkv):
     first = c.run()
     c.verify(first)
     assert torch.equal(first, c.run())
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("new,rows", [([3, 0, 0], [1, 5, 5]), ([2, 0, 1, 0], [300, 40, 7, 0]), ([0, 3, 0, 1, 0], [9, 4000, 0, 2500, 1]), ([0, 0, 1], [5, 0, 1])])
+def test_few_tokens_of_many_sequences(dtype, D, new, rows):
+    """No more tokens than sequences: some have several, some none, some more than rows; queries from a projection."""
+    c = Case(23, new, rows, 4, 2, D, dtype, 16)
+    both = torch.cat([c.Q, c.Q.flip(0), c.Q * 3], 1)
+    c.verify(c.run(Q=both[:, :4]))
+
+
+def test_scale_and_no_workspace():
+    c = Case(2, [1, 1], [45, 300], 2, 2, 64, torch.float32, 16)
+    O = torch.empty_like(c.Q)
+    l2kv.l2kv_paged_attn(c.Q, c.Kc, c.Vc, offsets(c.new), ints(c.table), 16, ints(c.rows), 300, O, None, 0.7)
+    c.verify(O, scale=0.7)
