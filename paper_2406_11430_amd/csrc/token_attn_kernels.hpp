@@ -37,6 +37,12 @@ void token_attn_kernel(const RowsArgs a) {
     constexpr float kLowest = -__FLT_MAX__;
     constexpr int kVec = G * D <= kDecThreads ? 1 : (G * D <= 2 * kDecThreads ? 2 : 4);
     static_assert(G * D <= 4 * kDecThreads && G <= kTokenRows, "output elements per thread");
+    // Groups of 7 and 8 heads form their scores on the matrix unit, as in decode_item: with that many the vector unit bounds a stream of
+    // products and cross-lane sums (64 sequences of 500 to 4000 rows, 8 KV heads of 8 query heads 128 us, 115 so; of 6 105 and 107).  A tile
+    // of K, the weights and the factors of a rescaling pass through LDS, in the place of the sums after the loop.
+    constexpr bool kMfma = kBf16 && D == 128 && G >= 7;
+    constexpr int kKtFloats = kDecWaves * 16 * kKtRow / 4;
+    static_assert(!kMfma || kKtFloats + kDecWaves * G * 16 + kDecWaves * 8 <= kGroups * G * D, "room for what the loop keeps");
     __shared__ __attribute__((aligned(16))) float s_acc[kGroups * G * D];
     __shared__ float s_m[kGroups * G], s_l[kGroups * G];
 
@@ -65,11 +71,26 @@ void token_attn_kernel(const RowsArgs a) {
         const char* const Vh = a.V + (int64_t)it.head * a.kv_head_stride * E::kBytes;
         table_t* const table = (table_t*)(uintptr_t)(a.page_table + (int64_t)it.seq * a.max_pages);
 
-        uint32_t qw[G][W];
+        uint32_t qw[kMfma ? 1 : G][W];
         float qf[kBf16 ? 1 : G][kBf16 ? 1 : EPL];
         const char* const Q = a.Q + (token * a.q_stride + (int64_t)it.head * G * D) * E::kBytes;
+        [[maybe_unused]] bf16x8_t qa[4];                       // head c, elements 32j + 8rg ..
+        [[maybe_unused]] float cm[4], cl[4];                   // heads 4rg + i: maximum, and the weights of row c of the tiles
+        [[maybe_unused]] char* const kt = reinterpret_cast<char*>(s_acc) + wave * 16 * kKtRow;
+        [[maybe_unused]] float* const sp = s_acc + kKtFloats + wave * G * 16;
+        [[maybe_unused]] float* const sa = s_acc + kKtFloats + kDecWaves * G * 16 + wave * 8;
+        if constexpr (kMfma) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
+            for (int j = 0; j < 4; ++j) {
+                u32x4_t raw = {0u, 0u, 0u, 0u};
+                if (c < G) raw = *reinterpret_cast<const u32x4_t*>(Q + c * kRowBytes + (j * 4 + rg) * 16);
+                qa[j] = __builtin_bit_cast(bf16x8_t, raw);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cm[i] = kLowest, cl[i] = 0.f;
+        }
+#pragma unroll
+        for (int g = 0; g < (kMfma ? 0 : G); ++g) {
             const Words<W> raw = cached_words<W>(Q + g * kRowBytes + (c % kLanesPerRow) * Pieces<W>::kBytes);
 #pragma unroll
             for (int w = 0; w < W; ++w) qw[g][w] = raw.w[w];
@@ -128,18 +149,71 @@ void token_attn_kernel(const RowsArgs a) {
             }
         };
 
-        auto consume = [&](Tile<E, D>& t, int32_t first, bool last) {
-            // Query heads at a time, whose scores and weights are in registers together: half of 5 to 8 (64 sequences of 500 to 4000 rows, 8 KV heads
-            // of 8 query heads 134 us, 128 so).
-            constexpr int kPass = G > 4 ? (G + 1) / 2 : G;
-            if (last) {
+        // Rows behind the last have no weight, and no value: 0 times an infinity is not zero.
+        auto hide = [&](Tile<E, D>& t, int32_t first) {
+#pragma unroll
+            for (int u = 0; u < kDecLoads; ++u) {
+                const bool there = first + (u * kRowsPerWaveLoad + rg) * Geo::kRowsPerSlot + c / kLanesPerRow < n;
+#pragma unroll
+                for (int w = 0; w < W; ++w) t.v[u].w[w] = there ? t.v[u].w[w] : 0u;
+            }
+        };
+        auto consume_mfma = [&](Tile<E, D>& t, int32_t first, bool last) {
+            if constexpr (kMfma) {
+                if (last) hide(t, first);
+                // the tile of K, rows a little apart, to the layout of the operand: row c, elements 32j + 8rg ..
+#pragma unroll
+                for (int u = 0; u < kDecLoads; ++u)
+                    *reinterpret_cast<u32x4_t*>(kt + (u * kRowsPerWaveLoad + rg) * kKtRow + c * 16) = u32x4_t{t.k[u].w[0], t.k[u].w[1], t.k[u].w[2], t.k[u].w[3]};
+                __builtin_amdgcn_wave_barrier();
+                f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(kt + c * kKtRow + (j * 4 + rg) * 16);
+                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qa[j], __builtin_bit_cast(bf16x8_t, w), sc, 0, 0, 0);
+                }
+                const bool there = !last || first + c < n;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float si = there ? sc[i] : -INFINITY;
+                    const float mn = fmaxf(cm[i], row16_max(si) * a.scale);
+                    const float alpha = fast_exp2(cm[i] - mn), pi = fast_exp2(fmaf(si, a.scale, -mn));
+                    cl[i] = fmaf(cl[i], alpha, pi);
+                    cm[i] = mn;
+                    if (const int g = 4 * rg + i; g < G) {
+                        sp[g * 16 + (c % 4) * 4 + c / 4] = pi;     // [head][row group of the row][load of the row]
+                        if (c == 0) sa[g] = alpha;
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+                float pw[G][kDecLoads];
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const f32x4_t pg = *reinterpret_cast<const f32x4_t*>(sp + g * 16 + rg * 4);
+#pragma unroll
+                    for (int u = 0; u < kDecLoads; ++u) pw[g][u] = pg[u];
+                    const float alpha = sa[g];
+#pragma unroll
+                    for (int e = 0; e < EPL; ++e) acc[g][e] *= alpha;
+                }
 #pragma unroll
                 for (int u = 0; u < kDecLoads; ++u) {
-                    const bool there = first + (u * kRowsPerWaveLoad + rg) * Geo::kRowsPerSlot + c / kLanesPerRow < n;
+                    float vx[EPL];
+                    widen_words<E, W>(t.v[u], vx);
 #pragma unroll
-                    for (int w = 0; w < W; ++w) t.v[u].w[w] = there ? t.v[u].w[w] : 0u;       // 0 times an infinity is not zero
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int e = 0; e < EPL; ++e) acc[g][e] = fmaf(pw[g][u], vx[e], acc[g][e]);
                 }
+                __builtin_amdgcn_wave_barrier();                   // the next tile goes where this one was
             }
+        };
+        auto consume_vector = [&](Tile<E, D>& t, int32_t first, bool last) {
+            // Query heads at a time, whose scores and weights are in registers together: half of 5 to 8 (64 sequences of 500 to 4000 rows, 8 KV heads
+            // of 8 query heads 134 us, 128 so).
+            if constexpr (!kMfma) {
+            constexpr int kPass = G > 4 ? (G + 1) / 2 : G;
+            if (last) hide(t, first);
 #pragma unroll
             for (int g0 = 0; g0 < G; g0 += kPass) {
                 float s[kPass][kDecLoads], p[kPass][kDecLoads];
@@ -212,6 +286,12 @@ void token_attn_kernel(const RowsArgs a) {
                 }
                 if (g0 + kPass < G) __builtin_amdgcn_sched_barrier(0);
             }
+            }
+        };
+
+        auto consume = [&](Tile<E, D>& t, int32_t first, bool last) {
+            if constexpr (kMfma) consume_mfma(t, first, last);
+            else consume_vector(t, first, last);
         };
 
         // Full tiles in two registers' worth in turn: the next is asked for before the one at hand is worked on, the page numbers of the one after
@@ -258,6 +338,24 @@ void token_attn_kernel(const RowsArgs a) {
             }
         }
 
+        if constexpr (kMfma) {
+            // to the layout of the row groups, which share the maximum; the sum of weights counts once
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float sum = row16_tree_sum(cl[i]);
+                if (const int g = 4 * rg + i; g < G && c == 0) {
+                    sa[g] = cm[i];
+                    sp[g] = sum;
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                m[g] = sa[g];
+                l[g] = rg == 0 ? sp[g] : 0.f;
+            }
+            __syncthreads();                                       // nobody reads the loop's part of it any more
+        }
         // the row groups of the workgroup through LDS
         const int grp = (wave * kRowsPerWaveLoad + rg) * Geo::kRowsPerSlot + c / kLanesPerRow, cr = c % kLanesPerRow;
 #pragma unroll
