@@ -37,10 +37,10 @@ void token_attn_kernel(const RowsArgs a) {
     constexpr float kLowest = -__FLT_MAX__;
     constexpr int kVec = G * D <= kDecThreads ? 1 : (G * D <= 2 * kDecThreads ? 2 : 4);
     static_assert(G * D <= 4 * kDecThreads && G <= kTokenRows, "output elements per thread");
-    // Groups of 7 and 8 heads form their scores on the matrix unit, as in decode_item: with that many the vector unit bounds a stream of
-    // products and cross-lane sums (64 sequences of 500 to 4000 rows, 8 KV heads of 8 query heads 128 us, 115 so; of 6 105 and 107).  A tile
+    // Groups of 6 to 8 heads form their scores on the matrix unit, as in decode_item: with that many the vector unit bounds a stream of
+    // products and cross-lane sums (64 sequences of 500 to 4000 rows, 8 KV heads of 8 query heads 128 us, 115 so; of 6 110 and 105).  A tile
     // of K, the weights and the factors of a rescaling pass through LDS, in the place of the sums after the loop.
-    constexpr bool kMfma = kBf16 && D == 128 && G >= 7;
+    constexpr bool kMfma = kBf16 && D == 128 && G >= 6;
     constexpr int kKtFloats = kDecWaves * 16 * kKtRow / 4;
     static_assert(!kMfma || kKtFloats + kDecWaves * G * 16 + kDecWaves * 8 <= kGroups * G * D, "room for what the loop keeps");
     __shared__ __attribute__((aligned(16))) float s_acc[kGroups * G * D];
