@@ -43,6 +43,8 @@ struct PagesShared {
     // entries that are looked at in every phase (place in the table, page, sequence), where they are few enough
     int32_t at[kKeptEntries], page[kKeptEntries];
     uint16_t seq[kKeptEntries];
+    bool flag[kKeptEntries];               // wants a new page, gives its page back: found out once
+    int32_t top[kPageThreads];             // the first pages to be handed out, asked for ahead
 };
 
 // Inclusive prefix sum over the workgroup, and the sum of all; below 2^31.
@@ -162,6 +164,25 @@ template <typename R> struct AllEntries {
         }
         __syncthreads();
     }
+    // What find(x, flags) says of a lane's entries, and how many it is true of: found out the first time, and again where it is not kept.
+    template <typename F> __device__ __forceinline__ int32_t flags_of(const Entries& x, int32_t e0, bool first, bool (&flags)[kPer], F&& find) {
+        bool* const at = sh.flag + (kept ? e0 + (int32_t)threadIdx.x * kPer : 0);
+        if (first || !kept) {
+            find(x, flags);
+            if (kept) {
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
+                    if (e0 + (int32_t)threadIdx.x * kPer + k < kKeptEntries) at[k] = flags[k];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) flags[k] = x.at[k] >= 0 && at[k];
+        }
+        int32_t n = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) n += flags[k] ? 1 : 0;
+        return n;
+    }
     template <typename F> __device__ __forceinline__ void each(F&& visit) {
         for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
             if (!kept) total = lay_out(sh, s0, a.n_seq, range);
@@ -211,8 +232,11 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
     __shared__ PagesShared sh;
     const PagesScratch w(workspace, a.n_pages);
     int32_t have = *a.free_count;
+    have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
+    const int32_t top = (int32_t)threadIdx.x < have ? a.free_pages[have - 1 - (int32_t)threadIdx.x] : -1;
+    int32_t own_from = 0, own_to = 0;                          // of the sequence that `range` was asked about last
     auto range = [&](int32_t s, int32_t& first, int32_t& count) {
-        const int64_t b = from[s], e = to[s];
+        const int64_t b = own_from = from[s], e = own_to = to[s];
         if (b < 0 || e <= b || e > (int64_t)a.max_pages << a.page_shift) return;
         first = (int32_t)(b >> a.page_shift);
         count = (int32_t)((e - 1) >> a.page_shift) - first + 1;
@@ -243,18 +267,17 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
             }
         });
     }
-    have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
-    // Which entries want a new page: those without one, and of a page's holders all but the last if all of them ask, else all.  The sum of
-    // the lane's.
+    sh.top[threadIdx.x] = top;
+    // Which entries want a new page: those without one, and of a page's holders all but the last if all of them ask, else all.
     auto wanted = [&](const Entries& x, bool (&want)[kPer]) {
-        int32_t n = 0;
+        int32_t left[kPer], last[kPer];
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
-            want[k] = x.at[k] >= 0 && x.page[k] < 0;
-            if (shared && x.page[k] >= 0) want[k] = own_load(w.left + x.page[k]) >= 0 || own_load(w.last + x.page[k]) != x.at[k];
-            n += want[k] ? 1 : 0;
+            left[k] = shared && x.page[k] >= 0 ? own_load(w.left + x.page[k]) : -1;
+            last[k] = shared && x.page[k] >= 0 ? own_load(w.last + x.page[k]) : x.at[k];
         }
-        return n;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) want[k] = x.at[k] >= 0 && (x.page[k] < 0 || left[k] >= 0 || last[k] != x.at[k]);
     };
     int32_t base = 0;                                          // new pages wanted by the sequences before these
     if (threadIdx.x == 0) sh.handed = sh.copied = 0;
@@ -266,9 +289,9 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         __syncthreads();
         // how many are wanted up to the end of each sequence
         int32_t sum = base;
-        all.each_of(s0, [&](const Entries& x, int32_t) {
+        all.each_of(s0, [&](const Entries& x, int32_t e0) {
             bool want[kPer];
-            const int32_t mine = wanted(x, want);
+            const int32_t mine = all.flags_of(x, e0, true, want, wanted);
             int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
             sum += these;
 #pragma unroll
@@ -283,7 +306,7 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         sum = base;
         all.each_of(s0, [&](const Entries& x, int32_t e0) {
             bool want[kPer];
-            const int32_t mine = wanted(x, want);
+            const int32_t mine = all.flags_of(x, e0, false, want, wanted);
             int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
             sum += these;
             int32_t page[kPer], number[kPer], most = 0;
@@ -291,7 +314,7 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
             for (int k = 0; k < kPer; ++k) {
                 so_far += want[k] ? 1 : 0;
                 number[k] = want[k] && sh.news[x.seq[k]] <= have ? so_far : 0;
-                if (number[k] > 0) page[k] = a.free_pages[have - number[k]];
+                if (number[k] > 0) page[k] = number[k] <= kPageThreads ? sh.top[number[k] - 1] : a.free_pages[have - number[k]];
             }
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
@@ -319,10 +342,9 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         }
         base = end;
         if (const int32_t s = s0 + (int32_t)threadIdx.x; s < a.n_seq) {
-            int32_t first, count = 0;
-            range(s, first, count);
-            const bool fits = count > 0 && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
-            ends[s] = fits ? to[s] : from[s];
+            // (a lane's sequence is the one that it laid out)
+            const bool fits = own_from >= 0 && own_to > own_from && own_to <= (int64_t)a.max_pages << a.page_shift && (sh.news[threadIdx.x] <= have || (sh.need[threadIdx.x] == 0 && !sh.others[threadIdx.x]));
+            ends[s] = fits ? own_to : own_from;
         }
         __syncthreads();
     }
@@ -388,31 +410,27 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
     });
     // Of the entries that name a page without holders the last gives it back; the first of these on top.
     auto freed = [&](const Entries& x, bool (&mine)[kPer]) {
-        int32_t refs[kPer], last[kPer], n = 0;
+        int32_t refs[kPer], last[kPer];
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             refs[k] = x.page[k] < 0 ? 1 : own_load(a.refs + x.page[k]);
             last[k] = x.page[k] < 0 ? 0 : own_load(w.last + x.page[k]);
         }
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            mine[k] = x.page[k] >= 0 && refs[k] <= 0 && last[k] == x.at[k];
-            n += mine[k] ? 1 : 0;
-        }
-        return n;
+        for (int k = 0; k < kPer; ++k) mine[k] = x.page[k] >= 0 && refs[k] <= 0 && last[k] == x.at[k];
     };
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
     int32_t all = 0, sum = 0;
-    every.each([&](const Entries& x, int32_t) {
+    every.each([&](const Entries& x, int32_t e0) {
         bool mine[kPer];
         int32_t these;
-        (void)block_prefix(freed(x, mine), sh.waves, these);
+        (void)block_prefix(every.flags_of(x, e0, true, mine, freed), sh.waves, these);
         all += these;
     });
-    every.each([&](const Entries& x, int32_t) {
+    every.each([&](const Entries& x, int32_t e0) {
         bool mine[kPer];
         int32_t these;
-        int32_t upto = sum + block_prefix(freed(x, mine), sh.waves, these);
+        int32_t upto = sum + block_prefix(every.flags_of(x, e0, false, mine, freed), sh.waves, these);
         sum += these;
 #pragma unroll
         for (int k = kPer - 1; k >= 0; --k) {
