@@ -13,8 +13,12 @@
 // lie in one piece), of the rest, which is copied, and of V the same behind it.  (Two pieces side by side a lane, where nothing belongs
 // together: 3.4 TB/s instead of 4.2 for fp32 rows of 128 of which 16 elements are turned.)
 //
+// Heads are normed on the way (kMore): the sum of squares in fp64 over the lanes of a row, weights in LDS as doubles, so that a normed element
+// costs two products more, and slots may be found by a table of pages.
+//
 // Bound by memory: 36768 bf16 tokens of 32 + 8 + 8 heads of 128 take 173 to 179 us, 5.05 to 5.25 TB/s in and out (a large copy: 4.80), 183 without the
 // rows that are on their way ahead; 64 fp32 tokens of 8 + 4 + 4 heads of 64 take 4.4 to 4.8 us, a launch and three loads that wait for one another.
+// With norms, into pages: the 36768 tokens 189 us (204 with a branch for every element), 64 tokens of 32 + 8 + 8 heads of 128 5.3 to 7 us.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 #include "row_norm.hpp"
