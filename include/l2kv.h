@@ -671,7 +671,7 @@ size_t l2kv_paged_attn_workspace_bytes(int32_t n_seq, int32_t Hq, int32_t Hkv, i
  * l2kv_pages_init makes all pages free and every entry of a table -1 (several tables: -1 in the others is the caller's
  * to write).  Which page goes where depends on nothing but the order of the entries: sequence after sequence, page
  * after page.  Calls that share refs, free_pages or a workspace must not overlap in time.  n_seq <= 65535.
- * Errors of the four calls: NULL, SHAPE (also n_seq * max_pages or n_pages * page_size beyond 2^31-1), ALIGN, LAUNCH;
+ * Errors of the four calls: NULL, SHAPE (also n_seq * max_pages beyond 2^30 or n_pages * page_size beyond 2^31-1), ALIGN, LAUNCH;
  * of those with a workspace, l2kv_pages_workspace_bytes(n_pages) bytes, 16-aligned, contents irrelevant before
  * and after, WORKSPACE.
  */

@@ -704,10 +704,15 @@ l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float*
 
 constexpr int32_t kMaxPagedSeq = 65535;
 
+// Sequences and tables of the bookkeeping, which counts entries in steps of some thousands in 31 bits.
+static bool books_ok(int32_t n_seq, int32_t max_pages) {
+    return n_seq <= kMaxPagedSeq && static_cast<int64_t>(n_seq) * max_pages <= int64_t{1} << 30;
+}
+
 l2kv_status l2kv_pages_init(int32_t* page_table, int32_t n_seq, int32_t max_pages, int32_t* refs, int32_t* free_pages,
                             int32_t* free_count, int32_t n_pages, void* stream) {
     if (page_table == nullptr || refs == nullptr || free_pages == nullptr || free_count == nullptr) return L2KV_ERR_NULL;
-    if (!pages_ok(n_seq, max_pages, 16, n_pages) || n_seq > kMaxPagedSeq) return L2KV_ERR_SHAPE;
+    if (!pages_ok(n_seq, max_pages, 16, n_pages) || !books_ok(n_seq, max_pages)) return L2KV_ERR_SHAPE;
     if (!aligned(page_table, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4)) return L2KV_ERR_ALIGN;
     return pages_init_dispatch(PagesArgs{page_table, refs, free_pages, free_count, n_seq, max_pages, n_pages, 4}, static_cast<hipStream_t>(stream));
 }
@@ -717,8 +722,8 @@ l2kv_status l2kv_pages_fork(const int32_t* table_in, const int32_t* lens_in, int
                             int32_t* lens_out, int32_t* refs, void* stream) {
     if (table_in == nullptr || lens_in == nullptr || parents == nullptr || table_out == nullptr || lens_out == nullptr || refs == nullptr)
         return L2KV_ERR_NULL;
-    if (!pages_ok(n_in, max_pages, page_size, n_pages) || !pages_ok(n_out, max_pages, page_size, n_pages) || n_in > kMaxPagedSeq ||
-        n_out > kMaxPagedSeq || table_in == table_out || lens_in == lens_out || parents == lens_out)
+    if (!pages_ok(n_in, max_pages, page_size, n_pages) || !pages_ok(n_out, max_pages, page_size, n_pages) || !books_ok(n_in, max_pages) ||
+        !books_ok(n_out, max_pages) || table_in == table_out || lens_in == lens_out || parents == lens_out)
         return L2KV_ERR_SHAPE;
     if (!aligned(table_in, 4) || !aligned(lens_in, 4) || !aligned(parents, 4) || !aligned(table_out, 4) || !aligned(lens_out, 4) || !aligned(refs, 4))
         return L2KV_ERR_ALIGN;
@@ -737,7 +742,7 @@ l2kv_status l2kv_pages_reserve(int32_t* page_table, int32_t n_seq, int32_t max_p
         free_count == nullptr || Kc == nullptr || Vc == nullptr || norms_c == nullptr || pos_c == nullptr)
         return L2KV_ERR_NULL;
     if (!dtype_ok(dt)) return L2KV_ERR_DTYPE;
-    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || n_seq > kMaxPagedSeq || n_planes <= 0 || !dim_ok(D, dt) || from == ends || to == ends)
+    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || !books_ok(n_seq, max_pages) || n_planes <= 0 || !dim_ok(D, dt) || from == ends || to == ends)
         return L2KV_ERR_SHAPE;
     if (workspace == nullptr || workspace_bytes < pages_workspace_bytes(n_pages)) return L2KV_ERR_WORKSPACE;
     if (!aligned(page_table, 4) || !aligned(from, 4) || !aligned(to, 4) || !aligned(ends, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) ||
@@ -751,7 +756,7 @@ l2kv_status l2kv_pages_release(int32_t* page_table, int32_t n_seq, int32_t max_p
                                const int32_t* keep_lens, int32_t* refs, int32_t* free_pages, int32_t* free_count,
                                int32_t n_pages, void* workspace, size_t workspace_bytes, void* stream) {
     if (page_table == nullptr || keep_lens == nullptr || refs == nullptr || free_pages == nullptr || free_count == nullptr) return L2KV_ERR_NULL;
-    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || n_seq > kMaxPagedSeq) return L2KV_ERR_SHAPE;
+    if (!pages_ok(n_seq, max_pages, page_size, n_pages) || !books_ok(n_seq, max_pages)) return L2KV_ERR_SHAPE;
     if (workspace == nullptr || workspace_bytes < pages_workspace_bytes(n_pages)) return L2KV_ERR_WORKSPACE;
     if (!aligned(page_table, 4) || !aligned(keep_lens, 4) || !aligned(refs, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4) ||
         !aligned(workspace, 16))

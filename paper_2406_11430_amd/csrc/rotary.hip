@@ -65,22 +65,39 @@ template <bool kMore> __device__ __forceinline__ int64_t token_slot(const Rotary
     return have + at < slots.count ? slots.first + have + at : kNoSlot;
 }
 
-// Slots behind which a sequence's rows end after the call: as many as there is room for, and in pages only as far as there are pages.
-template <bool kMore> __device__ __forceinline__ int64_t end_of_rows(const RotaryArgs& a, int64_t s) {
-    const int64_t n = clamped_range(a.token_off, s, a.total_tokens).count, have = a.lens_in[s] < 0 ? 0 : a.lens_in[s];
+// Where sequences s0 .. s0 + 63 end after the call, a lane each (in the last lane the first): as far as there is room, and in pages only as
+// far as there are pages.  Of new rows in many pages the whole wave looks for one that is missing (32768 tokens of 32 + 8 + 8 heads of 128 in pages
+// of 16, one entry after the other by a single lane: 390 us, 168 so).
+constexpr int64_t kFewPages = 4;
+template <bool kMore> __device__ __forceinline__ void write_lens(const RotaryArgs& a, int64_t s0, int lane) {
+    const int64_t s = s0 + (kWaveSize - 1 - lane);
+    const bool mine = s < a.n_seq;
+    const int64_t n = mine ? clamped_range(a.token_off, s, a.total_tokens).count : 0, have = !mine || a.lens_in[s] < 0 ? 0 : a.lens_in[s];
     if constexpr (kMore) {
         if (a.page_table != nullptr) {
-            int64_t index = have >> a.page_shift;
-            for (; index < a.max_pages && index << a.page_shift < have + n; ++index) {
-                const int32_t page = a.page_table[s * a.max_pages + index];
-                if (page < 0 || page >= a.n_pages) break;
+            auto held = [&](int64_t entry) { return a.page_table[entry] >= 0 && a.page_table[entry] < a.n_pages; };
+            const int64_t first = have >> a.page_shift, behind = ((have + n - 1) >> a.page_shift) + 1;
+            const int64_t wanted = n == 0 ? 0 : (behind < a.max_pages ? behind : a.max_pages) - first, entry = s * a.max_pages + first;
+            int64_t there = 0;
+            if (wanted <= kFewPages)
+                while (there < wanted && held(entry + there)) ++there;
+            for (uint64_t many = __ballot(wanted > kFewPages); many != 0; many &= many - 1) {
+                const int whose = __builtin_ctzll(many);
+                const int64_t e0 = __shfl(entry, whose), count = __shfl(wanted, whose);
+                int64_t i = 0;
+                uint64_t missing = 0;
+                for (; i < count && missing == 0; i += missing == 0 ? kWaveSize : __builtin_ctzll(missing))
+                    missing = __ballot(i + lane >= count || !held(e0 + i + lane));
+                if (lane == whose) there = i;                      // what is behind the last entry counts as missing
             }
-            const int64_t room = index << a.page_shift, end = have + n < room ? have + n : room;
-            return end > have ? end : have;
+            const int64_t room = (first + there) << a.page_shift, end = have + n < room ? have + n : room;
+            if (mine) a.lens_out[s] = (int32_t)(end > have ? end : have);
+            return;
         }
     }
+    if (!mine) return;
     const int64_t room = clamped_range(a.slot_off, s, a.total_slots).count, end = have + n < room ? have + n : room;
-    return end > have ? end : have;
+    a.lens_out[s] = (int32_t)(end > have ? end : have);
 }
 
 // Sum over the kLanes (4, 8 or 16) consecutive lanes that share a row, in every one of them the same.
@@ -136,9 +153,8 @@ void rotary_kernel(const RotaryArgs a) {
 
     if (a.lens_out != nullptr) {
         // by the last waves: the first ones look for slots
-        for (int64_t s = (int64_t)blockIdx.x * kRotThreads + (kRotThreads - 1 - threadIdx.x); s < a.n_seq; s += (int64_t)gridDim.x * kRotThreads) {
-            a.lens_out[s] = (int32_t)end_of_rows<kMore>(a, s);
-        }
+        for (int64_t s0 = (int64_t)blockIdx.x * kRotThreads + (kRotWaves - 1 - wave) * kWaveSize; s0 < a.n_seq; s0 += (int64_t)gridDim.x * kRotThreads)
+            write_lens<kMore>(a, s0, lane);
     }
     const int heads = a.Hq + 2 * a.Hkv, u = lane % kLanes;
     const int rows = tokens * heads;

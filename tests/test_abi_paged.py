@@ -71,7 +71,8 @@ def test_pages_refuse(name):
     for p in pointers:
         assert call(name, defaults, **{p: None}) == E_NULL, p
         assert call(name, defaults, **{p: defaults[p] + 2}) == E_ALIGN, p
-    for want, kw in PAGES_BAD + [(E_SHAPE, dict(n_seq=65536))]:
+    books = [(E_SHAPE, dict(n_seq=65536))] + ([(E_SHAPE, dict(n_seq=1 << 10, max_pages=(1 << 20) + 1))] if name != "l2kv_paged_compress" else [])
+    for want, kw in PAGES_BAD + books:
         if set(kw) <= set(defaults):
             assert call(name, defaults, **kw) == want, kw
     if "ws" in defaults:
@@ -83,7 +84,8 @@ def test_pages_refuse(name):
 
 
 @pytest.mark.parametrize("name,kw", [("l2kv_pages_fork", dict(out=P)), ("l2kv_pages_fork", dict(lens_out=P)), ("l2kv_pages_fork", dict(n_out=0)),
-                                     ("l2kv_pages_fork", dict(n_out=65536)), ("l2kv_pages_reserve", dict(ends=P)), ("l2kv_paged_compress", dict(out=P)),
+                                     ("l2kv_pages_fork", dict(n_out=65536)), ("l2kv_pages_fork", dict(n_out=1 << 10, max_pages=(1 << 20) + 1)),
+                                     ("l2kv_pages_reserve", dict(ends=P)), ("l2kv_paged_compress", dict(out=P)),
                                      ("l2kv_paged_compress", dict(lens_out=P)), ("l2kv_paged_compress", dict(rows=0)), ("l2kv_paged_compress", dict(kept=0)),
                                      ("l2kv_paged_compress", dict(kept=1 << 29)), ("l2kv_paged_compress", dict(max_len=101)), ("l2kv_paged_compress", dict(max_len=0)),
                                      ("l2kv_paged_compress", dict(max_out=0)), ("l2kv_paged_compress", dict(planes=1 << 30))])

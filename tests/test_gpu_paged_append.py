@@ -157,6 +157,25 @@ def test_missing_pages():
     assert (Kc[:, rest] == 9).all() and (norms[:, rest] == 9).all() and (pos[:, rest] == 9).all()
 
 
+@pytest.mark.parametrize("page,have", [(16, 0), (16, 21), (256, 300)])
+def test_many_pages_and_one_that_is_missing(page, have):
+    """Lengths of prompts over many pages end before the first that is missing, wherever in the table it is (among those of new rows)."""
+    D, places = 64, [0, 1, 3, 4, 5, 62, 63, 64, 65, 127, 128, 180, None]
+    pages = 180
+    table = [[0] * pages for _ in places]
+    for row, missing in zip(table, places):
+        if missing is not None and missing < pages:
+            row[missing] = -1
+    new = [pages * page - have - s for s in range(len(places))]
+    total = sum(new)
+    K = torch.zeros((total, 1, D), dtype=torch.bfloat16, device=DEV)
+    lens_out = ints([0] * len(places))
+    l2kv.l2kv_paged_append(None, K, K, torch.zeros(total, dtype=torch.int32, device=DEV), l2kv.l2kv_rotary_freqs(16).to(DEV), None,
+                           *cache(1, page, D, torch.bfloat16), offsets(new), ints(table), page, ints([have] * len(places)), lens_out)
+    rows = [have + n for n in new]
+    assert lens_out.tolist() == [r if m is None or m < have // page else max(have, min(r, m * page)) for r, m in zip(rows, places)]
+
+
 def test_inconsistent_arrays_stay_inside():
     Hkv, D, page = 2, 128, 16
     Q, K, V = inputs(2, 20, 2, Hkv, D, torch.bfloat16)

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 class Case:
     """Sequences with `rows` rows, of which the last `new` are queried; whatever is no row of a sequence holds NaN."""
 
-    def __init__(self, seed, new, rows, Hq, Hkv, D, dtype, page, table=None):
+    def __init__(self, seed, new, rows, Hq, Hkv, D, dtype, page):
         self.new, self.rows, self.page = new, rows, page
         self.table, self.n_pages, self.slots = table_of(rows, page, seed)
         gen = torch.Generator(device=DEV).manual_seed(seed)

@@ -98,13 +98,11 @@ def test_room_of_the_new_pages():
     c.b[1][1] = -1
     kept = c.run(keep=[50, 25, -4])
     assert kept == [32, 25, 0]
-    was = c.was[0].clone()
     c.b[1][1] = c.n_pages                                              # a page that is not there, for the rows of it
     for x in range(4):
         c.was[x] = torch.cat([c.was[x], torch.zeros_like(c.was[x][:, :16])], 1)
     c.cache = [torch.cat([x, torch.zeros_like(x[:, :16])], 1) for x in c.cache]
     old = [x.clone() for x in c.was]
-    c.verify_rows = None
     for s, k in ((0, 32), (1, 16)):
         at, src = slots_of(c.b[s], k, 16).to(DEV), c.old[s].to(DEV)
         all_kept = torch.sort(old[2][:, src], dim=-1, stable=True).indices[:, :kept[s]].sort(-1).values[:, :k]
@@ -112,7 +110,6 @@ def test_room_of_the_new_pages():
             x[:, at] = x[:, src].gather(1, all_kept if x.dim() == 2 else all_kept[..., None].expand(-1, -1, x.shape[2]))
     for x, y in zip(c.cache, c.was):
         assert torch.equal(x, y)
-    assert torch.equal(was, was)
 
 
 def test_shared_rows_and_a_graph():
