@@ -731,7 +731,7 @@ size_t l2kv_pages_workspace_bytes(int64_t n_pages);
  *             what goes beyond them is left out); total_kept < 2^28
  *   max_len : an upper bound of lens_in, at most total_rows (chooses the kernel variant; rows beyond it are left out)
  *   workspace: l2kv_paged_compress_workspace_bytes(...) bytes, 16-aligned; contents irrelevant before and after, one per call
- *             that may run at the same time
+ *             that may run at the same time.  One that was sized for no fewer planes, sequences, rows and kept rows is always enough.
  * Errors: NULL, DTYPE, SHAPE, WORKSPACE, ALIGN, LAUNCH.
  */
 l2kv_status l2kv_paged_compress(void* Kc, void* Vc, float* norms_c, int32_t* pos_c, l2kv_dtype dt, int32_t n_planes,

@@ -787,7 +787,7 @@ l2kv_status l2kv_paged_compress(void* Kc, void* Vc, float* norms_c, int32_t* pos
         !paged_compress_ok(n_planes, n_seq, total_rows, total_kept) || max_len <= 0 || max_len > total_rows || table_in == table_out ||
         lens_out == lens_in || lens_out == keep)
         return L2KV_ERR_SHAPE;
-    if (workspace == nullptr || workspace_bytes < paged_compress_workspace_bytes(n_planes, n_seq, total_rows, total_kept)) return L2KV_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < paged_compress_least_bytes(n_planes, n_seq, total_rows, total_kept)) return L2KV_ERR_WORKSPACE;
     if (!aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(norms_c, 4) || !aligned(pos_c, 4) || !aligned(table_in, 4) || !aligned(lens_in, 4) ||
         !aligned(keep, 4) || !aligned(table_out, 4) || !aligned(lens_out, 4) || !aligned(workspace, 16))
         return L2KV_ERR_ALIGN;
@@ -796,7 +796,7 @@ l2kv_status l2kv_paged_compress(void* Kc, void* Vc, float* norms_c, int32_t* pos
     a.table_in = table_in, a.lens_in = lens_in, a.keep = keep, a.table_out = table_out, a.lens_out = lens_out;
     a.total_rows = total_rows, a.total_kept = total_kept, a.max_len = max_len;
     a.n_planes = n_planes, a.n_seq = n_seq, a.max_in = max_in, a.max_out = max_out, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
-    return paged_compress_dispatch(a, dt, D, workspace, static_cast<hipStream_t>(stream));
+    return paged_compress_dispatch(a, dt, D, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 /* ---- attention-loss analysis ---------------------------------------------- */

@@ -200,7 +200,8 @@ struct PagedCompressArgs {
     int32_t n_planes, n_seq, max_in, max_out, n_pages, page_shift;
 };
 size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept);
-l2kv_status paged_compress_dispatch(const PagedCompressArgs& args, l2kv_dtype dt, int32_t D, void* workspace, hipStream_t stream);
+size_t paged_compress_least_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept);      // without what makes it faster
+l2kv_status paged_compress_dispatch(const PagedCompressArgs& args, l2kv_dtype dt, int32_t D, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 // The accepted path of a drafted tree (append_path.hip).
 l2kv_status append_path_dispatch(const void* Kt, const void* Vt, const float* norms_t, const int32_t* pos_t, l2kv_dtype dt,

@@ -2,8 +2,10 @@
 // pages of another table (arXiv 2406.11430, Sec. 1: keep the lowest-norm keys and their values).
 //
 // A workgroup selects for each (plane, sequence), with the norms in registers straight from their pages; kept rows are then copied from page to
-// page, 16 bytes a lane, with norms and token ids.  Longer sequences, and very many, have their norms gathered into one line per plane
-// first (4 bytes a row beside the 2 * row bytes of each kept one) for the selection of ragged batches.  Source and destination are
+// page, 16 bytes a lane, with norms and token ids.  Few and longer sequences are selected from by several workgroups each, in three launches that
+// put the norms into one line per plane on the way (8 planes of 131072 rows, a tenth kept, 92 us with one workgroup a plane, 47 so; of 1000000
+// 722 and 232).  Many longer sequences, and very many, have their norms gathered first (4 bytes a row beside the 2 * row bytes of each kept
+// one) for the selection of ragged batches.  Source and destination are
 // other pages, so rows that several sequences share are only read, and nothing has to be read before it is written over.
 //
 // Bound by memory: 64 sequences of 1k to 8k bf16 rows of 128 in 8 planes, half kept, 254 us, 4.9 TB/s in and out with 15 us of selection (rows of
@@ -79,13 +81,6 @@ __device__ __forceinline__ int32_t sequence_from(const int64_t* off, int32_t n_s
         else hi = mid;
     }
     return lo;
-}
-
-// Rows that the selection saw.
-__device__ __forceinline__ int64_t have_of(const PagedCompressArgs& a, const CompressScratch& w, int32_t s) {
-    const Rows r = rows_of(a, s);
-    const int64_t left = a.total_rows - w.in_off[s];
-    return r.have < left ? r.have : left;
 }
 
 // Grid (256 rows, planes): norms from their pages into the line.
@@ -172,15 +167,21 @@ void compress_copy_kernel(const PagedCompressArgs a, CompressScratch w, int64_t 
 
 }  // namespace
 
+size_t paged_compress_least_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
+    return (size_t)(16 * (n_seq + 1) + 4 * n_planes * (total_rows + total_kept) + 15) / 16 * 16;
+}
 size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows, int64_t total_kept) {
-    return (size_t)(16 * (n_seq + 1) + 4 * n_planes * (total_rows + total_kept));
+    return paged_compress_least_bytes(n_planes, n_seq, total_rows, total_kept) + select_paged_split_bytes(n_planes, n_seq, total_rows);
 }
 
-l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, int32_t D, void* workspace, hipStream_t stream) {
+l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, int32_t D, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     const CompressScratch w(workspace, a.n_planes, a.n_seq, a.total_rows);
     constexpr int64_t kMaxY = 65535;
     if (a.max_len <= kPagedSelectRows && a.n_seq <= kPagedSelectSeq) {
         if (l2kv_status st = select_paged_dispatch(a, w, stream); st != L2KV_OK) return st;
+    } else if (select_paged_split_applies(a) && workspace_bytes >= paged_compress_workspace_bytes(a.n_planes, a.n_seq, a.total_rows, a.total_kept)) {
+        char* const scratch = static_cast<char*>(workspace) + paged_compress_least_bytes(a.n_planes, a.n_seq, a.total_rows, a.total_kept);
+        if (l2kv_status st = select_paged_split_dispatch(a, w, scratch, stream); st != L2KV_OK) return st;
     } else {
         hipLaunchKernelGGL(compress_offsets_kernel, dim3(1), dim3(kPcScan), 0, stream, a, w);
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;

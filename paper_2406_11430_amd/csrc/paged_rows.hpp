@@ -46,6 +46,13 @@ __device__ __forceinline__ Held held_of(const PagedCompressArgs& a, const Rows& 
     return h;
 }
 
+// Rows that the selection saw.
+__device__ __forceinline__ int64_t have_of(const PagedCompressArgs& a, const CompressScratch& w, int32_t s) {
+    const Rows r = rows_of(a, s);
+    const int64_t left = a.total_rows - w.in_off[s];
+    return r.have < left ? r.have : left;
+}
+
 __device__ __forceinline__ int64_t slot_of(const int32_t* table, int32_t max_pages, int32_t seq, int64_t row, int32_t shift, int32_t n_pages) {
     int32_t p = table[(int64_t)seq * max_pages + (row >> shift)];
     p = p < 0 ? 0 : (p < n_pages ? p : n_pages - 1);
@@ -55,5 +62,11 @@ __device__ __forceinline__ int64_t slot_of(const int32_t* table, int32_t max_pag
 // Selection straight from the pages, for sequences that a workgroup holds in registers (select.hip).
 constexpr int64_t kPagedSelectRows = 32768, kPagedSelectSeq = 1024;
 l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScratch& w, hipStream_t stream);
+
+// The same of few and longer ones, each by several workgroups: whether it is one of those, what it needs beside the scratch memory above,
+// 16-aligned (0: there is no such selection of these sizes), and the launch.
+bool select_paged_split_applies(const PagedCompressArgs& a);
+size_t select_paged_split_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows);
+l2kv_status select_paged_split_dispatch(const PagedCompressArgs& a, const CompressScratch& w, void* scratch, hipStream_t stream);
 
 }  // namespace l2kv

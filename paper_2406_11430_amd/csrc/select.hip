@@ -633,6 +633,59 @@ struct SelectSplit {
     int32_t chunks;       // per head
 };
 
+// Of one head: its keys, how many of them are kept, where the keys of a digit are listed and where kept positions go.
+struct SplitHead {
+    const uint32_t* keys;
+    int64_t T;
+    uint32_t k;
+    uint32_t* cand;
+    int32_t* out;
+};
+struct DenseHeads {
+    static constexpr bool kPaged = false;
+    const uint32_t* norm_bits;
+    int64_t T;
+    uint32_t k;
+    int32_t* kept_idx;
+    __device__ __forceinline__ SplitHead at(int64_t head, const SelectSplit& sp) const {
+        return SplitHead{norm_bits + head * T, T, k, sp.cand + head * T, kept_idx + head * (int64_t)k};
+    }
+};
+// Sequences of a compaction in pages (64 at most), plane after plane.  Their lengths differ: chunks may be empty, and heads.  The first kernel
+// finds out where they begin and writes their norms, one behind the other, for the others.
+struct PagedHeads {
+    static constexpr bool kPaged = true;
+    PagedCompressArgs a;
+    CompressScratch w;
+    __device__ __forceinline__ SplitHead at(int64_t head, const SelectSplit& sp) const {
+        const int32_t seq = (int32_t)head % a.n_seq;
+        const int64_t plane = (int32_t)head / a.n_seq, line = plane * a.total_rows + w.in_off[seq];
+        return SplitHead{reinterpret_cast<const uint32_t*>(w.norms) + line, have_of(a, w, seq), (uint32_t)a.lens_out[seq], sp.cand + line,
+                         w.kept + plane * a.total_kept + w.out_off[seq]};
+    }
+    // Of the head's sequence; `note`: of all of them into the scratch memory.
+    __device__ __forceinline__ Held held(int64_t head, bool note) const {
+        const int lane = threadIdx.x % kWaveSize, seq = (int32_t)head % a.n_seq;
+        Rows r = {0, 0};
+        if (lane < a.n_seq) r = rows_of(a, lane);
+        int64_t rows = r.have, kept = r.keep;
+#pragma unroll
+        for (int d = 1; d < kWaveSize; d *= 2) {
+            const int64_t x = __shfl_up(rows, d), y = __shfl_up(kept, d);
+            rows += lane >= d ? x : 0;
+            kept += lane >= d ? y : 0;
+        }
+        const Held h = held_of(a, r, rows - r.have, kept - r.keep);
+        if (note && lane < a.n_seq) {
+            w.in_off[lane] = h.in_first;
+            w.out_off[lane] = h.out_first;
+            a.lens_out[lane] = (int32_t)h.keep;
+            if (lane == a.n_seq - 1) w.out_off[a.n_seq] = h.out_end;
+        }
+        return Held{__shfl(h.in_first, seq), __shfl(h.have, seq), __shfl(h.out_first, seq), __shfl(h.keep, seq), 0};
+    }
+};
+
 struct SelectPlan {
     int64_t chunk = 0;    // 0: one workgroup per head
     int32_t chunks = 0;
@@ -656,12 +709,12 @@ static size_t count_bytes(int64_t chunk) { return chunk <= kChunk16 ? sizeof(uin
 //   4 of 4M           2396 / 126        2438 / 331          2790 / 796         2095 / 4206
 //   64 of 4M          3285 / 1117       3296 / 1483         3450 / 2054        2562 / 5447
 // and log-normal 8 of 40k 22.9 / 16.1, 64 of 40k 23.9 / 28.6, 128 of 131k 80 / 69 (not split: 112 / 199 for equal keys).
+constexpr int64_t kSplitWorkgroups = 512, kSplitHeads = 64;      // two workgroups per compute unit
 static SelectPlan select_plan(int64_t n_heads, int64_t T) {
     SelectPlan p;
-    constexpr int64_t kWorkgroups = 512;             // two per compute unit
     if (T <= (int64_t)kSelThreads * kSelMaxRegKeys || T > (int64_t{1} << 22)) return p;
-    if (n_heads > 64 || n_heads > T / 2048) return p;
-    const int64_t want = (kWorkgroups + n_heads - 1) / n_heads;
+    if (n_heads > kSplitHeads || n_heads > T / 2048) return p;
+    const int64_t want = (kSplitWorkgroups + n_heads - 1) / n_heads;
     const int64_t chunk = ((T + want - 1) / want + kChunkUnit - 1) / kChunkUnit * kChunkUnit;
     p.chunk = chunk;
     p.chunks = (int32_t)((T + chunk - 1) / chunk);
@@ -672,13 +725,25 @@ static SelectPlan select_plan(int64_t n_heads, int64_t T) {
     return p;
 }
 
-template <typename Count>
+template <typename Count, typename Heads>
 __global__ __launch_bounds__(kSelThreads)
-void select_count_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint32_t flip, SelectSplit sp) {
+void select_count_kernel(const Heads heads, uint32_t flip, SelectSplit sp) {
     __shared__ __attribute__((aligned(16))) uint32_t s_hist[kTopBins * kCopies];
     const int64_t head = blockIdx.y;
     const int64_t slot = head * sp.chunks + blockIdx.x;
-    const uint32_t* src = norm_bits + head * T;
+    int64_t T;
+    const uint32_t* src;
+    [[maybe_unused]] uint32_t* line;
+    if constexpr (Heads::kPaged) {
+        const Held h = heads.held(head, head == 0 && blockIdx.x == 0 && threadIdx.x < kWaveSize);
+        const int64_t plane = (int32_t)head / heads.a.n_seq;
+        T = h.have;
+        src = reinterpret_cast<const uint32_t*>(heads.a.norms_c) + plane * ((int64_t)heads.a.n_pages << heads.a.page_shift);
+        line = reinterpret_cast<uint32_t*>(heads.w.norms) + plane * heads.a.total_rows + h.in_first;
+    } else {
+        T = heads.T;
+        src = heads.norm_bits + head * T;
+    }
     const int64_t first = blockIdx.x * sp.chunk;
     const int64_t last = first + sp.chunk < T ? first + sp.chunk : T;
     clear_counts(s_hist, kTopBins * kCopies);
@@ -687,8 +752,15 @@ void select_count_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint
         uint32_t key[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t t = base + u * kSelThreads + threadIdx.x;
-            key[u] = src[t < last ? t : last - 1] ^ flip;
+            const int64_t t = base + u * kSelThreads + threadIdx.x, at = t < last ? t : last - 1;
+            if constexpr (Heads::kPaged)
+                key[u] = src[slot_of(heads.a.table_in, heads.a.max_in, (int32_t)head % heads.a.n_seq, at, heads.a.page_shift, heads.a.n_pages)];
+            else key[u] = src[at] ^ flip;
+        }
+        if constexpr (Heads::kPaged) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (base + u * kSelThreads + threadIdx.x < last) line[base + u * kSelThreads + threadIdx.x] = key[u];
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -718,9 +790,9 @@ __device__ __forceinline__ Found find_lane(uint32_t count, uint32_t want) {
     return Found{(uint32_t)at, __shfl(incl - count, at), __shfl(count, at)};
 }
 
-template <typename Count>
+template <typename Count, typename Heads>
 __global__ __launch_bounds__(kSelThreads)
-void select_gather_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint32_t k, uint32_t flip, SelectSplit sp) {
+void select_gather_kernel(const Heads heads, uint32_t flip, SelectSplit sp) {
     __shared__ uint32_t s_sum[2][kSelWaves][kCoarse], s_part[kSelWaves][kFinePerCoarse];
     __shared__ uint32_t s_lt, s_n;
     const int64_t head = blockIdx.y;
@@ -728,6 +800,10 @@ void select_gather_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uin
     const int64_t slot = slot0 + blockIdx.x;
     const int lane = threadIdx.x % kWaveSize;
     const int wave = threadIdx.x / kWaveSize;
+    const SplitHead mine = heads.at(head, sp);
+    const int64_t T = mine.T;
+    const uint32_t k = mine.k;
+    if (Heads::kPaged && k == 0) return;
     // the digit of tau: coarse counts of all chunks, then the 64 digits of the coarse count that
     // holds the k-th key; the waves share the chunks and every wave ends with the same result
     uint32_t n = 0;
@@ -768,8 +844,8 @@ void select_gather_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uin
         sp.head_info[2 * head] = digit;
         sp.head_info[2 * head + 1] = g.below + f.below;
     }
-    uint32_t* cand = sp.cand + head * T + ahead;
-    const uint32_t* src = norm_bits + head * T;
+    uint32_t* cand = mine.cand + ahead;
+    const uint32_t* src = mine.keys;
     const int64_t first = blockIdx.x * sp.chunk;
     const int64_t last = first + sp.chunk < T ? first + sp.chunk : T;
     uint32_t lt = 0;
@@ -798,9 +874,9 @@ void select_gather_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uin
     if (threadIdx.x == 0) sp.info[slot] = make_uint2(s_lt, s_n);
 }
 
+template <typename Heads>
 __global__ __launch_bounds__(kSelThreads)
-void select_emit_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint32_t k, uint32_t flip,
-                        int32_t* __restrict__ kept_idx, int32_t* __restrict__ kept_count, SelectSplit sp) {
+void select_emit_kernel(const Heads heads, uint32_t flip, int32_t* __restrict__ kept_count, SelectSplit sp) {
     __shared__ __attribute__((aligned(16))) uint32_t s_hist[(kMidBins + kLowBins) * kCopies];
     __shared__ FindShared s_find;
     __shared__ EmitShared s_emit;
@@ -809,6 +885,10 @@ void select_emit_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint3
     const int64_t slot0 = head * sp.chunks;
     const int lane = threadIdx.x % kWaveSize;
     const int wave = threadIdx.x / kWaveSize;
+    const SplitHead mine = heads.at(head, sp);
+    const int64_t T = mine.T;
+    const uint32_t k = mine.k;
+    if (Heads::kPaged && (k == 0 || blockIdx.x * sp.chunk >= T)) return;
     uint32_t* const h_mid = s_hist;
     uint32_t* const h_low = s_hist + kMidBins * kCopies;
     clear_counts(s_hist, (kMidBins + kLowBins) * kCopies);
@@ -838,7 +918,7 @@ void select_emit_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint3
     const uint32_t want = k - sp.head_info[2 * head + 1];
     __syncthreads();
     const uint32_t n = s_cands < (uint32_t)T ? s_cands : (uint32_t)T, ahead = s_cand_ahead < n ? s_cand_ahead : n;
-    const uint32_t* cand = sp.cand + head * T;
+    const uint32_t* cand = mine.cand;
     constexpr int kCandBatch = 4;
     auto for_cands = [&](uint32_t end, auto&& body) {
         for (uint32_t i0 = 0; i0 < end; i0 += kSelThreads * kCandBatch) {
@@ -876,7 +956,7 @@ void select_emit_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint3
         atomicAdd(&s_cand_eq, eq);
     }
     __syncthreads();
-    const uint32_t* src = norm_bits + head * T;
+    const uint32_t* src = mine.keys;
     const int64_t first = blockIdx.x * sp.chunk;
     const int64_t last = first + sp.chunk < T ? first + sp.chunk : T;
     const int64_t iters = sp.chunk / kSelThreads;
@@ -889,7 +969,7 @@ void select_emit_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint3
             return t < end ? v : 0xffffffffu;
         },
         iters, t0, tau, need_eq, s_lt_ahead + s_cand_lt, s_cand_eq,
-        [&](uint32_t i, int32_t t) { kept_idx[head * (int64_t)k + i] = t; }, k, s_emit);
+        [&](uint32_t i, int32_t t) { mine.out[i] = t; }, k, s_emit);
     if (kept_count != nullptr && blockIdx.x == 0 && threadIdx.x == 0) kept_count[head] = (int32_t)k;
 }
 
@@ -957,6 +1037,32 @@ SelectScratch select_scratch(void* workspace, size_t bytes, int64_t n_heads, int
     return SelectScratch{workspace, plan.counts, static_cast<char*>(workspace) + plan.counts, plan.list};
 }
 
+template <typename Heads>
+static l2kv_status launch_split(const Heads& heads, int64_t n_heads, const SelectPlan& plan, void* counts, void* list, uint32_t flip,
+                                int32_t* kept_count, hipStream_t stream) {
+    SelectSplit sp;
+    const size_t n = (size_t)n_heads * (size_t)plan.chunks;
+    char* ws = static_cast<char*>(counts);
+    sp.fine = ws;
+    ws += round256(n * kTopBins * count_bytes(plan.chunk));
+    sp.coarse = reinterpret_cast<uint32_t*>(ws);
+    ws += round256(n * kCoarse * sizeof(uint32_t));
+    sp.info = reinterpret_cast<uint2*>(ws);
+    ws += round256(n * sizeof(uint2));
+    sp.head_info = reinterpret_cast<uint32_t*>(ws);
+    sp.cand = static_cast<uint32_t*>(list);
+    sp.chunk = plan.chunk;
+    sp.chunks = plan.chunks;
+    const dim3 grid((unsigned)plan.chunks, (unsigned)n_heads);
+    const bool short_counts = count_bytes(plan.chunk) == sizeof(uint16_t);
+    hipLaunchKernelGGL((short_counts ? select_count_kernel<uint16_t, Heads> : select_count_kernel<uint32_t, Heads>), grid, dim3(kSelThreads), 0,
+                       stream, heads, flip, sp);
+    hipLaunchKernelGGL((short_counts ? select_gather_kernel<uint16_t, Heads> : select_gather_kernel<uint32_t, Heads>), grid, dim3(kSelThreads), 0,
+                       stream, heads, flip, sp);
+    hipLaunchKernelGGL((select_emit_kernel<Heads>), grid, dim3(kSelThreads), 0, stream, heads, flip, kept_count, sp);
+    return launch_status();
+}
+
 l2kv_status select_dispatch(const float* norms, int64_t n_heads, int64_t T, int64_t k,
                             l2kv_mode mode, int32_t* kept_idx, int32_t* kept_count,
                             const SelectScratch& scratch, hipStream_t stream) {
@@ -968,29 +1074,25 @@ l2kv_status select_dispatch(const float* norms, int64_t n_heads, int64_t T, int6
                                  RaggedSelect{nullptr, nullptr, 0, 0, 0});
         return launch_status();
     }
-    SelectSplit sp;
-    const size_t n = (size_t)n_heads * (size_t)plan.chunks;
-    char* ws = static_cast<char*>(scratch.counts);
-    sp.fine = ws;
-    ws += round256(n * kTopBins * count_bytes(plan.chunk));
-    sp.coarse = reinterpret_cast<uint32_t*>(ws);
-    ws += round256(n * kCoarse * sizeof(uint32_t));
-    sp.info = reinterpret_cast<uint2*>(ws);
-    ws += round256(n * sizeof(uint2));
-    sp.head_info = reinterpret_cast<uint32_t*>(ws);
-    sp.cand = static_cast<uint32_t*>(scratch.list);
-    sp.chunk = plan.chunk;
-    sp.chunks = plan.chunks;
-    const dim3 grid((unsigned)plan.chunks, (unsigned)n_heads);
-    const uint32_t* bits = reinterpret_cast<const uint32_t*>(norms);
-    const bool short_counts = count_bytes(plan.chunk) == sizeof(uint16_t);
-    hipLaunchKernelGGL((short_counts ? select_count_kernel<uint16_t> : select_count_kernel<uint32_t>), grid, dim3(kSelThreads), 0,
-                       stream, bits, T, flip, sp);
-    hipLaunchKernelGGL((short_counts ? select_gather_kernel<uint16_t> : select_gather_kernel<uint32_t>), grid, dim3(kSelThreads), 0,
-                       stream, bits, T, (uint32_t)k, flip, sp);
-    hipLaunchKernelGGL(select_emit_kernel, grid, dim3(kSelThreads), 0, stream, bits, T, (uint32_t)k, flip, kept_idx,
-                       kept_count, sp);
-    return launch_status();
+    const DenseHeads heads = {reinterpret_cast<const uint32_t*>(norms), T, (uint32_t)k, kept_idx};
+    return launch_split(heads, n_heads, plan, scratch.counts, scratch.list, flip, kept_count, stream);
+}
+
+// Counts of as many workgroups as a plan has at most, and the list of a plane's line each.
+constexpr int64_t kSplitMost = kSplitWorkgroups + kSplitHeads;
+static size_t most_split_counts() {
+    return round256((size_t)kSplitMost * kTopBins * sizeof(uint32_t)) + round256((size_t)kSplitMost * kCoarse * sizeof(uint32_t)) +
+           round256((size_t)kSplitMost * sizeof(uint2)) + round256((size_t)kSplitHeads * 2 * sizeof(uint32_t));
+}
+bool select_paged_split_applies(const PagedCompressArgs& a) { return select_plan((int64_t)a.n_planes * a.n_seq, a.max_len).chunk != 0; }
+size_t select_paged_split_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows) {
+    if (total_rows <= (int64_t)kSelThreads * kSelMaxRegKeys || n_planes * n_seq > kSplitHeads) return 0;
+    return most_split_counts() + (size_t)n_planes * (size_t)total_rows * sizeof(uint32_t);
+}
+l2kv_status select_paged_split_dispatch(const PagedCompressArgs& a, const CompressScratch& w, void* scratch, hipStream_t stream) {
+    const int64_t n_heads = (int64_t)a.n_planes * a.n_seq;
+    return launch_split(PagedHeads{a, w}, n_heads, select_plan(n_heads, a.max_len), scratch, static_cast<char*>(scratch) + most_split_counts(), 0u, nullptr,
+                        stream);
 }
 
 template <int E, bool kAhead>

@@ -151,3 +151,54 @@ def test_long_sequences(have, ties):
     c = Case(sum(have), have, keep, 2, 64, torch.bfloat16, 64, ties)
     assert c.run() == keep
     c.verify(keep)
+
+
+@pytest.mark.parametrize("have,keep", [([40000], [20001]), ([131072], [13107]), ([100003], [100003]), ([100003], [1]), ([33000, 0, 500, 40000, 65536], [100, 3, 500, 0, 40000])])
+@pytest.mark.parametrize("planes", [1, 3, 17])
+@pytest.mark.parametrize("ties", [False, True])
+def test_few_and_long_sequences(have, keep, planes, ties):
+    """Sequences that several workgroups select from, empty ones and short ones among them; with too many planes one each."""
+    c = Case(len(have) + planes, have, keep, planes, 64, torch.bfloat16, 16, ties)
+    kept = [min(k, h) for k, h in zip(keep, have)]
+    assert c.run() == kept
+    c.verify(kept)
+
+
+def test_bounds_of_long_sequences():
+    have, keep = [50000, 40000, 70000], [25000, 20000, 35000]
+    for bounds, kept, seen in ((dict(total=400000, kept=100000, top=300000), keep, have), (dict(total=95000, kept=60000, top=90000), [25000, 20000, 5000], [50000, 40000, 5000]),
+                               (dict(total=52000, top=50000), [25000, 2000, 0], [50000, 2000, 0]), (dict(kept=30000, top=70000), [25000, 5000, 0], have),
+                               (dict(top=45000), keep, [45000, 40000, 45000])):
+        c = Case(1, have, keep, 2, 64, torch.bfloat16, 16)
+        assert c.run(**bounds) == kept
+        c.verify(kept, seen)
+
+
+def test_the_least_workspace_and_one_of_more_planes():
+    """A workspace of a call with more planes is enough; the selection is the same."""
+    have, keep, planes = [90000], [30000], 2
+    c = Case(2, have, keep, planes, 64, torch.bfloat16, 16)
+    ws = torch.empty(l2kv.l2kv_paged_compress_workspace_bytes(65, 1, 90000, 30000) * planes // 65 + 64, dtype=torch.uint8, device=DEV)
+    assert len(ws) < l2kv.l2kv_paged_compress_workspace_bytes(planes, 1, 90000, 30000)
+    out = ints([0])
+    c.was = [x.clone() for x in c.cache]
+    l2kv.l2kv_paged_compress(*c.cache, ints(c.a), ints(have), ints(keep), ints(c.b), out, 16, 90000, 30000, 90000, ws)
+    assert out.tolist() == keep
+    c.verify(keep)
+
+
+def test_a_graph_of_long_sequences():
+    c = Case(3, [60000, 50000], [30000, 25000], 2, 64, torch.bfloat16, 32)
+    ws = torch.empty(l2kv.l2kv_paged_compress_workspace_bytes(2, 2, 110000, 55000), dtype=torch.uint8, device=DEV)
+    a, b, lens, keep, out = ints(c.a), ints(c.b), ints([60000, 50000]), ints([30000, 25000]), ints([0, 0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        l2kv.l2kv_paged_compress(*c.cache, a, lens, keep, b, out, 32, 110000, 55000, 60000, ws)
+    for counts, rows in (([30000, 25000], [60000, 50000]), ([0, 20000], [5, 45000]), ([29999, 1], [60000, 1])):
+        c.cache[2].normal_().abs_(), c.cache[0].normal_()
+        keep.copy_(ints(counts)), lens.copy_(ints(rows))
+        c.was = [x.clone() for x in c.cache]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert out.tolist() == counts
+        c.verify(counts, rows)
