@@ -2,15 +2,15 @@
 // pages of another table (arXiv 2406.11430, Sec. 1: keep the lowest-norm keys and their values).
 //
 // A workgroup selects for each (plane, sequence), with the norms in registers straight from their pages; kept rows are then copied from page to
-// page, 16 bytes a lane, with norms and token ids.  Few and longer sequences are selected from by several workgroups each, in three launches that
+// page, 16 bytes a lane, with norms and token ids.  Short sequences take one launch for both (select_copy_paged_kernel).  Few and longer sequences are selected from by several workgroups each, in three launches that
 // put the norms into one line per plane on the way (8 planes of 131072 rows, a tenth kept, 92 us with one workgroup a plane, 47 so; of 1000000
 // 722 and 232).  Many longer sequences, and very many, have their norms gathered first (4 bytes a row beside the 2 * row bytes of each kept
 // one) for the selection of ragged batches.  Source and destination are
 // other pages, so rows that several sequences share are only read, and nothing has to be read before it is written over.
 //
 // Bound by memory: 64 sequences of 1k to 8k bf16 rows of 128 in 8 planes, half kept, 254 us, 4.9 TB/s in and out with 15 us of selection (rows of
-// pages in order 217, as from plane to slots; pages in no order cost the difference, of 16 rows and of 256 alike).  One of 777
-// rows 9.3 us, two launches of dependent loads.
+// pages in order 217, as from plane to slots; pages in no order cost the difference, of 16 rows and of 256 alike).  Four
+// planes of 777 rows 6.7 us, a launch of dependent loads.
 #include "paged_rows.hpp"
 
 namespace l2kv {
@@ -177,6 +177,8 @@ size_t paged_compress_workspace_bytes(int64_t n_planes, int64_t n_seq, int64_t t
 l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, int32_t D, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     const CompressScratch w(workspace, a.n_planes, a.n_seq, a.total_rows);
     constexpr int64_t kMaxY = 65535;
+    const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
+    if (select_copy_paged_applies(a, row_bytes)) return select_copy_paged_dispatch(a, row_bytes, stream);
     if (a.max_len <= kPagedSelectRows && a.n_seq <= kPagedSelectSeq) {
         if (l2kv_status st = select_paged_dispatch(a, w, stream); st != L2KV_OK) return st;
     } else if (select_paged_split_applies(a) && workspace_bytes >= paged_compress_workspace_bytes(a.n_planes, a.n_seq, a.total_rows, a.total_kept)) {
@@ -200,7 +202,6 @@ l2kv_status paged_compress_dispatch(const PagedCompressArgs& a, l2kv_dtype dt, i
                 return st;
         }
     }
-    const int row_bytes = D * (dt == L2KV_F32 ? 4 : 2);
     const int64_t per_block = row_bytes == 128 ? kPcRowsPerBlock<128> : kPcRowsPerBlock<256>;
     static_assert(kPcRowsPerBlock<256> == kPcRowsPerBlock<512>, "one chunk size for rows of 16 lanes");
     const unsigned chunks = (unsigned)((a.total_kept + per_block - 1) / per_block);

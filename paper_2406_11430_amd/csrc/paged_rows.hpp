@@ -63,7 +63,11 @@ __device__ __forceinline__ int64_t slot_of(const int32_t* table, int32_t max_pag
 constexpr int64_t kPagedSelectRows = 32768, kPagedSelectSeq = 1024;
 l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScratch& w, hipStream_t stream);
 
-// The same of few and longer ones, each by several workgroups: whether it is one of those, what it needs beside the scratch memory above,
+// Selection and copy of short sequences in one launch: whether these are such, and the launch.
+bool select_copy_paged_applies(const PagedCompressArgs& a, int32_t row_bytes);
+l2kv_status select_copy_paged_dispatch(const PagedCompressArgs& a, int32_t row_bytes, hipStream_t stream);
+
+// Selection of few and longer ones, each by several workgroups: whether it is one of those, what it needs beside the scratch memory above,
 // 16-aligned (0: there is no such selection of these sizes), and the launch.
 bool select_paged_split_applies(const PagedCompressArgs& a);
 size_t select_paged_split_bytes(int64_t n_planes, int64_t n_seq, int64_t total_rows);

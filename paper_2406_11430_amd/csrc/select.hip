@@ -339,16 +339,10 @@ void select_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, uint32_t k
 }
 
 // ---- selection of a compaction in pages ---------------------------------------------------------
-// Grid (sequences, planes).  Every workgroup adds up the rows and the kept rows of the sequences before its own (64 of them: one round trip
-// beside the first one of the keys); those of the first plane leave them for the copy.
-template <int E>
-__global__ __launch_bounds__(kSelThreads)
-void select_paged_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
-    __shared__ __attribute__((aligned(16))) SearchShared s_search;
-    __shared__ EmitShared s_emit;
-    __shared__ int64_t s_sums[2][kSelThreads / kWaveSize];
-    const int32_t seq = blockIdx.x;
-    const int64_t plane = first_plane + blockIdx.y;
+// What the bounds leave of sequence `seq`.  Every workgroup adds up the rows and the kept rows of the sequences before its own (64 of them: one
+// round trip beside the first one of the keys).
+struct PagedSums { int64_t of[2][kSelThreads / kWaveSize]; };
+__device__ __forceinline__ Held paged_held(const PagedCompressArgs& a, int32_t seq, PagedSums& sums) {
     int64_t rows = 0, kept = 0;
     for (int32_t s = threadIdx.x; s < seq; s += kSelThreads) {
         const Rows r = rows_of(a, s);
@@ -357,12 +351,28 @@ void select_paged_kernel(const PagedCompressArgs a, CompressScratch w, int64_t f
     const Rows mine = rows_of(a, seq);
 #pragma unroll
     for (int d = 1; d < kWaveSize; d *= 2) rows += __shfl_xor(rows, d), kept += __shfl_xor(kept, d);
-    if (threadIdx.x % kWaveSize == 0) s_sums[0][threadIdx.x / kWaveSize] = rows, s_sums[1][threadIdx.x / kWaveSize] = kept;
+    if (threadIdx.x % kWaveSize == 0) sums.of[0][threadIdx.x / kWaveSize] = rows, sums.of[1][threadIdx.x / kWaveSize] = kept;
     __syncthreads();
     rows = kept = 0;
 #pragma unroll
-    for (int i = 0; i < kSelThreads / kWaveSize; ++i) rows += s_sums[0][i], kept += s_sums[1][i];
-    const Held h = held_of(a, mine, rows, kept);
+    for (int i = 0; i < kSelThreads / kWaveSize; ++i) rows += sums.of[0][i], kept += sums.of[1][i];
+    return held_of(a, mine, rows, kept);
+}
+template <int E> __device__ __forceinline__ HeadKeys<E> paged_keys(const PagedCompressArgs& a, int32_t seq, int64_t plane, int64_t have) {
+    const uint32_t* const norms = reinterpret_cast<const uint32_t*>(a.norms_c) + plane * ((int64_t)a.n_pages << a.page_shift);
+    return HeadKeys<E>(have, 0u, [&](uint32_t t) { return norms[slot_of(a.table_in, a.max_in, seq, t, a.page_shift, a.n_pages)]; });
+}
+
+// Grid (sequences, planes); the workgroups of the first plane leave places and lengths for the copy.
+template <int E>
+__global__ __launch_bounds__(kSelThreads)
+void select_paged_kernel(const PagedCompressArgs a, CompressScratch w, int64_t first_plane) {
+    __shared__ __attribute__((aligned(16))) SearchShared s_search;
+    __shared__ EmitShared s_emit;
+    __shared__ PagedSums s_sums;
+    const int32_t seq = blockIdx.x;
+    const int64_t plane = first_plane + blockIdx.y;
+    const Held h = paged_held(a, seq, s_sums);
     if (plane == 0 && threadIdx.x == 0) {
         w.in_off[seq] = h.in_first;
         w.out_off[seq] = h.out_first;
@@ -371,9 +381,8 @@ void select_paged_kernel(const PagedCompressArgs a, CompressScratch w, int64_t f
     }
     const uint32_t k = (uint32_t)h.keep;
     if (k == 0) return;
-    const uint32_t* const norms = reinterpret_cast<const uint32_t*>(a.norms_c) + plane * ((int64_t)a.n_pages << a.page_shift);
     int32_t* const out = w.kept + plane * a.total_kept + h.out_first;
-    const HeadKeys<E> keys(h.have, 0u, [&](uint32_t t) { return norms[slot_of(a.table_in, a.max_in, seq, t, a.page_shift, a.n_pages)]; });
+    const HeadKeys<E> keys = paged_keys<E>(a, seq, plane, h.have);
     const Threshold th = find_threshold(keys, k, s_search);
     emit_ordered<E, false>([&](int64_t e) { return keys.fetch(e); }, E, keys.t0, th.tau, th.need_eq, 0u, 0u,
                            [&](uint32_t i, int32_t t) { out[i] = t; }, k, s_emit);
@@ -531,6 +540,54 @@ void select_compact_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, ui
         select_and_copy_ahead<E, kRowBytes>(keys, k, first, count, ahead, K, kept_idx, Kc, Vc, sh);
     } else {
         select_and_copy<E, kRowBytes>(keys, k, first, count, K, V, kept_idx, Kc, Vc, sh);
+    }
+}
+
+// The same of sequences in pages.  Grid (shares of the kept rows, sequences, planes): how many rows a share has goes by what its sequence keeps.
+// (Shares of a size that the launch knows are too large for some sequences and leave workgroups of others without rows, which still take their
+// turn: 8 planes of 16 sequences of 2000 rows, a tenth kept, 21.6 us, 13.0 so.)  One workgroup on a compute unit: two, which the keys leave room
+// for, take longer to begin than they save (8 planes of 4 sequences of 1000 bf16 rows of 128, half kept, 12.7 us, 10.5 so; 14 MB of rows 20.0 and 20.9).
+// Against a selection and a copy of their own, up to 20 MB of kept rows of K: one plane of 100 rows 9.4 us, 6.9 in one launch, 4 of 777 10.5 and
+// 7.8, 8 of 4000 15 and 12.6, 256 sequences and planes of 500 22.5 and 20; beyond it, 8 planes of 4 sequences of 8000 35.3 and 38.1.
+constexpr int64_t kDeviceShares = 256;
+constexpr uint32_t kPagedLeastShare = 16;
+template <int E, int kRowBytes>
+__global__ __launch_bounds__(kSelThreads, 4)
+void select_copy_paged_kernel(const PagedCompressArgs a) {
+    __shared__ __attribute__((aligned(16))) FuseShared sh;
+    __shared__ PagedSums s_sums;
+    const int32_t seq = blockIdx.y;
+    const int64_t plane = blockIdx.z, slots = (int64_t)a.n_pages << a.page_shift;
+    const Held h = paged_held(a, seq, s_sums);
+    if (plane == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.lens_out[seq] = (int32_t)h.keep;
+    const uint32_t k = (uint32_t)h.keep, fair = (k + gridDim.x - 1) / gridDim.x;
+    const uint32_t per_share = fair < kPagedLeastShare ? kPagedLeastShare : fair, r0 = blockIdx.x * per_share;
+    if (r0 >= k) return;
+    const uint32_t rows = k - r0 < per_share ? k - r0 : per_share;
+    const HeadKeys<E> keys = paged_keys<E>(a, seq, plane, h.have);
+    const Threshold th = find_threshold(keys, k, sh.search);
+    emit_ordered<E, false>([&](int64_t e) { return keys.fetch(e); }, E, keys.t0, th.tau, th.need_eq, 0u, 0u,
+                           [&](uint32_t i, int32_t t) {
+                               if (i - r0 < rows) sh.row[i - r0] = (uint16_t)t;
+                           }, k, sh.emit);
+    __syncthreads();
+    using P = RowCopy<kRowBytes>;
+    constexpr uint32_t kRowsPerStep = kSelThreads / P::kLanes;
+    const uint32_t c = threadIdx.x % P::kLanes, rg = threadIdx.x / P::kLanes;
+    for (uint32_t r = rg; r < rows; r += kRowsPerStep) {
+        const int64_t src = plane * slots + slot_of(a.table_in, a.max_in, seq, sh.row[r], a.page_shift, a.n_pages);
+        const uint32_t out = r0 + r;
+        const int32_t page = a.table_out[(int64_t)seq * a.max_out + (out >> a.page_shift)];
+        const Words<P::kWords> x = load_words_stream<P::kWords, P::kStride>(a.Kc + src * kRowBytes + c * 16);
+        const Words<P::kWords> y = load_words_stream<P::kWords, P::kStride>(a.Vc + src * kRowBytes + c * 16);
+        if (page < 0 || page >= a.n_pages) continue;               // nothing is written where there is no page
+        const int64_t dst = plane * slots + ((int64_t)page << a.page_shift) + (out & ((1 << a.page_shift) - 1));
+        if (c == 0) {
+            a.norms_c[dst] = a.norms_c[src];
+            a.pos_c[dst] = a.pos_c[src];
+        }
+        store_words_stream<P::kWords, P::kStride>(a.Kc + dst * kRowBytes + c * 16, x);
+        store_words_stream<P::kWords, P::kStride>(a.Vc + dst * kRowBytes + c * 16, y);
     }
 }
 
@@ -1193,6 +1250,27 @@ l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScra
         if (l2kv_status st = launch_status(); st != L2KV_OK) return st;
     }
     return L2KV_OK;
+}
+
+bool select_copy_paged_applies(const PagedCompressArgs& a, int32_t row_bytes) {
+    const int64_t n_heads = (int64_t)a.n_planes * a.n_seq;
+    return a.max_len <= kFuseMaxTokens && n_heads <= (a.max_len <= 4 * kSelThreads ? kFuseMaxHeads : kFuseMaxHeads / 2) &&
+           a.n_planes * a.total_kept * row_bytes <= kFuseMaxBytes;
+}
+template <int E> static void launch_select_copy_paged(const PagedCompressArgs& a, int32_t row_bytes, hipStream_t stream) {
+    const int64_t shares = kDeviceShares / ((int64_t)a.n_planes * a.n_seq);        // at least 1: kFuseMaxHeads
+    const int64_t kept = a.max_len < a.total_kept ? a.max_len : a.total_kept, most = (kept + kPagedLeastShare - 1) / kPagedLeastShare;
+    const dim3 grid((unsigned)(shares < most ? shares : most), (unsigned)a.n_seq, (unsigned)a.n_planes);
+    auto kernel = row_bytes == 128 ? select_copy_paged_kernel<E, 128> : row_bytes == 256 ? select_copy_paged_kernel<E, 256> : select_copy_paged_kernel<E, 512>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kSelThreads), 0, stream, a);
+}
+l2kv_status select_copy_paged_dispatch(const PagedCompressArgs& a, int32_t row_bytes, hipStream_t stream) {
+    const int64_t per_lane = (a.max_len + kSelThreads - 1) / kSelThreads;
+    if (per_lane <= 1) launch_select_copy_paged<1>(a, row_bytes, stream);
+    else if (per_lane <= 2) launch_select_copy_paged<2>(a, row_bytes, stream);
+    else if (per_lane <= 4) launch_select_copy_paged<4>(a, row_bytes, stream);
+    else launch_select_copy_paged<8>(a, row_bytes, stream);
+    return launch_status();
 }
 
 l2kv_status select_ragged_dispatch(const float* norms, int32_t n_planes, int32_t n_seq,

@@ -202,3 +202,14 @@ def test_a_graph_of_long_sequences():
         torch.cuda.synchronize()
         assert out.tolist() == counts
         c.verify(counts, rows)
+
+
+@pytest.mark.parametrize("have,keep,planes", [([8192], [8192], 1), ([8193], [8192], 1), ([8192, 8192, 7], [1, 8192, 3], 2), ([4096], [4096], 200), ([30] * 256, [29] * 256, 1),
+                                              ([30] * 257, [29] * 257, 1), ([40, 0, 4000] * 20, [40, 5, 2000] * 20, 2), ([1], [1], 1)])
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 128)])
+def test_shares_of_short_sequences(have, keep, planes, dtype, D):
+    """The largest sequences, and the most of them, that are selected from and copied in one launch, and the next larger."""
+    c = Case(len(have), have, keep, planes, D, dtype, 16)
+    kept = [min(k, h) for k, h in zip(keep, have)]
+    assert c.run() == kept
+    c.verify(kept)
