@@ -49,6 +49,38 @@ struct PagesShared {
     int32_t top[kPageThreads];             // the first pages to be handed out, asked for ahead
 };
 
+// Where there are few entries, what is asked about their pages is counted in LDS, in the room that more entries would take: open addressing,
+// page, number of entries that name it, the last of them.  (Counted in memory, two round trips more: a step of 4 branches SEEN_OLD us, SEEN_NEW so.)
+constexpr int kSeenEntries = 2048, kSeenSlots = 4096, kSeenBits = 12;
+static_assert(kSeenEntries + kSeenSlots + kSeenSlots / 2 <= kKeptEntries, "room for pages, numbers and last entries");
+struct Seen {
+    PagesShared& sh;
+    __device__ __forceinline__ int32_t* page(uint32_t i) const { return sh.at + kSeenEntries + i; }
+    __device__ __forceinline__ int32_t* number(uint32_t i) const { return sh.page + kSeenEntries + i; }
+    __device__ __forceinline__ int32_t* last(uint32_t i) const {
+        return (i < kSeenSlots / 2 ? sh.at : sh.page) + kSeenEntries + kSeenSlots + i % (kSeenSlots / 2);
+    }
+    __device__ __forceinline__ void clear() const {
+        for (uint32_t i = threadIdx.x; i < kSeenSlots; i += kPageThreads) *page(i) = -1, *number(i) = 0, *last(i) = -1;
+    }
+    static __device__ __forceinline__ uint32_t first(int32_t p) { return (uint32_t)p * 2654435769u >> (32 - kSeenBits); }
+    __device__ __forceinline__ void add(int32_t p, int32_t at) const {
+        uint32_t i = first(p);
+        for (;; i = (i + 1) % kSeenSlots) {                    // half of the slots stay free
+            int32_t was = -1;
+            if (__hip_atomic_compare_exchange_strong(page(i), &was, p, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) || was == p) break;
+        }
+        (void)__hip_atomic_fetch_add(number(i), 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        (void)__hip_atomic_fetch_max(last(i), at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    // of a page that was added
+    __device__ __forceinline__ uint32_t find(int32_t p) const {
+        uint32_t i = first(p);
+        while (*page(i) != p) i = (i + 1) % kSeenSlots;
+        return i;
+    }
+};
+
 // Inclusive prefix sum over the workgroup, and the sum of all; below 2^31.
 __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t (&waves)[kPageWaves], int32_t& total) {
     const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
@@ -144,10 +176,12 @@ template <typename R> struct AllEntries {
     const PagesArgs& a;
     R range;
     int32_t total;
-    bool kept;
+    bool kept, few;
     __device__ __forceinline__ AllEntries(PagesShared& sh_, const PagesArgs& a_, R range_) : sh(sh_), a(a_), range(range_) {
+        Seen{sh}.clear();
         total = lay_out(sh, 0, a.n_seq, range);
         kept = a.n_seq <= kPageThreads && total <= kKeptEntries;
+        few = kept && total <= kSeenEntries;
         if (!kept) return;
         for (int32_t e0 = 0; e0 < total; e0 += kEntries) {
             Entries x;
@@ -254,12 +288,20 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         for (int k = 0; k < kPer; ++k) {
             if (x.page[k] < 0) continue;
             shared |= refs[k] != 1;
+            if (all.few) continue;
             own_store(w.left + x.page[k], refs[k] - 1);             // the same whoever does it: without the one who asks
             own_store(w.last + x.page[k], -1);
         }
     });
     shared = __syncthreads_or(shared) != 0;
-    if (shared) {
+    const Seen seen{sh};
+    if (shared && all.few) {
+        all.each([&](const Entries& x, int32_t) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (x.page[k] >= 0) seen.add(x.page[k], x.at[k]);
+        });
+    } else if (shared) {
         all.each([&](const Entries& x, int32_t) {
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
@@ -275,8 +317,16 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         int32_t left[kPer], last[kPer];
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
-            left[k] = shared && x.page[k] >= 0 ? own_load(w.left + x.page[k]) : -1;
-            last[k] = shared && x.page[k] >= 0 ? own_load(w.last + x.page[k]) : x.at[k];
+            left[k] = -1, last[k] = x.at[k];
+            if (!shared || x.page[k] < 0) continue;
+            if (all.few) {
+                const uint32_t i = seen.find(x.page[k]);
+                left[k] = own_load(a.refs + x.page[k]) - 1 - *seen.number(i);
+                last[k] = *seen.last(i);
+            } else {
+                left[k] = own_load(w.left + x.page[k]);
+                last[k] = own_load(w.last + x.page[k]);
+            }
         }
 #pragma unroll
         for (int k = 0; k < kPer; ++k) want[k] = x.at[k] >= 0 && (x.page[k] < 0 || left[k] >= 0 || last[k] != x.at[k]);
@@ -397,17 +447,24 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
         count = a.max_pages - first;
     };
     AllEntries every(sh, a, range);
-    every.each([&](const Entries& x, int32_t) {
+    const Seen seen{sh};
+    if (!every.few) {
+        every.each([&](const Entries& x, int32_t) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
-            if (x.page[k] >= 0) own_store(w.last + x.page[k], -1);
-    });
+            for (int k = 0; k < kPer; ++k)
+                if (x.page[k] >= 0) own_store(w.last + x.page[k], -1);
+        });
+    }
     every.each([&](const Entries& x, int32_t) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             if (x.page[k] < 0) continue;
-            own_add(a.refs + x.page[k], -1);
-            own_max(w.last + x.page[k], x.at[k]);
+            if (every.few) {
+                seen.add(x.page[k], x.at[k]);
+            } else {
+                own_add(a.refs + x.page[k], -1);
+                own_max(w.last + x.page[k], x.at[k]);
+            }
         }
     });
     // Of the entries that name a page without holders the last gives it back; the first of these on top.
@@ -416,7 +473,16 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             refs[k] = x.page[k] < 0 ? 1 : own_load(a.refs + x.page[k]);
-            last[k] = x.page[k] < 0 ? 0 : own_load(w.last + x.page[k]);
+            last[k] = x.page[k] < 0 || every.few ? 0 : own_load(w.last + x.page[k]);
+        }
+        if (every.few) {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                if (x.page[k] < 0) continue;
+                const uint32_t i = seen.find(x.page[k]);
+                refs[k] -= *seen.number(i), last[k] = *seen.last(i);
+                if (last[k] == x.at[k]) own_store(a.refs + x.page[k], refs[k]);      // asked about once; who is not the last does not look
+            }
         }
 #pragma unroll
         for (int k = 0; k < kPer; ++k) mine[k] = x.page[k] >= 0 && refs[k] <= 0 && last[k] == x.at[k];
