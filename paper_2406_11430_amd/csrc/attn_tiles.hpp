@@ -307,21 +307,30 @@ template <typename E> __device__ __forceinline__ f32x16_t value_product(const u3
 // bits whatever they are.  Returns whether there are others.
 template <typename E, int D>
 __device__ __forceinline__ bool finite_values(const char* tile, const TileAddress<E, D>& at, const Weights<E>& p, f32x16_t (&o)[D / kTile]) {
+    // Rows of 512 bytes come here with every masked tile: as many operands at a time as there are
+    // registers for (one by one, and with the queries read again for every tile as bf16 has to, an fp32 prompt of 2000 tokens of 128 elements 96 us, 87 so).
+    constexpr bool kLong = AttnRow<E, D>::kBytes == 512;
+    constexpr int kTogether = !kLong ? 1 : (E::kBytes == 2 ? 2 : D / kTile), kSteps = kLong && E::kBytes == 4 ? 16 : 1;
     uint32_t any = 0;
-#pragma unroll 1
+#pragma unroll kSteps
     for (int t = 0; t < (E::kBytes == 2 ? 2 : 16); ++t) {
         const u32x4_t w = weights_operand<E>(p, t);
 #pragma unroll
-        for (int d = 0; d < D / kTile; ++d) {
-            u32x4_t v = values_operand<E, D>(tile, at, t, d);
+        for (int d0 = 0; d0 < D / kTile; d0 += kTogether) {
+            u32x4_t v[kTogether];
 #pragma unroll
-            for (int i = 0; i < (E::kBytes == 2 ? 4 : 1); ++i) {
-                const uint32_t bad = not_finite_bits<E>(v[i]);
-                v[i] &= ~bad;
-                any |= bad;
+            for (int d = 0; d < kTogether; ++d) v[d] = values_operand<E, D>(tile, at, t, d0 + d);
+#pragma unroll
+            for (int d = 0; d < kTogether; ++d) {
+#pragma unroll
+                for (int i = 0; i < (E::kBytes == 2 ? 4 : 1); ++i) {
+                    const uint32_t bad = not_finite_bits<E>(v[d][i]);
+                    v[d][i] &= ~bad;
+                    any |= bad;
+                }
+                o[d0 + d] = value_product<E>(v[d], w, o[d0 + d]);
             }
-            o[d] = value_product<E>(v, w, o[d]);
-            __builtin_amdgcn_sched_barrier(0);                     // one product at a time: registers
+            __builtin_amdgcn_sched_barrier(0);                     // no more of them at a time: registers
         }
     }
     return __ballot(any != 0) != 0;

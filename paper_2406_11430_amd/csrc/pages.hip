@@ -8,8 +8,8 @@
 // The tables are small (64 sequences of 500 pages: 128 KB) and every decision needs all those before it, so one workgroup works through them,
 // 1024 sequences and 2048 entries at a time; up to 8192 entries stay in LDS from phase to phase.  It is bound by the
 // memory round trips that follow one another and by the fetch of its own instructions.  The copies are a launch of their own behind it.
-// One more row for each of 64 sequences 8 us with the (empty) copy; release, fork and reservation of 32 branches of 1000 to 2000 rows with 34 MB copied, 34 us:
-// 6 + 2 + 8 and the copy 13, at 5.2 TB/s.
+// One more row for each of 64 sequences 8 us with the (empty) copy; release, fork and reservation of 32 branches of 1000 to 2000 rows with 34 MB copied, 33 us:
+// 5 + 2 + 8 and the copy 13, at 5.2 TB/s.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 
@@ -50,7 +50,8 @@ struct PagesShared {
 };
 
 // Where there are few entries, what is asked about their pages is counted in LDS, in the room that more entries would take: open addressing,
-// page, number of entries that name it, the last of them.  (Counted in memory, two round trips more: a step of 4 branches SEEN_OLD us, SEEN_NEW so.)
+// page, number of entries that name it, the last of them.  (Counted in memory, two round trips more: a step of 32 branches with
+// copies 35.3 us, 33.2 so.)
 constexpr int kSeenEntries = 2048, kSeenSlots = 4096, kSeenBits = 12;
 static_assert(kSeenEntries + kSeenSlots + kSeenSlots / 2 <= kKeptEntries, "room for pages, numbers and last entries");
 struct Seen {

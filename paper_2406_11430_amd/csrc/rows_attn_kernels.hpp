@@ -403,7 +403,7 @@ void rows_attn_kernel(const RowsArgs a) {
                 const uint32_t bits = seen(nodes, k0 + sub);
                 if (__ballot(bits != 0) == 0) continue;
                 TileAddress<E, D> at = place;
-                if constexpr (R::kBytes == 512) {
+                if constexpr (R::kBytes == 512 && E::kBytes == 2) {
                     // queries are read again and places worked out again instead of held: registers, for the few tiles with masks
                     int32_t again = row;
                     asm volatile("" : "+v"(again));
