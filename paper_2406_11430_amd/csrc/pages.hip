@@ -8,8 +8,8 @@
 // The tables are small (64 sequences of 500 pages: 128 KB) and every decision needs all those before it, so one workgroup works through them,
 // 1024 sequences and 2048 entries at a time; up to 8192 entries stay in LDS from phase to phase.  It is bound by the
 // memory round trips that follow one another and by the fetch of its own instructions.  The copies are a launch of their own behind it.
-// One more row for each of 64 sequences 8 us with the (empty) copy; release, fork and reservation of 32 branches of 1000 to 2000 rows with 34 MB copied, 33 us:
-// 5 + 2 + 8 and the copy 13, at 5.2 TB/s.
+// One more row for each of 64 sequences 8 us with the (empty) copy; release, fork and reservation of 32 branches of 1000 to 2000 rows with 34 MB copied, 32 us:
+// 5 + 2 + 7 and the copy 13, at 5.2 TB/s.
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 
@@ -51,7 +51,8 @@ struct PagesShared {
 
 // Where there are few entries, what is asked about their pages is counted in LDS, in the room that more entries would take: open addressing,
 // page, number of entries that name it, the last of them.  (Counted in memory, two round trips more: a step of 32 branches with
-// copies 35.3 us, 33.2 so.)
+// copies 35.3 us, 33.2 so.)  And as all of them come at once,
+// what one pass has found out of them the next has in registers (32.0).
 constexpr int kSeenEntries = 2048, kSeenSlots = 4096, kSeenBits = 12;
 static_assert(kSeenEntries + kSeenSlots + kSeenSlots / 2 <= kKeptEntries, "room for pages, numbers and last entries");
 struct Seen {
@@ -109,6 +110,7 @@ __device__ __forceinline__ bool is_page(int32_t p, int32_t n_pages) { return p >
 // sequence's last.  (Two: a kernel that works through eight is 33 KB of instructions that every call fetches anew, 41 us a step of 32 branches,
 // 31 so; with one tables of 64 sequences of 250 pages take 114 us, 100 with two.)
 constexpr int kPer = 2, kEntries = kPageThreads * kPer;
+static_assert(kSeenEntries <= kEntries, "few entries come once");
 struct Entries {
     int32_t at[kPer], seq[kPer], page[kPer];
     bool last[kPer];
@@ -268,12 +270,15 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
                           void* workspace) {
     __shared__ PagesShared sh;
     const PagesScratch w(workspace, a.n_pages);
+    // the rows of the first sequences beside the number of free pages, not behind it
+    const bool early = (int32_t)threadIdx.x < a.n_seq;
+    const int32_t early_from = early ? from[threadIdx.x] : 0, early_to = early ? to[threadIdx.x] : 0;
     int32_t have = *a.free_count;
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
     const int32_t top = (int32_t)threadIdx.x < have ? a.free_pages[have - 1 - (int32_t)threadIdx.x] : -1;
     int32_t own_from = 0, own_to = 0;                          // of the sequence that `range` was asked about last
     auto range = [&](int32_t s, int32_t& first, int32_t& count) {
-        const int64_t b = own_from = from[s], e = own_to = to[s];
+        const int64_t b = own_from = s < kPageThreads ? early_from : from[s], e = own_to = s < kPageThreads ? early_to : to[s];
         if (b < 0 || e <= b || e > (int64_t)a.max_pages << a.page_shift) return;
         first = (int32_t)(b >> a.page_shift);
         count = (int32_t)((e - 1) >> a.page_shift) - first + 1;
@@ -333,6 +338,8 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         for (int k = 0; k < kPer; ++k) want[k] = x.at[k] >= 0 && (x.page[k] < 0 || left[k] >= 0 || last[k] != x.at[k]);
     };
     int32_t base = 0;                                          // new pages wanted by the sequences before these
+    bool once_want[kPer];                                      // of few entries: what the first pass has found out of the lane's
+    int32_t once_upto = 0;
     if (threadIdx.x == 0) sh.handed = sh.copied = 0;
     for (int32_t s0 = 0; s0 < a.n_seq; s0 += kPageThreads) {
         if (!all.kept) all.total = lay_out(sh, s0, a.n_seq, range);
@@ -347,8 +354,10 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
             const int32_t mine = all.flags_of(x, e0, true, want, wanted);
             int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
             sum += these;
+            once_upto = so_far;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
+                once_want[k] = want[k];
                 so_far += want[k] ? 1 : 0;
                 if (want[k]) (void)__hip_atomic_fetch_add(&sh.need[x.seq[k]], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                 if (x.last[k]) sh.news[x.seq[k]] = so_far;
@@ -359,9 +368,16 @@ void pages_reserve_kernel(const PagesArgs a, const int32_t* __restrict__ from, c
         sum = base;
         all.each_of(s0, [&](const Entries& x, int32_t e0) {
             bool want[kPer];
-            const int32_t mine = all.flags_of(x, e0, false, want, wanted);
-            int32_t these, so_far = sum + block_prefix(mine, sh.waves, these) - mine;
-            sum += these;
+            int32_t so_far = once_upto;
+            if (all.few) {
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) want[k] = once_want[k];
+            } else {
+                const int32_t mine = all.flags_of(x, e0, false, want, wanted);
+                int32_t these;
+                so_far = sum + block_prefix(mine, sh.waves, these) - mine;
+                sum += these;
+            }
             int32_t page[kPer], number[kPer], most = 0;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
@@ -490,17 +506,20 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
     };
     have = have < 0 ? 0 : (have > a.n_pages ? a.n_pages : have);
     int32_t all = 0, sum = 0;
+    if (!every.few) {
+        every.each([&](const Entries& x, int32_t e0) {
+            bool mine[kPer];
+            int32_t these;
+            (void)block_prefix(every.flags_of(x, e0, true, mine, freed), sh.waves, these);
+            all += these;
+        });
+    }
     every.each([&](const Entries& x, int32_t e0) {
         bool mine[kPer];
         int32_t these;
-        (void)block_prefix(every.flags_of(x, e0, true, mine, freed), sh.waves, these);
-        all += these;
-    });
-    every.each([&](const Entries& x, int32_t e0) {
-        bool mine[kPer];
-        int32_t these;
-        int32_t upto = sum + block_prefix(every.flags_of(x, e0, false, mine, freed), sh.waves, these);
+        int32_t upto = sum + block_prefix(every.flags_of(x, e0, every.few, mine, freed), sh.waves, these);
         sum += these;
+        if (every.few) all = these;                            // few entries come once, all together
 #pragma unroll
         for (int k = kPer - 1; k >= 0; --k) {
             if (mine[k]) {
