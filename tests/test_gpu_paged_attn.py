@@ -237,3 +237,19 @@ def test_scale_and_no_workspace():
     O = torch.empty_like(c.Q)
     l2kv.l2kv_paged_attn(c.Q, c.Kc, c.Vc, offsets(c.new), ints(c.table), 16, ints(c.rows), 300, O, None, 0.7)
     c.verify(O, scale=0.7)
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("rows", [[700, 40, 9, 300, 1, 60], [5000, 40, 9, 3000, 1, 60]])
+def test_padded_single_tokens_any_distance_apart(dtype, D, rows):
+    """A batch of single tokens with sequences that have none, fewer tokens than the buffers, queries out of wider rows, lengths beyond the bound."""
+    new = [1, 0, 0, 1, 0, 1]
+    c = Case(31, new, rows, 4, 2, D, dtype, 16)
+    wide = torch.full((5, 7, D), float("nan"), dtype=dtype, device=DEV)
+    wide[:3, 2:6] = c.Q
+    for top in (max(rows), 600):
+        O = torch.full((5, 4, D), 7.0, dtype=dtype, device=DEV)
+        ws = torch.full((l2kv.l2kv_paged_attn_workspace_bytes(6, 4, 2, 5, top, D, dtype),), 0xff, dtype=torch.uint8, device=DEV)
+        l2kv.l2kv_paged_attn(wide[:, 2:6], c.Kc, c.Vc, offsets(new), ints(c.table), 16, ints(rows), top, O, ws)
+        c.verify(O[:3])
+        assert (O[3:] == 7).all()

@@ -126,9 +126,9 @@ def test_nothing_asked_for(first, to):
     assert p.reserve(t, first, to) == first and int(p.count) == 10
 
 
-@pytest.mark.parametrize("n_seq,width,page", [(1, 2000, 16), (65, 40, 16), (1030, 5, 32), (2500, 3, 16), (40, 500, 16), (3000, 11, 16), (3, 7000, 16)])
+@pytest.mark.parametrize("n_seq,width,page", [(1, 2000, 16), (65, 40, 16), (1030, 5, 32), (2500, 3, 16), (2, 1024, 16), (1, 2049, 16), (3, 1000, 32), (8, 512, 16), (1024, 2, 16), (40, 500, 16), (3000, 11, 16), (3, 7000, 16)])
 def test_many_entries(n_seq, width, page):
-    """More than 1024 sequences and more than 1024 entries, random lengths, forks and releases."""
+    """More than 1024 sequences and more entries than a pass, LDS or a workgroup takes, random lengths, forks and releases."""
     rng = random.Random(n_seq)
     n_pages = 3 * n_seq * width // 2 + 5
     p = Pool(n_pages, page, 1, 64, torch.bfloat16)
