@@ -548,8 +548,9 @@ void select_compact_kernel(const uint32_t* __restrict__ norm_bits, int64_t T, ui
 // turn: 8 planes of 16 sequences of 2000 rows, a tenth kept, 21.6 us, 13.0 so.)  One workgroup on a compute unit: two, which the keys leave room
 // for, take longer to begin than they save (8 planes of 4 sequences of 1000 bf16 rows of 128, half kept, 12.7 us, 10.5 so; 14 MB of rows 20.0 and 20.9).
 // Against a selection and a copy of their own, up to 20 MB of kept rows of K: one plane of 100 rows 9.4 us, 6.9 in one launch, 4 of 777 10.5 and
-// 7.8, 8 of 4000 15 and 12.6, 256 sequences and planes of 500 22.5 and 20; beyond it, 8 planes of 4 sequences of 8000 35.3 and 38.1.
+// 7.8, 8 of 4000 15 and 12.6, 256 sequences and planes of 500 22.5 and 20, one of 32768 36.9 and 23.9; beyond it, 8 planes of 4 sequences of 8000 35.3 and 38.1.
 constexpr int64_t kDeviceShares = 256;
+constexpr int kFuseLongHeads = 32;                     // of more than 8192 rows
 constexpr uint32_t kPagedLeastShare = 16;
 template <int E, int kRowBytes>
 __global__ __launch_bounds__(kSelThreads, 4)
@@ -1252,10 +1253,12 @@ l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScra
     return L2KV_OK;
 }
 
+// Indices of a share in LDS: of the longest sequences so many shares that they fit.
 bool select_copy_paged_applies(const PagedCompressArgs& a, int32_t row_bytes) {
     const int64_t n_heads = (int64_t)a.n_planes * a.n_seq;
-    return a.max_len <= kFuseMaxTokens && n_heads <= (a.max_len <= 4 * kSelThreads ? kFuseMaxHeads : kFuseMaxHeads / 2) &&
-           a.n_planes * a.total_kept * row_bytes <= kFuseMaxBytes;
+    static_assert(kPagedSelectRows <= 65536 && kPagedSelectRows <= kFuseRows * (kDeviceShares / kFuseLongHeads), "16-bit indices, room for a share's");
+    return n_heads <= (a.max_len <= 4 * kSelThreads ? kFuseMaxHeads : a.max_len <= kFuseMaxTokens ? kFuseMaxHeads / 2 : kFuseLongHeads) &&
+           a.max_len <= kPagedSelectRows && a.n_planes * a.total_kept * row_bytes <= kFuseMaxBytes;
 }
 template <int E> static void launch_select_copy_paged(const PagedCompressArgs& a, int32_t row_bytes, hipStream_t stream) {
     const int64_t shares = kDeviceShares / ((int64_t)a.n_planes * a.n_seq);        // at least 1: kFuseMaxHeads
@@ -1269,7 +1272,9 @@ l2kv_status select_copy_paged_dispatch(const PagedCompressArgs& a, int32_t row_b
     if (per_lane <= 1) launch_select_copy_paged<1>(a, row_bytes, stream);
     else if (per_lane <= 2) launch_select_copy_paged<2>(a, row_bytes, stream);
     else if (per_lane <= 4) launch_select_copy_paged<4>(a, row_bytes, stream);
-    else launch_select_copy_paged<8>(a, row_bytes, stream);
+    else if (per_lane <= 8) launch_select_copy_paged<8>(a, row_bytes, stream);
+    else if (per_lane <= 16) launch_select_copy_paged<16>(a, row_bytes, stream);
+    else launch_select_copy_paged<32>(a, row_bytes, stream);
     return launch_status();
 }
 

@@ -213,3 +213,13 @@ def test_shares_of_short_sequences(have, keep, planes, dtype, D):
     kept = [min(k, h) for k, h in zip(keep, have)]
     assert c.run() == kept
     c.verify(kept)
+
+
+@pytest.mark.parametrize("have,planes", [([900], 300), ([2000, 3], 150), ([4000], 260), ([8000], 130), ([20000, 9000], 20), ([16000], 33), ([32768], 33), ([32768], 32), ([16001], 32)])
+@pytest.mark.parametrize("ties", [False, True])
+def test_many_planes(have, planes, ties):
+    """As many heads as the selection and the copy go apart for, at every number of keys of a lane, and the most that go together."""
+    keep = [h // 10 for h in have]
+    c = Case(planes, have, keep, planes, 64, torch.bfloat16, 16, ties)
+    assert c.run() == keep
+    c.verify(keep)
