@@ -1253,15 +1253,21 @@ l2kv_status select_paged_dispatch(const PagedCompressArgs& a, const CompressScra
     return L2KV_OK;
 }
 
-// Indices of a share in LDS: of the longest sequences so many shares that they fit.
+static int64_t paged_shares(const PagedCompressArgs& a) { return kDeviceShares / ((int64_t)a.n_planes * a.n_seq); }
+// Not where what a share of the longest sequence copies, if all keep alike, takes longer than the launch that it saves (20 MB of K on the whole
+// device; 4 planes of 22 sequences of 1 to 4827 rows, 0.3 kept, 27.3 us apart and 38 together).
+// Indices of a share are in LDS: of the longest sequences so many shares that they fit.
 bool select_copy_paged_applies(const PagedCompressArgs& a, int32_t row_bytes) {
     const int64_t n_heads = (int64_t)a.n_planes * a.n_seq;
     static_assert(kPagedSelectRows <= 65536 && kPagedSelectRows <= kFuseRows * (kDeviceShares / kFuseLongHeads), "16-bit indices, room for a share's");
-    return n_heads <= (a.max_len <= 4 * kSelThreads ? kFuseMaxHeads : a.max_len <= kFuseMaxTokens ? kFuseMaxHeads / 2 : kFuseLongHeads) &&
-           a.max_len <= kPagedSelectRows && a.n_planes * a.total_kept * row_bytes <= kFuseMaxBytes;
+    if (n_heads > (a.max_len <= 4 * kSelThreads ? kFuseMaxHeads : a.max_len <= kFuseMaxTokens ? kFuseMaxHeads / 2 : kFuseLongHeads) ||
+        a.max_len > kPagedSelectRows)
+        return false;
+    const double longest = (double)a.total_kept * (double)a.max_len / (double)a.total_rows;
+    return longest * row_bytes <= (double)paged_shares(a) * (double)(kFuseMaxBytes / kDeviceShares);
 }
 template <int E> static void launch_select_copy_paged(const PagedCompressArgs& a, int32_t row_bytes, hipStream_t stream) {
-    const int64_t shares = kDeviceShares / ((int64_t)a.n_planes * a.n_seq);        // at least 1: kFuseMaxHeads
+    const int64_t shares = paged_shares(a);                    // at least 1: kFuseMaxHeads
     const int64_t kept = a.max_len < a.total_kept ? a.max_len : a.total_kept, most = (kept + kPagedLeastShare - 1) / kPagedLeastShare;
     const dim3 grid((unsigned)(shares < most ? shares : most), (unsigned)a.n_seq, (unsigned)a.n_planes);
     auto kernel = row_bytes == 128 ? select_copy_paged_kernel<E, 128> : row_bytes == 256 ? select_copy_paged_kernel<E, 256> : select_copy_paged_kernel<E, 512>;

@@ -223,3 +223,11 @@ def test_many_planes(have, planes, ties):
     c = Case(planes, have, keep, planes, 64, torch.bfloat16, 16, ties)
     assert c.run() == keep
     c.verify(keep)
+
+
+def test_uneven_batches():
+    """One long sequence among short ones, kept alike and not."""
+    for keep in ([1400, 3, 10, 0, 200], [4800, 1, 30, 9, 1], [1, 11, 30, 9, 650]):
+        c = Case(sum(keep), [4827, 11, 30, 9, 650], keep, 20, 128, torch.bfloat16, 64)
+        assert c.run() == keep
+        c.verify(keep)
