@@ -43,8 +43,14 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
 //   64 of 700 (D 64, groups of 3)       18.2 / 32.8 / 22.9 / 20.6      64 of 500 to 4000         105 / 143 / 102 / 102
 //   1 of 8192                            109 / 17.8 / 17.0 / 19.6      256 of 500 to 700         120 / 193 / 122 / 122
 constexpr int kTokens = 3;                 // the shape of such launches
-constexpr int64_t kTokenOwnRows = 512, kTokenOwnRowsMany = 1024;
-static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int64_t total_q, int64_t max_kv, int32_t D, int row_bytes) {
+// The rows at which both take as long go by what a row costs a workgroup, its bytes and the heads it is for: bf16 D 128 with groups of 1 800, of 8
+// 470, D 64 of 8 780, D 256 of 3 380, fp32 D 128 of 7 340; twice as many where there are
+// items for all compute units.  Over 140 sizes what this chooses takes 1.4 % longer than the better of the two (512 and 1024 rows for all: 3.5 %).
+static int64_t token_own_rows(int32_t G, int row_bytes, bool many) {
+    const int64_t few = 900 * 9 * 256 / ((row_bytes < 192 ? 192 : row_bytes) * (8 + G));
+    return many ? 2 * few : few;
+}
+static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64_t max_kv, int32_t D, int row_bytes) {
     const int64_t units = device_compute_units(), items = total_q * Hkv;
     const int32_t keys = row_bytes == 128 ? TokenGeometry<BF16, 64>::kBlock : TokenGeometry<BF16, 128>::kBlock;
     RowsPlan p = {};
@@ -53,7 +59,7 @@ static RowsPlan token_plan(int32_t n_seq, int32_t Hkv, int64_t total_q, int64_t 
     p.n_blocks = (int32_t)(total_q + n_seq);
     p.least_tiles = rows_item_tiles(false) + 1;
     // the search for a stretch's beginning goes over all sequences
-    if (n_seq <= 1024 && max_kv > (items >= 2 * units ? kTokenOwnRowsMany : kTokenOwnRows)) {
+    if (n_seq <= 1024 && max_kv > token_own_rows(G, row_bytes, items >= units)) {
         const int64_t most = items * (max_kv / keys + 2) / 2;
         p.workgroups = (int32_t)(most < units ? most : units);
     }
@@ -86,7 +92,7 @@ RowsPlan rows_plan(int32_t n_seq, int32_t Hkv, int32_t G, int64_t total_q, int64
     // the smallest block that takes the rows of a sequence, somewhat more than the average where there are several
     const int64_t rows = mean * G, room = n_seq == 1 ? rows : rows + rows / 4;
     // (a launch has fewer than 2^32 lanes)
-    if (kind == kRowsPaged && total_q <= n_seq && (total_q + n_seq) * Hkv < (1 << 24)) return token_plan(n_seq, Hkv, total_q, max_kv, D, row_bytes);
+    if (kind == kRowsPaged && total_q <= n_seq && (total_q + n_seq) * Hkv < (1 << 24)) return token_plan(n_seq, Hkv, G, total_q, max_kv, D, row_bytes);
     RowsPlan p;
     p.shape = kNarrowest;
     while (p.shape > 0 && sizes(p.shape).rows < room) --p.shape;
