@@ -601,7 +601,8 @@ l2kv_status l2kv_stream_append_path(const void* Kt, const void* Vt, const float*
  * page_table: DEVICE int32 [n_seq][max_pages], the same for all planes (layers and KV heads); -1 where there is no page.
  * A sequence has at most max_pages * page_size rows (at most 2^31-1).  An entry that is no page's number is forced into
  * them where rows are read, and takes no row where they are written.  Several sequences may hold the same page: who
- * writes rows first asks l2kv_pages_reserve for them.
+ * writes rows first asks l2kv_pages_reserve for them, and writes those only that it was given: a sequence whose request is refused
+ * still names the pages that it shares, and what is written there reaches all who hold them.  l2kv_paged_append_reserved takes what was given.
  * ------------------------------------------------------------------------ */
 
 /*
@@ -639,6 +640,23 @@ l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_
                               const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
                               int32_t page_size, int32_t n_pages, const int32_t* lens_in, int32_t* lens_out,
                               void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream);
+
+/*
+ * The same within what l2kv_pages_reserve gave: rows from ends[s] on are not stored either, whatever their entries say, and
+ * lens_out[s] ends before them.  So where free pages do not suffice, sequences without room keep their length, and nobody
+ * writes a page that others hold, without a word from the device in between.
+ *   ends : DEVICE int32 [n_seq], NULL: no such ends (l2kv_paged_append); must not be lens_out, may be lens_in (nothing is stored)
+ * Errors: as l2kv_paged_append.
+ */
+l2kv_status l2kv_paged_append_reserved(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                                       int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                                       const int32_t* positions, const double* freqs, int32_t rot_dim,
+                                       l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                                       const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
+                                       int32_t page_size, int32_t n_pages, const int32_t* lens_in, const int32_t* ends,
+                                       int32_t* lens_out, void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c,
+                                       void* stream);
 
 /*
  * Attention of the last tokens of every sequence, one or many, over all its rows in pages: l2kv_prompt_attn with the

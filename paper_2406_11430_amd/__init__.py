@@ -14,7 +14,7 @@ from .binding import (  # noqa: F401
     l2kv_norm_ranks, l2kv_norm_ranks_workspace_bytes, l2kv_alr, l2kv_alr_workspace_bytes,
     l2kv_length_order, l2kv_decode_attn_static, l2kv_device_info, l2kv_compress, l2kv_decode_attn_out, l2kv_read_probe,
     l2kv_rotary_freqs, l2kv_rotary_append, l2kv_prompt_attn, l2kv_prompt_attn_workspace_bytes, l2kv_tree_attn,
-    l2kv_tree_attn_workspace_bytes, l2kv_stream_append_path, l2kv_norm_rotary_append, l2kv_paged_append, l2kv_paged_attn,
-    l2kv_paged_attn_workspace_bytes, l2kv_pages_init, l2kv_pages_fork, l2kv_pages_reserve, l2kv_pages_release,
+    l2kv_tree_attn_workspace_bytes, l2kv_stream_append_path, l2kv_norm_rotary_append, l2kv_paged_append,
+    l2kv_paged_append_reserved, l2kv_paged_attn, l2kv_paged_attn_workspace_bytes, l2kv_pages_init, l2kv_pages_fork, l2kv_pages_reserve, l2kv_pages_release,
     l2kv_pages_workspace_bytes, l2kv_paged_compress, l2kv_paged_compress_workspace_bytes,
 )

@@ -111,6 +111,12 @@ SIGNATURES = {
                                     C.c_double, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                     C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p]),
+    "l2kv_paged_append_reserved": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int32,
+                                             C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                             C.c_void_p, C.c_double, C.c_void_p, C.c_void_p, C.c_int32, C.c_int,
+                                             C.c_double, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                             C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "l2kv_paged_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
@@ -160,7 +166,7 @@ _calls = None
 class _PythonCalls:
     """In place of the native calls: leaves every call to the checks and the marshalling in this file."""
     decode_attn = decode_attn_out = compress = rotary_append = prompt_attn = tree_attn = append_path = staticmethod(lambda *args: None)
-    norm_rotary_append = paged_append = paged_attn = pages_fork = pages_reserve = pages_release = paged_compress = staticmethod(lambda *args: None)
+    norm_rotary_append = paged_append = paged_append_reserved = paged_attn = pages_fork = pages_reserve = pages_release = paged_compress = staticmethod(lambda *args: None)
 
 
 def _load_calls():
@@ -186,7 +192,8 @@ def calls():
                 handle.l2kv_decode_attn, handle.l2kv_decode_attn_out, handle.l2kv_compress, handle.l2kv_keep_count,
                 handle.l2kv_rotary_append, handle.l2kv_prompt_attn, handle.l2kv_tree_attn, handle.l2kv_stream_append_path,
                 handle.l2kv_paged_append, handle.l2kv_paged_attn, handle.l2kv_pages_fork, handle.l2kv_pages_reserve,
-                handle.l2kv_pages_release, handle.l2kv_paged_compress, handle.l2kv_norm_rotary_append)))
+                handle.l2kv_pages_release, handle.l2kv_paged_compress, handle.l2kv_norm_rotary_append,
+                handle.l2kv_paged_append_reserved)))
         except ImportError as e:
             warnings.warn("%s; calls go through ctypes (build with `python -m paper_2406_11430_amd.build`)" % e, RuntimeWarning)
             module = _PythonCalls
@@ -777,17 +784,41 @@ def l2kv_paged_append(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tenso
                                         lens_out, q_weight, k_weight, eps, layout, amplitude, stream, _stream)
     if st is not None:
         return _check("l2kv_paged_append", st)
+    upto_lens_in, behind = _paged_append_arguments(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size,
+                                                   lens_in, None, lens_out, q_weight, k_weight, eps, layout, amplitude)
+    _check("l2kv_paged_append", lib().l2kv_paged_append(*upto_lens_in, *behind, _stream(stream)))
+
+
+def l2kv_paged_append_reserved(Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor,
+                               Qr: Optional[torch.Tensor], Kc: torch.Tensor, Vc: torch.Tensor, norms_c: torch.Tensor, pos_c: torch.Tensor,
+                               token_offsets: torch.Tensor, page_table: torch.Tensor, page_size: int, lens_in: torch.Tensor,
+                               ends: Optional[torch.Tensor], lens_out: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                               k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, layout: int = L2KV_ROTARY_HALF,
+                               amplitude: float = 1.0, stream=None) -> None:
+    """l2kv_paged_append of the rows below ends ``[n_seq]`` int32 only, as l2kv_pages_reserve leaves them."""
+    st = (_calls or calls()).paged_append_reserved(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size,
+                                                 lens_in, ends, lens_out, q_weight, k_weight, eps, layout, amplitude, stream, _stream)
+    if st is not None:
+        return _check("l2kv_paged_append_reserved", st)
+    upto_lens_in, behind = _paged_append_arguments(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size,
+                                                   lens_in, ends, lens_out, q_weight, k_weight, eps, layout, amplitude)
+    _check("l2kv_paged_append_reserved", lib().l2kv_paged_append_reserved(*upto_lens_in, _ptr(ends), *behind, _stream(stream)))
+
+
+def _paged_append_arguments(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size, lens_in, ends, lens_out,
+                            q_weight, k_weight, eps, layout, amplitude):
+    """Checked and marshalled, what is before the ends of rows and what is behind them."""
     total, Hkv, D, Hq, strides, slots = _append_shapes(Q, K, V, q_weight, k_weight, positions, freqs, Qr, Kc, Vc, norms_c, pos_c)
-    _dev(token_offsets, lens_in, lens_out)
+    _dev(token_offsets, lens_in, ends, lens_out)
     n_seq, max_pages, n_pages = _page_table(page_table, page_size, slots)
     _i64(token_offsets, n_seq + 1), _i32(lens_in, n_seq)
-    if lens_out is not None:
-        _i32(lens_out, n_seq)
-    _check("l2kv_paged_append", lib().l2kv_paged_append(
-        _ptr(Q), _ptr(K), _ptr(V), _dtype_code(K), total, Hq, Hkv, D, *strides, _ptr(q_weight), _ptr(k_weight), float(eps),
-        _ptr(positions), _ptr(freqs), 2 * freqs.numel(), int(layout), float(amplitude), n_seq, _ptr(token_offsets), _ptr(page_table),
-        max_pages, int(page_size), n_pages, _ptr(lens_in), _ptr(lens_out), _ptr(Qr), _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c),
-        _stream(stream)))
+    for t in (ends, lens_out):
+        if t is not None:
+            _i32(t, n_seq)
+    return ((_ptr(Q), _ptr(K), _ptr(V), _dtype_code(K), total, Hq, Hkv, D, *strides, _ptr(q_weight), _ptr(k_weight), float(eps),
+             _ptr(positions), _ptr(freqs), 2 * freqs.numel(), int(layout), float(amplitude), n_seq, _ptr(token_offsets), _ptr(page_table),
+             max_pages, int(page_size), n_pages, _ptr(lens_in)),
+            (_ptr(lens_out), _ptr(Qr), _ptr(Kc), _ptr(Vc), _ptr(norms_c), _ptr(pos_c)))
 
 
 def l2kv_paged_attn_workspace_bytes(n_seq: int, Hq: int, Hkv: int, total_q: int, max_kv: int, D: int, dtype) -> int:

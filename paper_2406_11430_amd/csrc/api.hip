@@ -491,7 +491,7 @@ static l2kv_status rotary_append(RotaryArgs a, l2kv_dtype dt, int32_t D, l2kv_ro
     if (!aligned(a.Q, 16) || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Qr, 16) || !aligned(a.Kc, 16) || !aligned(a.Vc, 16) ||
         !aligned(a.norms_c, 4) || !aligned(a.pos_c, 4) || !aligned(a.positions, 4) || !aligned(a.freqs, 8) || !aligned(a.token_off, 8) ||
         !aligned(a.slot_off, 8) || !aligned(a.lens_in, 4) || !aligned(a.lens_out, 4) || !aligned(a.q_weight, 4) || !aligned(a.k_weight, 4) ||
-        !aligned(a.page_table, 4))
+        !aligned(a.page_table, 4) || !aligned(a.ends, 4))
         return L2KV_ERR_ALIGN;
     return rotary_dispatch(a, dt, D, layout == L2KV_ROTARY_INTERLEAVED, static_cast<hipStream_t>(stream));
 }
@@ -551,6 +551,25 @@ l2kv_status l2kv_rotary_append(const void* Q, const void* K, const void* V, l2kv
                                    norms_c, pos_c, stream);
 }
 
+l2kv_status l2kv_paged_append_reserved(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
+                                       int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
+                                       const int32_t* positions, const double* freqs, int32_t rot_dim,
+                                       l2kv_rotary_layout layout, double amplitude, int32_t n_seq,
+                                       const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
+                                       int32_t page_size, int32_t n_pages, const int32_t* lens_in, const int32_t* ends,
+                                       int32_t* lens_out, void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
+    if (rotary_null(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c) || token_offsets == nullptr || page_table == nullptr ||
+        lens_in == nullptr)
+        return L2KV_ERR_NULL;
+    if (dtype_ok(dt) && (!pages_ok(n_seq, max_pages, page_size, n_pages) || (ends != nullptr && ends == lens_out))) return L2KV_ERR_SHAPE;
+    RotaryArgs a = rotary_args(Q, K, V, total_tokens, Hq, Hkv, q_stride, k_stride, v_stride, q_weight, k_weight, eps, positions, freqs, rot_dim,
+                               amplitude, n_seq, token_offsets, lens_in, lens_out, Qr, Kc, Vc, norms_c, pos_c);
+    a.page_table = page_table, a.ends = ends, a.max_pages = max_pages, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
+    a.total_slots = static_cast<int64_t>(n_pages) * page_size;
+    return rotary_append(a, dt, D, layout, stream);
+}
+
 l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_dtype dt, int64_t total_tokens,
                               int32_t Hq, int32_t Hkv, int32_t D, int64_t q_stride, int64_t k_stride,
                               int64_t v_stride, const float* q_weight, const float* k_weight, double eps,
@@ -559,15 +578,9 @@ l2kv_status l2kv_paged_append(const void* Q, const void* K, const void* V, l2kv_
                               const int64_t* token_offsets, const int32_t* page_table, int32_t max_pages,
                               int32_t page_size, int32_t n_pages, const int32_t* lens_in, int32_t* lens_out,
                               void* Qr, void* Kc, void* Vc, float* norms_c, int32_t* pos_c, void* stream) {
-    if (rotary_null(Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c) || token_offsets == nullptr || page_table == nullptr ||
-        lens_in == nullptr)
-        return L2KV_ERR_NULL;
-    if (dtype_ok(dt) && !pages_ok(n_seq, max_pages, page_size, n_pages)) return L2KV_ERR_SHAPE;
-    RotaryArgs a = rotary_args(Q, K, V, total_tokens, Hq, Hkv, q_stride, k_stride, v_stride, q_weight, k_weight, eps, positions, freqs, rot_dim,
-                               amplitude, n_seq, token_offsets, lens_in, lens_out, Qr, Kc, Vc, norms_c, pos_c);
-    a.page_table = page_table, a.max_pages = max_pages, a.n_pages = n_pages, a.page_shift = page_shift_of(page_size);
-    a.total_slots = static_cast<int64_t>(n_pages) * page_size;
-    return rotary_append(a, dt, D, layout, stream);
+    return l2kv_paged_append_reserved(Q, K, V, dt, total_tokens, Hq, Hkv, D, q_stride, k_stride, v_stride, q_weight, k_weight, eps, positions, freqs,
+                                      rot_dim, layout, amplitude, n_seq, token_offsets, page_table, max_pages, page_size, n_pages, lens_in, nullptr,
+                                      lens_out, Qr, Kc, Vc, norms_c, pos_c, stream);
 }
 
 // Sizes shared by the two attentions of many query rows, and by their workspaces.

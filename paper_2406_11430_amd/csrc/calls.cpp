@@ -25,6 +25,7 @@ decltype(&l2kv_tree_attn) tree_attn_entry = nullptr;
 decltype(&l2kv_stream_append_path) append_path_entry = nullptr;
 decltype(&l2kv_norm_rotary_append) norm_rotary_append_entry = nullptr;
 decltype(&l2kv_paged_append) paged_append_entry = nullptr;
+decltype(&l2kv_paged_append_reserved) paged_append_reserved_entry = nullptr;
 decltype(&l2kv_paged_attn) paged_attn_entry = nullptr;
 decltype(&l2kv_pages_fork) pages_fork_entry = nullptr;
 decltype(&l2kv_pages_reserve) pages_reserve_entry = nullptr;
@@ -465,9 +466,9 @@ Cache cache_of(Arguments& a) {
 }
 
 // (Q, K, V, positions, freqs, Qr, Kc, Vc, norms_c, pos_c, token_offsets, page_table, page_size, lens_in, lens_out, q_weight, k_weight, eps,
-// layout, amplitude, stream, stream's handle)
-PyObject* paged_append_checked(PyObject* const* args, Py_ssize_t n_args) {
-    if (n_args != 22) Py_RETURN_NONE;
+// layout, amplitude, stream, stream's handle); kReserved: ends behind lens_in
+template <bool kReserved> PyObject* paged_append_checked(PyObject* const* args, Py_ssize_t n_args) {
+    if (n_args != (kReserved ? 23 : 22)) Py_RETURN_NONE;
     Arguments a{args};
     int64_t q_stride = 0, k_stride = 0, v_stride = 0, Hq = 0;
     l2kv_dtype dt;
@@ -497,6 +498,10 @@ PyObject* paged_append_checked(PyObject* const* args, Py_ssize_t n_args) {
     int64_t n_pages;
     const int64_t size = page_size_of(a, c.slots, &n_pages);
     const int32_t* const lens_in = a.ints(table.n_seq);
+    const int32_t* ends = nullptr;
+    if constexpr (kReserved) {
+        if (!a.none()) ends = a.ints(table.n_seq);
+    }
     int32_t* const lens_out = a.none() ? nullptr : a.ints(table.n_seq);
     const float* const q_weight = a.none() ? nullptr : a.data<float>(at::kFloat, D);
     const float* const k_weight = a.none() ? nullptr : a.data<float>(at::kFloat, D);
@@ -513,6 +518,11 @@ PyObject* paged_append_checked(PyObject* const* args, Py_ssize_t n_args) {
     void* s;
     if (!a.stream(&s)) return nullptr;
     return status_of([&] {
+        if constexpr (kReserved)
+            return paged_append_reserved_entry(q, k, v, dt, total, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, q_stride, k_stride, v_stride, q_weight, k_weight,
+                                               eps, positions, f, rot_dim, (l2kv_rotary_layout)layout, amplitude, (int32_t)table.n_seq, token_off,
+                                               table.pages, (int32_t)table.max_pages, (int32_t)size, (int32_t)n_pages, lens_in, ends, lens_out, Qr, c.Kc,
+                                               c.Vc, c.norms, c.pos, s);
         return paged_append_entry(q, k, v, dt, total, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, q_stride, k_stride, v_stride, q_weight, k_weight, eps,
                                   positions, f, rot_dim, (l2kv_rotary_layout)layout, amplitude, (int32_t)table.n_seq, token_off, table.pages,
                                   (int32_t)table.max_pages, (int32_t)size, (int32_t)n_pages, lens_in, lens_out, Qr, c.Kc, c.Vc, c.norms, c.pos, s);
@@ -665,7 +675,8 @@ PyObject* paged_compress_checked(PyObject* const* args, Py_ssize_t n_args) {
     });
 }
 
-PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_append_checked(a, n); }); }
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_append_checked<false>(a, n); }); }
+PyObject* paged_append_reserved(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_append_checked<true>(a, n); }); }
 PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return paged_attn_checked(a, n); }); }
 PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return pages_fork_checked(a, n); }); }
 PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return pages_reserve_checked(a, n); }); }
@@ -678,12 +689,13 @@ PyObject* norm_rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) { retu
 PyObject* append_path(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return append_path_checked(a, n); }); }
 
 PyObject* bind(PyObject*, PyObject* args) {
-    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path, append, paged, fork, reserve, release, compact, norm;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path, &append, &paged, &fork, &reserve,
-                          &release, &compact, &norm))
+    unsigned long long attn, attn_out, comp, count, rotary, prompt, tree, path, append, paged, fork, reserve, release, compact, norm, reserved;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKKKK", &attn, &attn_out, &comp, &count, &rotary, &prompt, &tree, &path, &append, &paged, &fork, &reserve,
+                          &release, &compact, &norm, &reserved))
         return nullptr;
     norm_rotary_append_entry = reinterpret_cast<decltype(norm_rotary_append_entry)>(norm);
     paged_append_entry = reinterpret_cast<decltype(paged_append_entry)>(append);
+    paged_append_reserved_entry = reinterpret_cast<decltype(paged_append_reserved_entry)>(reserved);
     paged_attn_entry = reinterpret_cast<decltype(paged_attn_entry)>(paged);
     pages_fork_entry = reinterpret_cast<decltype(pages_fork_entry)>(fork);
     pages_reserve_entry = reinterpret_cast<decltype(pages_reserve_entry)>(reserve);
@@ -710,6 +722,7 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"append_path", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_path)), METH_FASTCALL, nullptr},
                          {"norm_rotary_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_rotary_append)), METH_FASTCALL, nullptr},
                          {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+                         {"paged_append_reserved", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append_reserved)), METH_FASTCALL, nullptr},
                          {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attn)), METH_FASTCALL, nullptr},
                          {"pages_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_fork)), METH_FASTCALL, nullptr},
                          {"pages_reserve", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(pages_reserve)), METH_FASTCALL, nullptr},

@@ -163,9 +163,10 @@ struct RotaryArgs {
     int64_t total_tokens, total_slots, q_stride, k_stride, v_stride;      // strides of tokens, in elements
     double amplitude;
     int32_t n_seq, Hq, Hkv, rot, tokens_per_block;
-    // weights of the norm of queries and of keys (NULL: none), and the pages that slots are found by (NULL: slot_off)
+    // weights of the norm of queries and of keys (NULL: none), the pages that slots are found by (NULL: slot_off), and with pages
+    // the rows at which sequences end whatever pages they have (NULL: they do not)
     const float *q_weight, *k_weight;
-    const int32_t* page_table;
+    const int32_t *page_table, *ends;
     double eps;
     int32_t max_pages, n_pages, page_shift;
 };

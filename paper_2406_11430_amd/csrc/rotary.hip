@@ -56,7 +56,7 @@ template <bool kMore> __device__ __forceinline__ int64_t token_slot(const Rotary
     if constexpr (kMore) {
         if (a.page_table != nullptr) {
             const int64_t row = have + at, index = row >> a.page_shift;
-            if (index >= a.max_pages) return kNoSlot;
+            if (index >= a.max_pages || (a.ends != nullptr && row >= a.ends[lo])) return kNoSlot;
             const int32_t page = a.page_table[(int64_t)lo * a.max_pages + index];
             return page < 0 || page >= a.n_pages ? kNoSlot : ((int64_t)page << a.page_shift) + (row & ((1 << a.page_shift) - 1));
         }
@@ -66,7 +66,7 @@ template <bool kMore> __device__ __forceinline__ int64_t token_slot(const Rotary
 }
 
 // Where sequences s0 .. s0 + 63 end after the call, a lane each (in the last lane the first): as far as there is room, and in pages only as
-// far as there are pages.  Of new rows in many pages the whole wave looks for one that is missing (32768 tokens of 32 + 8 + 8 heads of 128 in pages
+// far as there are pages and as the sequence's end allows.  Of new rows in many pages the whole wave looks for one that is missing (32768 tokens of 32 + 8 + 8 heads of 128 in pages
 // of 16, one entry after the other by a single lane: 390 us, 168 so).
 constexpr int64_t kFewPages = 4;
 template <bool kMore> __device__ __forceinline__ void write_lens(const RotaryArgs& a, int64_t s0, int lane) {
@@ -90,7 +90,8 @@ template <bool kMore> __device__ __forceinline__ void write_lens(const RotaryArg
                     missing = __ballot(i + lane >= count || !held(e0 + i + lane));
                 if (lane == whose) there = i;                      // what is behind the last entry counts as missing
             }
-            const int64_t room = (first + there) << a.page_shift, end = have + n < room ? have + n : room;
+            const int64_t pages = (first + there) << a.page_shift, given = mine && a.ends != nullptr ? a.ends[s] : pages;
+            const int64_t room = given < pages ? given : pages, end = have + n < room ? have + n : room;
             if (mine) a.lens_out[s] = (int32_t)(end > have ? end : have);
             return;
         }
