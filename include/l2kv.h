@@ -743,8 +743,10 @@ size_t l2kv_pages_workspace_bytes(int64_t n_pages);
  * lower row is the earlier token and ties go to it, as in l2kv_select.
  *   Kc, Vc, norms_c, pos_c: [n_planes][n_pages*page_size], read and written; the pages of table_out must not be those of
  *             table_in (l2kv_pages_reserve before, l2kv_pages_release behind); pages that several sequences hold are only read
- *   table_in [n_seq][max_in], lens_in, keep [n_seq]; table_out [n_seq][max_out], lens_out [n_seq] = rows kept (capped at the
- *             pages' room; rows whose entry is no page are not written).  lens_out must not be an input.
+ *   table_in [n_seq][max_in], lens_in, keep [n_seq]; table_out [n_seq][max_out], lens_out [n_seq] = rows kept, at most
+ *             max_out * page_size.  A row whose entry of table_out is no page is counted and not written, so where room may have been
+ *             refused, keep is what the reservation of it (from 0 to the rows to be kept) left in its ends: a sequence
+ *             without room then keeps no row in table_out, and its rows stay in table_in.  lens_out must not be an input.
  *   total_rows, total_kept: upper bounds of the sums of lens_in and of the rows kept (size the workspace and the launches;
  *             what goes beyond them is left out); total_kept < 2^28
  *   max_len : an upper bound of lens_in, at most total_rows (chooses the kernel variant; rows beyond it are left out)

@@ -144,3 +144,49 @@ def test_a_captured_loop_that_runs_out():
             check(O[s:s + 1], attend(Qr[s:s + 1], p.Kc[:, at], p.Vc[:, at], torch.ones((1, m), dtype=torch.bool, device=DEV)), m)
         want = more
     assert int(p.count) == 0 and want == [48, 32, 32]
+
+
+@pytest.mark.parametrize("dtype,D", ROWS)
+@pytest.mark.parametrize("spare,served", [(4, [True, False, False]), (2, [False, False, False]), (7, [True, True, True]), (6, [True, True, False])])
+def test_a_compaction_that_gets_no_room(dtype, D, spare, served):
+    """The ends of the reservation are what is kept: sequences that got no room keep nothing in the new table and all in the old one, and go on
+    from it, a token each."""
+    page, Hq, Hkv, have, want = 16, 4, 2, [90, 64, 40], [45, 32, 20]
+    p = Pool(6 + 4 + 3 + spare, page, Hkv, D, dtype)
+    t = p.init(3, 7)
+    p.reserve(t, [0] * 3, have)
+    cache = (p.Kc, p.Vc, p.norms, p.pos)
+    p.norms.square_()
+    lens, keep, zero, ends, lens_new, out = ints(have), ints(want), ints([0] * 3), ints([0] * 3), ints([0] * 3), ints([0] * 3)
+    new = torch.full_like(t, -1)
+    old = [slots_of(row, n, page).to(DEV) for row, n in zip(t.tolist(), have)]
+    was = [x.clone() for x in cache]
+
+    def reserve(table, first, to):
+        l2kv.l2kv_pages_reserve(table, first, to, ends, p.refs, p.free, p.count, page, *cache, p.ws)
+    reserve(new, zero, keep)
+    ws = torch.empty(l2kv.l2kv_paged_compress_workspace_bytes(Hkv, 3, sum(have), sum(want)), dtype=torch.uint8, device=DEV)
+    l2kv.l2kv_paged_compress(*cache, t, lens, ends, new, lens_new, page, sum(have), sum(want), max(have), ws)
+    there = ends == keep
+    l2kv.l2kv_pages_release(t, torch.where(there, 0, lens).int(), p.refs, p.free, p.count, page, p.ws)
+    table, lens = torch.where(there[:, None], new, t), torch.where(there, lens_new, lens).int()
+    # one more token of each; what compaction gave back is enough for it where there was a compaction
+    reserve(table, lens, lens + 1)
+    Q, K, V = inputs(3, 3, Hq, Hkv, D, dtype)
+    Qr, freqs = torch.empty((3, Hq, D), dtype=dtype, device=DEV), l2kv.l2kv_rotary_freqs(D).to(DEV)
+    l2kv.l2kv_paged_append_reserved(Q, K, V, lens, freqs, Qr, *cache, offsets([1] * 3), table, page, lens, ends, out)
+    O = attention(Qr, p, [1] * 3, table, out, 91)
+
+    assert there.tolist() == served and lens_new.tolist() == [w if x else 0 for w, x in zip(want, served)]
+    before = [w if x else h for h, w, x in zip(have, want, served)]
+    assert lens.tolist() == before and out.tolist() == [n + 1 for n in before]
+    for s, n in enumerate(before):
+        at = slots_of(table[s].tolist(), n + 1, page).to(DEV)
+        for h in range(Hkv):
+            rows = old[s]
+            if served[s]:
+                rows = rows[torch.sort(was[2][h, rows], stable=True).indices[:n].sort().values]
+            for x, y in zip(cache, was):
+                assert torch.equal(x[h, at[:n]], y[h, rows])
+        assert torch.equal(p.Vc[:, at[n]], V[s])
+        check(O[s:s + 1], attend(Qr[s:s + 1], p.Kc[:, at], p.Vc[:, at], torch.ones((1, n + 1), dtype=torch.bool, device=DEV)), n + 1)
