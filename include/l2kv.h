@@ -670,7 +670,14 @@ l2kv_status l2kv_paged_append_reserved(const void* Q, const void* K, const void*
  *               rows beyond it are still attended to)
  *   O     out : [total_q][Hq][D], dense, of type dt
  *   workspace : l2kv_paged_attn_workspace_bytes(...), as for l2kv_prompt_attn, with the same bound for all sizes
- * Arithmetic and errors: as l2kv_prompt_attn; SHAPE for page_size, max_pages, n_pages and where n_seq * max_pages exceeds 2^31-1.
+ * How a batch is worked on goes by its sizes, which are all that the host knows of it:
+ *   total_q <= n_seq: as a decode step, every token by itself.  Softmax weights are held in fp32 for both types (as in
+ *             l2kv_decode_attn*), so O is off by its own rounding alone.  A sequence with several tokens has its rows read for each of them:
+ *             a chunk among places without tokens belongs into a call without those places.
+ *   total_q > n_seq : as chunks, the rows of a sequence once for a block of tokens.  Arithmetic as l2kv_prompt_attn, bf16 weights rounded for the
+ *             matrix unit, for the single tokens of such a batch as well: the same token may differ in its last bits between the two.
+ *   more than 1024 sequences: an item for each (block of tokens, KV head) and none is cut, so one that is far longer than the others runs long.
+ * Otherwise arithmetic and errors: as l2kv_prompt_attn; SHAPE for page_size, max_pages, n_pages and where n_seq * max_pages exceeds 2^31-1.
  */
 l2kv_status l2kv_paged_attn(const void* Q, const void* Kc, const void* Vc, l2kv_dtype dt, int32_t n_seq, int32_t Hq,
                             int32_t Hkv, int32_t D, int64_t total_q, int64_t q_stride, const int64_t* q_offsets,
