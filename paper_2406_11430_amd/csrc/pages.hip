@@ -9,7 +9,8 @@
 // 1024 sequences and 2048 entries at a time; up to 8192 entries stay in LDS from phase to phase.  It is bound by the
 // memory round trips that follow one another and by the fetch of its own instructions.  The copies are a launch of their own behind it.
 // One more row for each of 64 sequences 8 us with the (empty) copy; release, fork and reservation of 32 branches of 1000 to 2000 rows with 34 MB copied, 32 us:
-// 5 + 2 + 7 and the copy 13, at 5.2 TB/s.
+// 5 + 2 + 7 and the copy 13, at 5.2 TB/s.  A reservation is one workgroup's whatever its size, and grows with it: 64 new sequences of 64 pages 24 us, of 140
+// 49, of 250 (beyond what LDS keeps) 79, of 8192 2300; one of 8192 40.  (Releases of that many are spread: pages_release_begin_kernel.)
 #include "l2kv_device.hpp"
 #include "l2kv_host.hpp"
 
@@ -532,8 +533,8 @@ void pages_release_kernel(const PagesArgs a, const int32_t* __restrict__ keep, v
     if (threadIdx.x == 0) *a.free_count = have + all < a.n_pages ? have + all : a.n_pages;
 }
 
-// The same for large tables, by many workgroups with a stretch of the table each and a launch for every phase (64 sequences of 8192 pages,
-// with their reservation: 1400 us by one workgroup).
+// The same for large tables, by many workgroups with a stretch of the table each and a launch for every phase: 64 sequences of 8192 pages 24 us,
+// of 140 or 250 18.
 struct LargeRelease {
     int32_t *have, *counts;                // free pages before, pages freed by each workgroup
     __device__ __forceinline__ explicit LargeRelease(const PagesScratch& w) : have(w.n_copies + 1), counts(reinterpret_cast<int32_t*>(w.copies)) {}

@@ -45,7 +45,9 @@ template <int kRowBytes> static ShapeSizes shape_sizes(int shape) {
 constexpr int kTokens = 3;                 // the shape of such launches
 // The rows at which both take as long go by what a row costs a workgroup, its bytes and the heads it is for: bf16 D 128 with groups of 1 800, of 8
 // 470, D 64 of 8 780, D 256 of 3 380, fp32 D 128 of 7 340; twice as many where there are
-// items for all compute units.  Over 140 sizes what this chooses takes 1.4 % longer than the better of the two (512 and 1024 rows for all: 3.5 %).
+// items for all compute units.  How the tokens are spread over the sequences is not known here: a batch of 256 places of which one has 200 tokens over
+// 8000 rows takes 807 us, that chunk alone 57; 16 of 64 sequences with 4 tokens each over 4000 rows 170 and 48.  1025 sequences, one of 131072 rows and the
+// others of 100, 1860 us, 1024 of them in stretches 250.  Over 140 sizes what this chooses takes 1.4 % longer than the better of the two (512 and 1024 rows for all: 3.5 %).
 static int64_t token_own_rows(int32_t G, int row_bytes, bool many) {
     const int64_t few = 900 * 9 * 256 / ((row_bytes < 192 ? 192 : row_bytes) * (8 + G));
     return many ? 2 * few : few;

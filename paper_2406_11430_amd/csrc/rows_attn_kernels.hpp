@@ -1,4 +1,5 @@
-// Kernels of l2kv_prompt_attn and l2kv_tree_attn: attention of many query rows, packed over sequences.
+// Kernels of l2kv_prompt_attn, l2kv_tree_attn and, where sequences have several new tokens, l2kv_paged_attn: attention of many query rows,
+// packed over sequences, over rows that lie one behind the other or in pages.
 //
 // The G query heads of a KV head are rows of one problem: row r of a block is token r / G, head r % G, so K and V are read once for all of
 // them.  An item is one block of rows of one (sequence, KV head) over all keys that it sees.  A launch either has one workgroup per item
@@ -281,6 +282,14 @@ template <typename E, int D, int kRows, int kWaves> struct TilePages {
 // busy for 55 % of the cycles, exponentials, maxima and roundings for 46, and the clock falls as they are busier.  A prompt of 32768 tokens (32 query heads, 8 KV heads) takes 7.7 to 8.4 ms
 // from card to card, 1.05 to 1.14 PFLOP/s of the 1.37 that a large matrix product reaches.  Batches of trees are bound by memory:
 // 64 of 1 to 32 nodes over 500 to 4000 rows 119 to 121 us, 5.1 TB/s (a large copy: 4.80).
+//
+// Chunks over pages by row type, 4096 tokens at the end of 32768, 32 query heads, 8 KV heads; share of the SIMDs' cycles that the matrix unit and the
+// vector unit (4 cycles an instruction, 16 an exponential) are busy:
+//   bf16 D 128  1.82 to 2.03 ms  1.0 to 1.1 PFLOP/s  51 %, 50 %: softmax and products, as in prompts
+//   bf16 D 64   1.16 ms          0.89                37 %, 67 %: the softmax of a score costs the same and its products half
+//   bf16 D 256  4.06 ms          1.02                43 %, 36 %: waits; registers for 32 keys a tile, whose values are read behind the softmax
+//   fp32 D 128  15.6 ms          0.132               85 %, 8 %: the matrix unit (a large fp32 product: 0.154)
+//   fp32 D 64   7.85 ms          0.131               84 %, 10 %: the same
 template <typename E, int D, int kWR, int kWK, int kNK, int kStages, int kKind, bool kOnce>
 __global__ __launch_bounds__(kWaveSize * kWR * kWK, 2)
 void rows_attn_kernel(const RowsArgs a) {

@@ -12,7 +12,9 @@
 //
 // Bound by memory: 64 sequences of 500 to 4000 rows (bf16, D 128, 8 KV heads of 4 query heads) 102 us, 5.8 TB/s, of which the stream takes 95 and the join
 // 4; one of 131072 rows 89 us, 6.0 TB/s (a bare read: 7.2).  One of 2048 rows with 32 KV heads 12 us: launch, three loads that wait for one
-// another, 34 MB, join.  The kernel of many rows (loads to LDS, products on the matrix unit) takes 116 to 160 us for the first of these in eight shapes.
+// another, 34 MB, join.  Other rows and groups, the same 64 sequences, TB/s: bf16 D 64 with groups of 1, 4, 8 5.7, 5.1, 3.8 (products on the vector
+// unit), D 128 6.2, 5.8, 5.3, D 256 with 1 to 4 6.5, 6.4, 6.4, 6.2; fp32 D 64 with 1, 4, 8 6.2, 6.1, 5.2, D 128 with 1, 4, 6, 8 6.5, 6.4, 6.2, 5.9: one wave a
+// SIMD is enough for the long rows.  The kernel of many rows (loads to LDS, products on the matrix unit) takes 116 to 160 us for the first of these in eight shapes.
 #pragma once
 
 #include "decode_kernels.hpp"
@@ -217,80 +219,80 @@ void token_attn_kernel(const RowsArgs a) {
             // Query heads at a time, whose scores and weights are in registers together: half of 5 to 8 (64 sequences of 500 to 4000 rows, 8 KV heads
             // of 8 query heads 134 us, 128 so).
             if constexpr (!kMfma) {
-            constexpr int kPass = G > 4 ? (G + 1) / 2 : G;
-            if (last) hide(t, first);
+                constexpr int kPass = G > 4 ? (G + 1) / 2 : G;
+                if (last) hide(t, first);
 #pragma unroll
-            for (int g0 = 0; g0 < G; g0 += kPass) {
-                float s[kPass][kDecLoads], p[kPass][kDecLoads];
+                for (int g0 = 0; g0 < G; g0 += kPass) {
+                    float s[kPass][kDecLoads], p[kPass][kDecLoads];
 #pragma unroll
-                for (int u = 0; u < kDecLoads; ++u) {
-                    float kx[kBf16 ? 1 : EPL];
-                    if constexpr (!kBf16) widen_words<E, W>(t.k[u], kx);
+                    for (int u = 0; u < kDecLoads; ++u) {
+                        float kx[kBf16 ? 1 : EPL];
+                        if constexpr (!kBf16) widen_words<E, W>(t.k[u], kx);
 #pragma unroll
-                    for (int i = 0; i < kPass; ++i) {
-                        if (g0 + i >= G) continue;
-                        float x;
-                        if constexpr (kBf16) {
-                            x = dot2_bf16(qw[g0 + i][0], t.k[u].w[0], 0.f);
+                        for (int i = 0; i < kPass; ++i) {
+                            if (g0 + i >= G) continue;
+                            float x;
+                            if constexpr (kBf16) {
+                                x = dot2_bf16(qw[g0 + i][0], t.k[u].w[0], 0.f);
 #pragma unroll
-                            for (int w = 1; w < W; ++w) x = dot2_bf16(qw[g0 + i][w], t.k[u].w[w], x);
-                        } else {
-                            x = qf[g0 + i][0] * kx[0];
+                                for (int w = 1; w < W; ++w) x = dot2_bf16(qw[g0 + i][w], t.k[u].w[w], x);
+                            } else {
+                                x = qf[g0 + i][0] * kx[0];
 #pragma unroll
-                            for (int e = 1; e < EPL; ++e) x = fmaf(qf[g0 + i][e], kx[e], x);
+                                for (int e = 1; e < EPL; ++e) x = fmaf(qf[g0 + i][e], kx[e], x);
+                            }
+                            s[i][u] = x;
                         }
-                        s[i][u] = x;
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < kPass; ++i)
+                    for (int i = 0; i < kPass; ++i)
 #pragma unroll
-                    for (int u = 0; u < kDecLoads; ++u)
-                        if (g0 + i < G) s[i][u] = row_tree_sum<kLanesPerRow>(s[i][u]);
-                if (last) {
+                        for (int u = 0; u < kDecLoads; ++u)
+                            if (g0 + i < G) s[i][u] = row_tree_sum<kLanesPerRow>(s[i][u]);
+                    if (last) {
 #pragma unroll
-                    for (int u = 0; u < kDecLoads; ++u) {
-                        const bool there = first + (u * kRowsPerWaveLoad + rg) * Geo::kRowsPerSlot + c / kLanesPerRow < n;
+                        for (int u = 0; u < kDecLoads; ++u) {
+                            const bool there = first + (u * kRowsPerWaveLoad + rg) * Geo::kRowsPerSlot + c / kLanesPerRow < n;
 #pragma unroll
-                        for (int i = 0; i < kPass; ++i)
-                            if (g0 + i < G) s[i][u] = there ? s[i][u] : -INFINITY;
+                            for (int i = 0; i < kPass; ++i)
+                                if (g0 + i < G) s[i][u] = there ? s[i][u] : -INFINITY;
+                        }
                     }
-                }
-#pragma unroll
-                for (int i = 0; i < kPass; ++i) {
-                    const int g = g0 + i;
-                    if (g >= G) continue;
-                    float top = s[i][0];
-#pragma unroll
-                    for (int u = 1; u < kDecLoads; ++u) top = fmaxf(top, s[i][u]);
-                    const float mn = fmaxf(m[g], top * a.scale);
-                    const float alpha = fast_exp2(m[g] - mn);
-                    m[g] = mn;
-                    asm volatile("" : "+v"(m[g]));                     // one head after the other, as in decode_item
-                    l[g] *= alpha;
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) acc[g][e] *= alpha;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int u = 0; u < kDecLoads; ++u) {
-                        p[i][u] = fast_exp2(fmaf(s[i][u], a.scale, -m[g]));
-                        sum += p[i][u];
-                    }
-                    l[g] += sum;
-                }
-#pragma unroll
-                for (int u = 0; u < kDecLoads; ++u) {
-                    float vx[EPL];
-                    widen_words<E, W>(t.v[u], vx);
 #pragma unroll
                     for (int i = 0; i < kPass; ++i) {
-                        if (g0 + i >= G) continue;
+                        const int g = g0 + i;
+                        if (g >= G) continue;
+                        float top = s[i][0];
 #pragma unroll
-                        for (int e = 0; e < EPL; ++e) acc[g0 + i][e] = fmaf(p[i][u], vx[e], acc[g0 + i][e]);
+                        for (int u = 1; u < kDecLoads; ++u) top = fmaxf(top, s[i][u]);
+                        const float mn = fmaxf(m[g], top * a.scale);
+                        const float alpha = fast_exp2(m[g] - mn);
+                        m[g] = mn;
+                        asm volatile("" : "+v"(m[g]));                     // one head after the other, as in decode_item
+                        l[g] *= alpha;
+#pragma unroll
+                        for (int e = 0; e < EPL; ++e) acc[g][e] *= alpha;
+                        float sum = 0.f;
+#pragma unroll
+                        for (int u = 0; u < kDecLoads; ++u) {
+                            p[i][u] = fast_exp2(fmaf(s[i][u], a.scale, -m[g]));
+                            sum += p[i][u];
+                        }
+                        l[g] += sum;
                     }
+#pragma unroll
+                    for (int u = 0; u < kDecLoads; ++u) {
+                        float vx[EPL];
+                        widen_words<E, W>(t.v[u], vx);
+#pragma unroll
+                        for (int i = 0; i < kPass; ++i) {
+                            if (g0 + i >= G) continue;
+#pragma unroll
+                            for (int e = 0; e < EPL; ++e) acc[g0 + i][e] = fmaf(p[i][u], vx[e], acc[g0 + i][e]);
+                        }
+                    }
+                    if (g0 + kPass < G) __builtin_amdgcn_sched_barrier(0);
                 }
-                if (g0 + kPass < G) __builtin_amdgcn_sched_barrier(0);
-            }
             }
         };
 
